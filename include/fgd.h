@@ -38,7 +38,8 @@
  *  - Device arrays are worker-major [M][ld] with ld >= P elements; element p
  *    of worker m is at index m * ld + p.  Each row must start on a 16-byte
  *    boundary (base pointer 16-byte aligned and ld * element size a multiple
- *    of 16).
+ *    of 16).  The fgd_mx4_* calls and fgd_sample take matrices and logits of
+ *    any element-aligned address and stride instead, as their notes say.
  *  - The caller owns every device buffer; the engine only borrows them for
  *    the work it enqueues, so they must stay alive until `stream` has passed
  *    that work.  Host arrays handed to the engine are copied before return.
@@ -54,13 +55,13 @@
  *  - The engine's compute calls are not meant to be recorded by HIP stream
  *    capture: a topology upload copies from a pinned host staging slot that
  *    later uploads reuse, after waiting on the slot's event from the host.
- *    fgd_js_distance, fgd_stream_js_pattern and fgd_stream_copy enqueue
- *    kernels only.
+ *    fgd_js_distance, the fgd_mx4_* calls, fgd_sample, fgd_stream_js_pattern
+ *    and fgd_stream_copy enqueue kernels only.
  *  - Engine calls run on the engine's device (fgd_config.device): they make
  *    it current for their duration and restore the caller's current device
- *    before returning.  The engine-free calls (fgd_js_distance,
- *    fgd_stream_js_pattern, fgd_stream_copy) run on the caller's current
- *    device.
+ *    before returning.  The engine-free calls (fgd_js_distance, the
+ *    fgd_mx4_* calls, fgd_sample, fgd_stream_js_pattern, fgd_stream_copy)
+ *    run on the caller's current device.
  */
 #ifndef FGD_H
 #define FGD_H
@@ -403,6 +404,134 @@ fgd_status fgd_js_distance(const void *logits_avg, const void *logits_workers, i
  * ((M + 1) U rows) and 4 KiB plus 4 bytes per token (either dtype).  Host
  * only. */
 fgd_status fgd_js_workspace_size(int32_t dtype, int32_t num_workers, int64_t num_tokens, int64_t *bytes);
+
+/* ---------------------------------------------------------------------
+ * Microscaled 4-bit floating point: a model's matrices in 4 bits, and
+ * products of them.
+ *
+ * A quantised matrix of `rows` x `cols` holds, for every 32 consecutive
+ * elements of a row (the last of a row may be fewer), one scale 2^(byte -
+ * 127) and for every element a 4-bit code.  With top the block's largest
+ * magnitude, byte = max(floor(log2 top) + 125, 0), and a code stands for the
+ * number of {0, 0.5, 1, 1.5, 2, 3, 4, 6} nearest to |x| / scale (of two
+ * equally near the one with an even code, which is its place in that list;
+ * above 6, 6), plus 8 for a negative x.  A block with an infinity or a NaN
+ * has byte 255 and stands for NaNs.  Reading back is exact: the values have
+ * two significant bits.
+ *
+ * Codes and scales lie in two arrays, in tiles of 64 rows x 128 columns of
+ * 4096 and 256 bytes, tile (r, k) of batch entry b at index (b * ceil(rows /
+ * 64) + r) * ceil(cols / 128) + k.  Element (i, 32 q + j) of a tile, q in
+ * [0, 4), is nibble j % 2 (low first) of byte (i / 16) * 1024 + (i % 16 + 16
+ * q) * 16 + j / 2 of the tile's codes, and its block's scale is byte (i % 16
+ * + 16 q) * 4 + i / 16 of the tile's scales.  Rows and columns past the
+ * matrix hold zeros.  Both arrays are 16-byte aligned.
+ *
+ * Every array of these calls is the caller's; outputs may overlap neither
+ * inputs nor each other; sizes of zero are allowed (there is nothing to
+ * write, or a product over no terms writes zeros).  `batch` matrices of one
+ * size are handled by one call, for instance every worker's.  Dense matrices
+ * have element strides and need only their element's alignment.  Equal calls
+ * on one device give equal bits; the order of a product's sums depends on its
+ * sizes, so the same rows in a call of other sizes may differ in the last
+ * bits of a float32 sum. */
+#define FGD_MX4_BLOCK 32
+
+/* Bytes of the code and the scale array of `batch` matrices.  Host only. */
+fgd_status fgd_mx4_size(int32_t batch, int64_t rows, int64_t cols, int64_t *code_bytes, int64_t *scale_bytes);
+
+/* Quantises x, whose element (b, r, k) is at b * batch_stride + r *
+ * row_stride + k * col_stride; row_stride or col_stride must be 1.  With
+ * row_stride = 1 the blocks run along the columns of the stored matrix, as
+ * the operands of a layer's gradients need them.
+ *   x               device, dtype FGD_F32 or FGD_BF16; any values
+ *   codes, scales   device, fgd_mx4_size bytes, 16-byte aligned
+ * Enqueued on `stream`. */
+fgd_status fgd_mx4_quantize(const void *x, int32_t dtype, int32_t batch, int64_t rows, int64_t cols,
+                            int64_t batch_stride, int64_t row_stride, int64_t col_stride, void *codes, void *scales,
+                            void *stream);
+
+/* Writes the values that codes and scales stand for to out, rows contiguous
+ * (element (b, r, k) at b * batch_stride + r * row_stride + k).  Exact in
+ * either dtype, but for bf16 values below its smallest normal number, which
+ * round to its denormals.  Enqueued on `stream`. */
+fgd_status fgd_mx4_dequantize(const void *codes, const void *scales, int32_t batch, int64_t rows, int64_t cols,
+                              void *out, int32_t dtype, int64_t batch_stride, int64_t row_stride, void *stream);
+
+/* out[b][i][j] = sum over k of a[b][i][k] w[b][j][k], both operands
+ * quantised along k: a is m x k, w is n x k, out m x n (rows contiguous).
+ * Products are exact and summed in float32 by the matrix instruction; one
+ * rounding to out_dtype.  A NaN block makes its row or column NaN.  Enqueued
+ * on `stream`. */
+fgd_status fgd_mx4_matmul(const void *a_codes, const void *a_scales, const void *w_codes, const void *w_scales,
+                          int32_t batch, int64_t m, int64_t n, int64_t k, void *out, int32_t out_dtype,
+                          int64_t out_batch_stride, int64_t out_row_stride, void *stream);
+
+/* A layer with 4-bit weights: quantises x (tokens x k, rows contiguous) as
+ * fgd_mx4_quantize would and multiplies as fgd_mx4_matmul would, giving the
+ * same bits as the two calls.
+ *   workspace   device memory of at least fgd_mx4_linear_workspace_size
+ *               bytes, 16-byte aligned, overlapping none of the arrays; left
+ *               undefined.  Calls that share one must not run concurrently.
+ * Enqueued on `stream`. */
+fgd_status fgd_mx4_linear(const void *x, int32_t x_dtype, int64_t x_batch_stride, int64_t x_row_stride,
+                          const void *w_codes, const void *w_scales, int32_t batch, int64_t tokens, int64_t n,
+                          int64_t k, void *out, int32_t out_dtype, int64_t out_batch_stride, int64_t out_row_stride,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Device workspace fgd_mx4_linear needs: its quantised x.  Host only. */
+fgd_status fgd_mx4_linear_workspace_size(int32_t batch, int64_t tokens, int64_t k, int64_t *bytes);
+
+#define FGD_MAX_SAMPLE_VOCAB (1 << 22) /* largest vocab of fgd_sample */
+
+/* Settings of fgd_sample.  A *_rows array (device, one value per row) takes
+ * the place of the scalar before it; NULL: the scalar holds for every row. */
+typedef struct {
+    uint32_t struct_size;          /* sizeof(fgd_sampling), checked for equality */
+    float temperature;             /* T; not above 0 (or NaN, or 1/T infinite): the most likely token */
+    const float *temperature_rows;
+    float top_p;                   /* below 1: keep the likeliest tokens whose mass reaches top_p */
+    float min_p;                   /* above 0: keep tokens at least min_p times as likely as the likeliest */
+    const float *top_p_rows;
+    const float *min_p_rows;
+    int32_t top_k;                 /* above 0: keep the top_k likeliest tokens */
+    int32_t reserved;              /* 0 */
+    const int32_t *top_k_rows;
+} fgd_sampling;
+
+/* Samples one token per row of logits, from one uniform random number per
+ * row.  The tokens of a row stand in descending order of their logits (equal
+ * logits: the lower index first); a token's weight is w = 2^t, t = (z - max
+ * z) * ((1 / T) * log2(e)), each operation rounded to float32, and its mass
+ * the whole number floor(w 2^31 + 1/2), so that all sums are exact.  top_k
+ * keeps the first top_k tokens; of these top_p keeps the tokens before which
+ * less than ceil(top_p * mass of the kept) lies (the first at least; a value
+ * of 1 or more, or NaN, keeps all); of these min_p keeps those with w >=
+ * min(min_p, 1) (NaN: all).  The token drawn is the first up to and with
+ * which more than floor(u * mass of the kept) lies.
+ *   logits      device [num_rows][ldk] FGD_F32 or FGD_BF16; -inf masks a
+ *               token; +inf takes all the mass (shared by all that are +inf)
+ *   vocab       V in [1, FGD_MAX_SAMPLE_VOCAB], V <= ldk; elements [V, ldk)
+ *               are never used
+ *   uniform     device float[num_rows], u in [0, 1) (values outside are
+ *               taken as the nearest inside, NaN as 0)
+ *   tokens_out  device int32[num_rows]: the token; -1 where every logit is
+ *               -inf or any is NaN
+ *   probs_out   device float[num_rows] or NULL: the token's mass over the
+ *               mass of the kept tokens; 0 where every logit is -inf, NaN
+ *               where any is NaN
+ *   workspace   device memory of at least fgd_sample_workspace_size bytes,
+ *               16-byte aligned (may be NULL where that is 0), overlapping
+ *               none of the arrays; left undefined.  Calls that share one
+ *               must not run concurrently.
+ * Enqueued on `stream`.  A row's result depends on its logits, settings and
+ * u alone. */
+fgd_status fgd_sample(const void *logits, int32_t dtype, int64_t num_rows, int64_t vocab, int64_t ldk,
+                      const float *uniform, const fgd_sampling *settings, int32_t *tokens_out, float *probs_out,
+                      void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Device workspace fgd_sample needs for these sizes.  Host only. */
+fgd_status fgd_sample_workspace_size(int32_t dtype, int64_t num_rows, int64_t vocab, int64_t *bytes);
 
 /* Streaming reference with the fused step's memory traffic and none of its
  * arithmetic: the tiles, lane vectors, cache hints and launch shape of

@@ -26,6 +26,7 @@ FGD_W_IDENTITY, FGD_W_GLOBAL_MEAN, FGD_W_CSR = 0, 1, 2
 FGD_REWEIGHT_NONE, FGD_REWEIGHT_METROPOLIS, FGD_REWEIGHT_SELF = 0, 1, 2
 FGD_MAX_WORKERS, FGD_MAX_ROUNDS, FGD_MAX_SUBSET_SEGMENTS = 64, 8, 4096
 FGD_MAX_JS_TOPK, FGD_MAX_JS_WORKERS = 1024, 4096
+FGD_MX4_BLOCK, FGD_MAX_SAMPLE_VOCAB = 32, 1 << 22
 
 DTYPES = {"f32": FGD_F32, "bf16": FGD_BF16}
 KINDS = {"identity": FGD_W_IDENTITY, "global": FGD_W_GLOBAL_MEAN, "csr": FGD_W_CSR}
@@ -82,6 +83,14 @@ def _load():
         "fgd_stream_step_pattern": (I32, [P, P, P, P, P]),
         "fgd_js_distance": (I32, [P, P, I32, I32, I64, I64, I64, I32, P, P, P, P, I64, P]),
         "fgd_js_workspace_size": (I32, [I32, I32, I64, ctypes.POINTER(I64)]),
+        "fgd_mx4_size": (I32, [I32, I64, I64, ctypes.POINTER(I64), ctypes.POINTER(I64)]),
+        "fgd_mx4_quantize": (I32, [P, I32, I32, I64, I64, I64, I64, I64, P, P, P]),
+        "fgd_mx4_dequantize": (I32, [P, P, I32, I64, I64, P, I32, I64, I64, P]),
+        "fgd_mx4_matmul": (I32, [P, P, P, P, I32, I64, I64, I64, P, I32, I64, I64, P]),
+        "fgd_mx4_linear": (I32, [P, I32, I64, I64, P, P, I32, I64, I64, I64, P, I32, I64, I64, P, I64, P]),
+        "fgd_mx4_linear_workspace_size": (I32, [I32, I64, I64, ctypes.POINTER(I64)]),
+        "fgd_sample": (I32, [P, I32, I64, I64, I64, P, P, P, P, P, I64, P]),
+        "fgd_sample_workspace_size": (I32, [I32, I64, I64, ctypes.POINTER(I64)]),
         "fgd_stream_js_pattern": (I32, [P, P, I32, I32, I64, I64, I64, P, I64, P]),
         "fgd_status_string": (ctypes.c_char_p, [I32]),
         "fgd_last_error": (ctypes.c_char_p, []),
@@ -565,3 +574,11 @@ class Engine:
 
     def read_timing(self):
         return fgd_read_timing(self.handle)
+
+
+# ------------------------------------- operators on matrices and logits
+
+from .mx4 import (Mx4, fgd_mx4_dequantize, fgd_mx4_linear, fgd_mx4_linear_workspace_size,  # noqa: E402
+                  fgd_mx4_matmul, fgd_mx4_quantize, fgd_mx4_size, mx4_dequantize, mx4_linear, mx4_linear_grads,
+                  mx4_matmul, mx4_quantize)
+from .sampling import fgd_sample, fgd_sample_workspace_size, fgd_sampling, sample  # noqa: E402

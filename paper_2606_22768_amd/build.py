@@ -33,7 +33,7 @@ HIP_SOURCES = ["engine.hip", "kernels_f32.hip", "kernels_bf16.hip", "kernels_f32
                "kernels_f32_split.hip", "kernels_bf16_split.hip", "kernels_f32_class.hip", "kernels_bf16_class.hip",
                "kernels_f32_ms_class.hip", "kernels_bf16_ms_class.hip", "kernels_f32_split_class.hip",
                "kernels_bf16_split_class.hip", "kernels_wg.hip", "kernels_common.hip",
-               "js.hip", "js_api.hip"]
+               "js.hip", "js_api.hip", "mx4.hip", "mx4_gemm.hip", "mx4_api.hip", "sample.hip", "sample_api.hip"]
 CXX_SOURCES = ["topology.cpp"]
 
 ARCH = "gfx950"
@@ -44,6 +44,9 @@ HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall", "-
 CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
 
 HASH_COMPONENTS = ("all", "step", "js")
+JS_SOURCES = ("js.hip", "js.hpp", "js_api.hip")
+# Operators on matrices and logits: in the whole library's hash alone.
+OPERATOR_SOURCES = ("mx4.hip", "mx4.hpp", "mx4_gemm.hip", "mx4_api.hip", "sample.hip", "sample.hpp", "sample_api.hip")
 
 
 def source_hashes(root: str = ROOT) -> dict:
@@ -51,7 +54,7 @@ def source_hashes(root: str = ROOT) -> dict:
     all   every file under paper_2606_22768_amd/csrc and include/fgd.h;
     step  the HIP sources of the outer step, its split halves, consensus,
           finalize and copy kernels and their launches (every .hip/.hpp but
-          the JS distance's js.hip, js.hpp and js_api.hip);
+          the JS distance's and the operators');
     js    the JS distance kernels, their launcher header, their C entry
           points and the headers those include (kernels.hpp, api.hpp).
     Traffic counters and timings are valid only for the hash they were
@@ -64,9 +67,9 @@ def source_hashes(root: str = ROOT) -> dict:
             data = name.encode() + b"\0" + f.read()
         hs["all"].update(data)
         if name.endswith((".hip", ".hpp")):
-            if name not in ("js.hip", "js.hpp", "js_api.hip"):
+            if name not in JS_SOURCES + OPERATOR_SOURCES:
                 hs["step"].update(data)
-            if name in ("js.hip", "js.hpp", "js_api.hip", "kernels.hpp", "api.hpp"):
+            if name in JS_SOURCES + ("kernels.hpp", "api.hpp"):
                 hs["js"].update(data)
     with open(os.path.join(root, "include", "fgd.h"), "rb") as f:
         hs["all"].update(b"fgd.h\0" + f.read())

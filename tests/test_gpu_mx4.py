@@ -1,0 +1,332 @@
+"""GPU tests of the 4-bit operators against 64-bit references.
+
+Quantisation is exact: the scale is a power of two and the rounding is to a
+grid that both sides know, so values and scale bytes must agree bit for bit.
+
+Products of 4-bit values are exact in float32; what the kernels round are
+the sums of up to K of them.  A sum of n float32 terms in any order is off by
+at most n eps sum|terms| (eps = 2^-24); the instruction adds 128 of them per
+step, so the bar is (K / 128 + 128) eps sum|a b|.  A bf16 output is the float32
+one rounded once, bit for bit.
+"""
+
+import numpy as np
+import pytest
+
+from oracle import operators as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    import paper_2606_22768_amd as fgd
+
+    return fgd, torch
+
+
+def _t(torch, dtype):
+    return torch.float32 if dtype == "f32" else torch.bfloat16
+
+
+def _host(t):
+    return t.detach().to("cpu").double().numpy()
+
+
+def _values(shape, seed, spread=3.0):
+    """Normal values whose blocks differ in size by a few binades."""
+    rng = np.random.default_rng(seed)
+    return (rng.standard_normal(shape) * np.exp2(rng.uniform(-spread, spread, shape[:-1] + (1,)))).astype(np.float32)
+
+
+def _tensor(torch, a, dtype):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda().to(_t(torch, dtype))
+
+
+SHAPES = [(1, 1), (1, 32), (1, 33), (3, 31), (16, 128), (17, 129), (64, 127), (65, 256), (5, 1000), (200, 96),
+          (1, 4097), (130, 513)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_round_trip_along_rows_and_columns(env, shape, dtype):
+    fgd, torch = env
+    print(f"[mx4] round trip {shape} {dtype}", flush=True)
+    x = _tensor(torch, _values(shape, 1 + shape[0] * shape[1]), dtype)
+    for view in (x, x.mT):
+        q = fgd.mx4_quantize(view)
+        assert q.shape == tuple(view.shape)
+        want = ref.mx4_values(_host(view))
+        for out in ("f32", "bf16"):
+            got = _host(fgd.mx4_dequantize(q, out))
+            assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_round_trip_of_batches_and_strides(env, dtype):
+    """Batches of padded rows, rows that start off any 16-byte boundary, a
+    broadcast batch, and the columns of the same storage."""
+    fgd, torch = env
+    rng = np.random.default_rng(3)
+    pool = _tensor(torch, rng.standard_normal(3 * 70 * 211 + 5).astype(np.float32), dtype)
+    for off in (0, 1, 3):
+        base = pool[off:off + 3 * 70 * 211].view(3, 70, 211)
+        for x in (base, base[:, :, 1:200], base[:, 3:68, :], base[1:2].expand(3, 70, 211), base.mT, base[:, 2:].mT):
+            got = _host(fgd.mx4_dequantize(fgd.mx4_quantize(x)))
+            assert np.array_equal(got, ref.mx4_values(_host(x)))
+    out = torch.full((3, 70, 300), 7.0, dtype=_t(torch, dtype), device="cuda")
+    q = fgd.mx4_quantize(base)
+    fgd.mx4_dequantize(q, out=out[:, :, 5:216])
+    assert np.array_equal(_host(out[:, :, 5:216]), ref.mx4_values(_host(base)))
+    assert (out[:, :, :5] == 7).all() and (out[:, :, 216:] == 7).all()  # nothing beside the view
+
+
+def test_every_binade_and_tie(env):
+    """Blocks whose largest magnitude runs through every float32 binade,
+    denormals included, with elements on, just below and just above every
+    rounding boundary; scale bytes as the header lays them out."""
+    fgd, torch = env
+    edges = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0], np.float64)
+    rows = []
+    for e in range(-149, 128):
+        unit = 2.0 ** (e - 2)
+        v = np.concatenate([edges, edges * (1 - 2 ** -20), edges * (1 + 2 ** -20), -edges]) * unit
+        with np.errstate(over="ignore"):
+            v = v.astype(np.float32)
+        v[np.abs(v) >= 2.0 ** min(e + 1, 127)] = 0
+        v[31] = np.float32(2.0 ** e)
+        rows.append(v)
+    x = np.stack(rows)
+    q = fgd.mx4_quantize(_tensor(torch, x, "f32"))
+    assert np.array_equal(_host(fgd.mx4_dequantize(q)), ref.mx4_values(x))
+    s = q.scales.cpu().numpy().reshape(-1, 64, 4)  # [row tile][lane][fragment]: one column tile
+    got = np.array([s[r // 64, r % 16, (r % 64) // 16] for r in range(x.shape[0])])
+    assert np.array_equal(got, ref.mx4_scale_bytes(x)[:, 0])
+
+
+def test_zero_signs_infinities_and_nan(env):
+    fgd, torch = env
+    x = np.zeros((6, 96), np.float32)
+    x[0, 3] = -0.0
+    x[1, 40] = np.inf
+    x[2, 70] = -np.inf
+    x[3, 5] = np.nan
+    x[4, 33] = np.finfo(np.float32).max
+    x[5] = -np.finfo(np.float32).max
+    for dtype in ("f32", "bf16"):
+        t = _tensor(torch, x, dtype)
+        got = _host(fgd.mx4_dequantize(fgd.mx4_quantize(t)))
+        want = ref.mx4_values(_host(t))
+        assert np.array_equal(got, want, equal_nan=True)
+        assert np.signbit(got[0, 3]) and np.isnan(got[1, 32:64]).all() and not np.isnan(got[1, :32]).any()
+
+
+def _check_product(got, a, w):
+    """The float32 output `got` against the 64-bit product of the quantised
+    values a, w."""
+    want = a @ np.swapaxes(w, -1, -2)
+    size = np.abs(a) @ np.swapaxes(np.abs(w), -1, -2)
+    K = a.shape[-1]
+    bar = (K / 128 + 128) * 2.0 ** -24 * size
+    bad = ~(np.abs(got - want) <= bar)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} off, worst {np.nanmax(np.abs(got - want) / (size + 1e-300))}"
+
+
+PRODUCTS = [(1, 1, 1), (1, 5, 33), (1, 128, 256), (2, 64, 1000), (3, 257, 129), (16, 300, 96), (17, 65, 640),
+            (31, 1000, 224), (64, 64, 128), (65, 33, 300), (100, 513, 2048), (129, 255, 1024), (256, 256, 256),
+            (257, 300, 520), (300, 1030, 385), (1, 700, 9000), (40, 90, 8200)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mnk", PRODUCTS, ids=str)
+def test_product(env, mnk, dtype):
+    fgd, torch = env
+    m, n, k = mnk
+    print(f"[mx4] product {mnk} {dtype}", flush=True)
+    x, w = _tensor(torch, _values((m, k), m + k), dtype), _tensor(torch, _values((n, k), n + k, 1.0), dtype)
+    a4, w4 = fgd.mx4_quantize(x), fgd.mx4_quantize(w)
+    a, b = ref.mx4_values(_host(x)), ref.mx4_values(_host(w))
+    y = fgd.mx4_matmul(a4, w4, "f32")
+    assert y.dtype == torch.float32
+    _check_product(_host(y), a, b)
+    assert torch.equal(fgd.mx4_matmul(a4, w4), y.to(torch.bfloat16))
+    for out_dtype in ("f32", "bf16"):  # the same bits from one call
+        assert torch.equal(fgd.mx4_linear(x, w4, out_dtype), y.to(_t(torch, out_dtype)))
+    assert torch.equal(fgd.mx4_linear(x, w4), fgd.mx4_linear(x, w4, dtype))
+
+
+@pytest.mark.parametrize("T", [1, 3, 20, 70, 200])
+@pytest.mark.parametrize("M", [2, 9])
+def test_product_of_workers(env, M, T):
+    """A batch gives each worker's own product, also from strided rows and
+    into a strided output."""
+    fgd, torch = env
+    N, K = 333, 420
+    print(f"[mx4] batch M={M} T={T}", flush=True)
+    x = _tensor(torch, _values((M, T, K + 13), 7), "bf16")[:, :, 3:3 + K]
+    w = _tensor(torch, _values((M, N, K), 8), "bf16")
+    w4 = fgd.mx4_quantize(w)
+    pool = torch.full((M, T + 2, N + 9), 3.0, dtype=torch.float32, device="cuda")
+    y = fgd.mx4_linear(x, w4, out=pool[:, 1:T + 1, 2:N + 2])
+    for i in range(M):
+        a, b = ref.mx4_values(_host(x[i])), ref.mx4_values(_host(w[i]))
+        _check_product(_host(y[i]), a, b)
+        _check_product(_host(fgd.mx4_linear(x[i], fgd.mx4_quantize(w[i]), "f32")), a, b)
+    pool[:, 1:T + 1, 2:N + 2] = 3.0
+    assert (pool == 3.0).all()
+
+
+def test_every_number_of_tokens(env):
+    """The first n tokens of a batch, for n on both sides of every tile."""
+    fgd, torch = env
+    x = _tensor(torch, _values((300, 1500), 5), "bf16")
+    w = _tensor(torch, _values((700, 1500), 6), "bf16")
+    w4 = fgd.mx4_quantize(w)
+    a, b = ref.mx4_values(_host(x)), ref.mx4_values(_host(w))
+    for n in (1, 2, 4, 5, 8, 9, 15, 16, 17, 31, 32, 33, 48, 63, 64, 65, 100, 127, 128, 129, 191, 192, 193, 256, 257):
+        y = fgd.mx4_linear(x[:n], w4, "f32")
+        _check_product(_host(y), a[:n], b)
+        assert torch.equal(y, fgd.mx4_linear(x[:n], w4, "f32"))
+
+
+def test_nan_blocks_reach_only_their_row_and_column(env):
+    fgd, torch = env
+    for T in (4, 300):
+        x = _tensor(torch, _values((T, 256), 1), "f32")
+        w = _tensor(torch, _values((300, 256), 2), "f32")
+        x[2, 100] = float("inf")
+        w[77, 3] = float("nan")
+        y = fgd.mx4_linear(x, fgd.mx4_quantize(w))
+        nan = torch.zeros((T, 300), dtype=torch.bool, device="cuda")
+        nan[2], nan[:, 77] = True, True
+        assert torch.equal(torch.isnan(y), nan)
+
+
+def test_sizes_of_zero(env):
+    fgd, torch = env
+    z = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
+    assert fgd.mx4_dequantize(fgd.mx4_quantize(z(0, 5))).shape == (0, 5)
+    assert fgd.mx4_dequantize(fgd.mx4_quantize(z(0, 3, 5))).shape == (0, 3, 5)
+    assert fgd.mx4_linear(z(0, 64), fgd.mx4_quantize(z(7, 64))).shape == (0, 7)
+    assert fgd.mx4_linear(z(3, 64), fgd.mx4_quantize(z(0, 64))).shape == (3, 0)
+    out = torch.full((3, 7), 5.0, device="cuda")
+    fgd.mx4_linear(z(3, 0), fgd.mx4_quantize(z(7, 0)), out=out)
+    assert (out == 0).all()  # a product over nothing
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mtnk", [(None, 1, 40, 64), (None, 130, 200, 96), (2, 77, 100, 210), (None, 300, 513, 290)],
+                         ids=str)
+def test_gradients_against_their_formula(env, mtnk, dtype):
+    fgd, torch = env
+    M, T, N, K = mtnk
+    lead = () if M is None else (M,)
+    print(f"[mx4] grads {mtnk} {dtype}", flush=True)
+    x, w = _tensor(torch, _values((*lead, T, K), 1), dtype), _tensor(torch, _values((*lead, N, K), 2), dtype)
+    dy = _tensor(torch, _values((*lead, T, N), 3), dtype)
+    w_t = fgd.mx4_quantize(w.mT)
+    dx, dw = fgd.mx4_linear_grads(dy, x, w_t)
+    assert dx.dtype == dy.dtype and dw.dtype == torch.float32
+    sw = lambda a: np.swapaxes(a, -1, -2)  # noqa: E731
+    hx, hw, hdy = _host(x), _host(w), _host(dy)
+    _check_product(_host(dw), ref.mx4_values(sw(hdy)), ref.mx4_values(sw(hx)))
+    kept = fgd.mx4_linear_grads(dy, fgd.mx4_quantize(x.mT), w_t, dx_dtype="f32", dw_dtype="bf16")
+    _check_product(_host(kept[0]), ref.mx4_values(hdy), ref.mx4_values(sw(hw)))
+    assert kept[0].dtype == torch.float32 and torch.equal(kept[0].to(dx.dtype), dx)
+    assert torch.equal(kept[1], dw.to(torch.bfloat16))
+
+
+def test_gradients_against_differences(env):
+    """Where every operand stands on the 4-bit grid along both axes, rounding
+    is the identity, so the layer is bilinear and differences of its loss
+    sum(dy y) are exact: moving one x or w by 1 (which stays on the grid) moves
+    the loss by that element's gradient."""
+    fgd, torch = env
+    rng = np.random.default_rng(4)
+    T, N, K = 64, 96, 64
+
+    def grid(shape):
+        """Whole numbers of {-2..2}, with a 4 in every block of 32 of both
+        axes, so that every block's scale is 1 and +1 moves stay on it."""
+        a = rng.integers(-2, 3, shape).astype(np.float32)
+        for i in range(0, shape[0], 32):
+            for j in range(0, shape[1], 32):
+                d = rng.permutation(32)
+                a[i + np.arange(32), j + d] = 4.0
+        return a
+
+    x, w, dy = grid((T, K)), grid((N, K)), grid((T, N))
+    t = lambda a: _tensor(torch, a, "f32")  # noqa: E731
+    dx, dw = (_host(g) for g in fgd.mx4_linear_grads(t(dy), t(x), fgd.mx4_quantize(t(w).mT)))
+
+    def loss(x, w):
+        return float((_host(fgd.mx4_linear(t(x), fgd.mx4_quantize(t(w)))) * dy).sum())
+
+    base = loss(x, w)
+    for _ in range(12):
+        i, j = int(rng.integers(T)), int(rng.integers(K))
+        if x[i, j] < 2:
+            moved = x.copy()
+            moved[i, j] += 1
+            assert loss(moved, w) - base == dx[i, j]
+        i = int(rng.integers(N))
+        if w[i, j] < 2:
+            moved = w.copy()
+            moved[i, j] += 1
+            assert loss(x, moved) - base == dw[i, j]
+
+
+def test_offsets_past_32_bits(env):
+    """A matrix whose source and output elements lie past 2^31 elements and
+    2^32 bytes: the last rows of a large strided array."""
+    fgd, torch = env
+    rows, ld = 3, 1_500_000_000
+    print("[mx4] far rows", flush=True)
+    pool = torch.zeros(2 * ld + 300, dtype=torch.bfloat16, device="cuda")
+    x = pool.as_strided((rows, 300), (ld, 1))
+    x.copy_(_tensor(torch, _values((rows, 300), 9), "bf16"))
+    q = fgd.mx4_quantize(x)
+    want = ref.mx4_values(_host(x))
+    assert np.array_equal(_host(fgd.mx4_dequantize(q)), want)
+    w = _tensor(torch, _values((300, 300), 10), "bf16")
+    near = fgd.mx4_linear(x, fgd.mx4_quantize(w))
+    fgd.mx4_linear(x.clone(), fgd.mx4_quantize(w), out=x)
+    assert torch.equal(x, near)
+
+
+def test_other_stream_and_graph(env):
+    """The calls run on the stream they are given, and may be captured; a
+    replay reads what the inputs hold then."""
+    fgd, torch = env
+    x = _tensor(torch, _values((40, 512), 1), "bf16")
+    w = _tensor(torch, _values((300, 512), 2), "bf16")
+    w4 = fgd.mx4_quantize(w)
+    want = fgd.mx4_linear(x, w4)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    y = torch.empty_like(want)
+    ws = torch.empty(fgd.fgd_mx4_linear_workspace_size(1, 40, 512), dtype=torch.uint8, device="cuda")
+    fgd.mx4_linear(x, w4, out=y, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want)
+    q = fgd.mx4_quantize(w)
+    back = torch.empty_like(w)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        fgd.mx4_linear(x, w4, out=y, workspace=ws)
+        fgd.mx4_dequantize(q, out=back)
+    torch.cuda.synchronize()
+    for rep in range(3):
+        x.copy_(_tensor(torch, _values((40, 512), 20 + rep), "bf16"))
+        y.zero_()
+        back.zero_()
+        ws.fill_(0xA5)
+        want = fgd.mx4_linear(x, w4)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), rep
+        assert np.array_equal(_host(back), ref.mx4_values(_host(w)))

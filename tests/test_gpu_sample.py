@@ -1,0 +1,290 @@
+"""GPU tests of sampling against a 64-bit reference of the whole-number
+definition.
+
+With T chosen so that the scaled logits are the logits' own whole-number
+differences, every weight is a power of two, the masses are exact on both
+sides, and the token must be equal.  With ordinary logits the two sides'
+powers of two differ by up to 1.5 float32 ulps (3 2^-24 relative) and a mass by
+one unit from its rounding, so a sum of n masses differs by at most
+3 2^-24 of it plus n units; the drawn token must be one whose span of the
+reference's mass, widened by four such errors, holds the reference's target,
+and its probability must agree within the same error.
+"""
+
+import numpy as np
+import pytest
+
+from oracle import operators as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    import paper_2606_22768_amd as fgd
+
+    return fgd, torch
+
+
+def _unit_temperature():
+    """A float32 T with (1 / T) log2(e) = 1 exactly."""
+    t = np.float32(np.log2(np.e))
+    for _ in range(8):
+        for s in (-np.inf, np.inf):
+            v = t
+            for _ in range(4):
+                if (np.float32(1) / v) * np.float32(np.log2(np.e)) == np.float32(1):
+                    return float(v)
+                v = np.nextafter(v, np.float32(s))
+    raise AssertionError("no such temperature")
+
+
+UNIT_T = _unit_temperature()
+
+
+def _cuda(torch, a, dtype="f32"):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t.to(torch.bfloat16) if dtype == "bf16" else t
+
+
+def _rows(torch, v, dtype=np.float32):
+    return torch.from_numpy(np.asarray(v, dtype)).cuda()
+
+
+def _run(env, z, u, dtype="f32", **kw):
+    fgd, torch = env
+    t, p = fgd.sample(_cuda(torch, z, dtype), _rows(torch, u), **kw)
+    return t.cpu().numpy(), p.cpu().numpy()
+
+
+SIZES = [1, 2, 3, 63, 64, 65, 255, 1000, 1025, 4099, 8192, 32000, 50257, 128256, 152064]
+SETTINGS = [dict(), dict(top_k=1), dict(top_k=7), dict(top_k=300), dict(top_k=5000), dict(top_p=0.5),
+            dict(top_p=0.95), dict(top_p=1e-9), dict(min_p=0.25), dict(min_p=2.0 ** -20), dict(min_p=3.0),
+            dict(top_k=40, top_p=0.8), dict(top_k=1000, top_p=0.99, min_p=0.01), dict(top_p=0.0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", SIZES)
+def test_exact_weights_give_equal_tokens(env, V, dtype):
+    """Whole-number logits (many ties), several rows and settings at once,
+    some tokens masked."""
+    rng = np.random.default_rng(V)
+    n = len(SETTINGS)
+    z = np.minimum(rng.geometric(0.2, (n, V)), 40).astype(np.float32)
+    z[rng.random((n, V)) < 0.2] = -np.inf
+    z[:, rng.integers(V)] = 3.0
+    u = rng.random(n).astype(np.float32)
+    print(f"[sample] exact V={V} {dtype}", flush=True)
+    fgd, torch = env
+    get = lambda k, d: _rows(torch, [s.get(k, d) for s in SETTINGS],  # noqa: E731
+                             np.int32 if k == "top_k" else np.float32)
+    tok, prob = _run(env, z, u, dtype, temperature=UNIT_T, top_k=get("top_k", 0), top_p=get("top_p", 1.0),
+                     min_p=get("min_p", 0.0))
+    for i, s in enumerate(SETTINGS):
+        t, mass, total, _, _, _ = ref.sample(z[i], u[i], UNIT_T, **s)
+        assert tok[i] == t, (s, u[i])
+        assert prob[i] == np.float32(np.float32(mass) / np.float32(total)), s
+        one, p1 = _run(env, z[i:i + 1], u[i:i + 1], dtype, temperature=UNIT_T, **s)  # a row alone, scalar settings
+        assert one[0] == t and p1[0] == prob[i], s
+
+
+@pytest.mark.parametrize("V", [5, 1000, 32001])
+def test_every_draw_of_a_tied_row(env, V):
+    """All logits equal: the draw walks the indices in order."""
+    n = 64
+    u = (np.arange(n) / n).astype(np.float32)
+    z = np.full((n, V), -7.25, np.float32)
+    tok, prob = _run(env, z, u)
+    total = V << 31
+    assert np.array_equal(tok, [int(np.float64(x) * total) >> 31 for x in u])
+    assert (prob == np.float32(2.0 ** 31) / np.float32(total)).all()
+    k = V // 2 + 1
+    tok, _ = _run(env, z, u, top_k=k)
+    assert np.array_equal(tok, [int(np.float64(x) * (k << 31)) >> 31 for x in u])
+
+
+def _check_row(z, u, tok, prob, temperature, s):
+    t, mass, total, before, idx, keep = ref.sample(z, u, temperature, **s)
+    if t < 0 or not temperature > 0:
+        assert tok == t
+        return
+    m, _ = ref.sample_masses(z, temperature)
+    m = m[idx]
+    # A cut may fall a few tokens away where masses lie within the error of
+    # it; the tokens there are equally likely to within that error.
+    err = 4 * (3 * 2.0 ** -24 * float(m.sum()) + z.size)
+    at = int(np.nonzero(idx == tok)[0][0])
+    lo = float(m[:at].sum())
+    target = float(np.float64(np.float32(u))) * total
+    assert lo - err <= target <= lo + float(m[at]) + err, (s, tok, t)
+    assert abs(prob - float(m[at]) / total) <= err / total + 2.0 ** -22, s
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [17, 777, 5000, 50257, 128256])
+def test_ordinary_logits(env, V, dtype):
+    fgd, torch = env
+    rng = np.random.default_rng(V + 1)
+    temps = [0.3, 0.7, 1.0, 1.5, 5.0]
+    cases = [(t, s) for t in temps for s in SETTINGS]
+    print(f"[sample] ordinary V={V} {dtype}", flush=True)
+    z = (rng.standard_normal((len(cases), V)) * 2.5).astype(np.float32)
+    z[np.arange(len(cases)), rng.integers(0, V, len(cases))] += 8
+    z = _cuda(torch, z, dtype)
+    u = rng.random(len(cases)).astype(np.float32)
+    get = lambda k, d: _rows(torch, [s.get(k, d) for _, s in cases],  # noqa: E731
+                             np.int32 if k == "top_k" else np.float32)
+    tok, prob = fgd.sample(z, _rows(torch, u), _rows(torch, [t for t, _ in cases]), get("top_k", 0),
+                           get("top_p", 1.0), get("min_p", 0.0))
+    tok, prob, h = tok.cpu().numpy(), prob.cpu().numpy(), z.float().cpu().numpy()
+    for i, (t, s) in enumerate(cases):
+        _check_row(h[i], u[i], tok[i], prob[i], t, s)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [6, 1000, 40000])
+def test_rows_with_little_left(env, V, dtype):
+    """Masked rows, infinities, NaN, the type's lowest value, extreme
+    settings."""
+    inf, low = np.inf, float(np.finfo(np.float32).min) if dtype == "f32" else -3.3895313892515355e38
+    z = np.zeros((14, V), np.float32)
+    z[0] = -inf
+    z[1] = -inf
+    z[1, V - 1] = -3.0                       # one token left
+    z[2, 3] = np.nan
+    z[3, 2] = inf                            # all the mass on one
+    z[4, 1] = z[4, V - 1] = inf              # ... on two
+    z[5] = low                               # nothing masked: all equal
+    z[6] = low
+    z[6, 4] = 0.0
+    z[7, 5] = -inf
+    z[8], z[8, 0] = -inf, np.nan
+    z[9], z[9, 5] = 0.0, -0.0                # the zeros are equal
+    z[10], z[10, 4] = 1.0, 2.0
+    z[11], z[11, 4] = 1.0, 2.0
+    z[12], z[12, 4] = 1.0, 2.0
+    z[13] = 3.0e38 if dtype == "f32" else 2.9e38
+    z[13, 2] = low
+    u = np.array([0.5, 0.99, 0.5, 0.9, 0.75, 0.0, 0.999, 0.0, 0.1, 0.0, np.nan, -1.0, 2.0, 0.0], np.float32)
+    tok, prob = _run(env, z, u, dtype)
+    assert tok[0] == -1 and prob[0] == 0
+    assert tok[1] == V - 1 and prob[1] == 1
+    assert tok[2] == -1 and np.isnan(prob[2])
+    assert tok[3] == 2 and prob[3] == 1
+    assert tok[4] == V - 1 and prob[4] == 0.5
+    assert tok[5] == 0 and prob[5] == np.float32(2.0 ** 31) / np.float32(V << 31)
+    assert tok[6] == 4 and prob[6] == 1
+    assert tok[7] == 0
+    assert tok[8] == -1 and np.isnan(prob[8])
+    assert tok[9] == 0
+    assert tok[10] == 4 and tok[11] == 4     # NaN and negative: as 0
+    last = [i for i in range(V) if i != 4][-1]
+    assert tok[12] == last                   # above 1: as just below
+    assert tok[13] == 0
+    for t in (0.0, -1.0, float("nan"), 1e-45, 1e-39):  # greedy: the first of the largest
+        tok, prob = _run(env, z, u, dtype, temperature=t)
+        assert list(tok) == [-1, V - 1, -1, 2, 1, 0, 4, 0, -1, 0, 4, 4, 4, 0]
+        ok = tok >= 0
+        assert (prob[ok] == 1).all()
+    tok, prob = _run(env, z[10:13], np.zeros(3, np.float32), dtype, temperature=float("inf"))
+    assert (tok == 4).all() and (prob == np.float32(2.0 ** 31) / np.float32(V << 31)).all()
+
+
+def test_long_tail_of_ties_and_padding(env):
+    """bf16 logits tie by the thousand; a padded row's tail is never used,
+    whatever it holds; rows may start off any boundary."""
+    fgd, torch = env
+    rng = np.random.default_rng(2)
+    for V, ld in ((9001, 9001), (9001, 9013), (777, 1000)):
+        z = np.round(rng.standard_normal((5, V)) * 4).astype(np.float32)
+        u = rng.random(5).astype(np.float32)
+        for dtype in ("f32", "bf16"):
+            pool = torch.full((5, ld + 3), float("nan"), device="cuda",
+                              dtype=torch.float32 if dtype == "f32" else torch.bfloat16)
+            pool[:, 3:3 + V] = _cuda(torch, z, dtype)
+            for s in SETTINGS:
+                tok, _ = fgd.sample(pool[:, 3:], _rows(torch, u), UNIT_T, vocab=V, **s)
+                assert tok.tolist() == [ref.sample(z[i], u[i], UNIT_T, **s)[0] for i in range(5)], s
+
+
+def test_rows_do_not_depend_on_their_batch(env):
+    fgd, torch = env
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    U, V = 700, 30011
+    z = torch.randn((U, V), generator=g, device="cuda") * 3
+    u = torch.rand(U, generator=g, device="cuda")
+    kw = dict(temperature=1.1, top_k=2000, top_p=0.97, min_p=1e-4)
+    tok, prob = fgd.sample(z, u, **kw)
+    for n in (1, 2, 9, 100, 257):
+        t, p = fgd.sample(z[:n], u[:n], **kw)
+        assert torch.equal(t, tok[:n]) and torch.equal(p, prob[:n])
+    t, p = fgd.sample(z, u, **kw)
+    assert torch.equal(t, tok) and torch.equal(p, prob)
+
+
+def test_draws_follow_the_distribution(env):
+    """20 000 draws of one row at evenly spaced random numbers: each token is
+    drawn its share, to one draw at each end of its span."""
+    fgd, torch = env
+    rng = np.random.default_rng(8)
+    V, n = 300, 20000
+    z = (rng.standard_normal(V) * 2).astype(np.float32)
+    u = ((np.arange(n) + 0.5) / n).astype(np.float32)
+    tok, _ = fgd.sample(_cuda(torch, z[None]).expand(n, V).contiguous(), _rows(torch, u), temperature=0.8)
+    got = np.bincount(tok.cpu().numpy(), minlength=V)
+    p = np.exp(z.astype(np.float64) / 0.8)
+    p /= p.sum()
+    assert np.all(np.abs(got - n * p) <= 2)
+
+
+def test_far_rows(env):
+    """Rows that start past 2^32 bytes."""
+    fgd, torch = env
+    ld = 1_500_000_000
+    V = 1003
+    rng = np.random.default_rng(6)
+    z = np.minimum(rng.geometric(0.3, (3, V)), 30).astype(np.float32)
+    print("[sample] far rows", flush=True)
+    pool = torch.zeros(2 * ld + V, dtype=torch.bfloat16, device="cuda")
+    view = pool.as_strided((3, V), (ld, 1))
+    view.copy_(_cuda(torch, z, "bf16"))
+    u = np.array([0.2, 0.6, 0.9], np.float32)
+    tok, _ = fgd.sample(view, _rows(torch, u), UNIT_T)
+    assert tok.tolist() == [ref.sample(z[i], u[i], UNIT_T)[0] for i in range(3)]
+
+
+def test_other_stream_and_graph(env):
+    fgd, torch = env
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    for U, V in ((2, 128256), (300, 5000)):
+        z = torch.randn((U, V), generator=g, device="cuda") * 3
+        u = torch.rand(U, generator=g, device="cuda")
+        tok = torch.zeros(U, dtype=torch.int32, device="cuda")
+        prob = torch.zeros(U, device="cuda")
+        need = fgd.fgd_sample_workspace_size("f32", U, V)
+        ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+        kw = dict(temperature=0.9, top_k=50, top_p=0.9, tokens_out=tok, probs_out=prob, workspace=ws)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        want = fgd.sample(z, u, 0.9, 50, 0.9)
+        fgd.sample(z, u, stream=side, **kw)
+        side.synchronize()
+        assert torch.equal(tok, want[0]) and torch.equal(prob, want[1])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            fgd.sample(z, u, **kw)
+        torch.cuda.synchronize()
+        for rep in range(3):
+            u.copy_(torch.rand(U, generator=g, device="cuda"))
+            ws.fill_(0x5A + rep)
+            tok.zero_()
+            want = fgd.sample(z, u, 0.9, 50, 0.9)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(tok, want[0]) and torch.equal(prob, want[1])
