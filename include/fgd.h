@@ -422,10 +422,11 @@ fgd_status fgd_js_workspace_size(int32_t dtype, int32_t num_workers, int64_t num
  * Codes and scales lie in two arrays, in tiles of 64 rows x 128 columns of
  * 4096 and 256 bytes, tile (r, k) of batch entry b at index (b * ceil(rows /
  * 64) + r) * ceil(cols / 128) + k.  Element (i, 32 q + j) of a tile, q in
- * [0, 4), is nibble j % 2 (low first) of byte (i / 16) * 1024 + (i % 16 + 16
- * q) * 16 + j / 2 of the tile's codes, and its block's scale is byte (i % 16
- * + 16 q) * 4 + i / 16 of the tile's scales.  Rows and columns past the
- * matrix hold zeros.  Both arrays are 16-byte aligned.
+ * [0, 4), belongs to fragment f = 2 (i / 32) + q / 2 and lane l = i % 32 + 32
+ * (q % 2): it is nibble j % 2 (low first) of byte 1024 f + 16 l + j / 2 of
+ * the tile's codes, and its block's scale is byte 4 l + f of the tile's
+ * scales.  Rows and columns past the matrix hold zeros.  Both arrays are
+ * 16-byte aligned.
  *
  * Every array of these calls is the caller's; outputs may overlap neither
  * inputs nor each other; sizes of zero are allowed (there is nothing to

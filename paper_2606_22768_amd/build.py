@@ -46,7 +46,8 @@ CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
 HASH_COMPONENTS = ("all", "step", "js")
 JS_SOURCES = ("js.hip", "js.hpp", "js_api.hip")
 # Operators on matrices and logits: in the whole library's hash alone.
-OPERATOR_SOURCES = ("mx4.hip", "mx4.hpp", "mx4_gemm.hip", "mx4_api.hip", "sample.hip", "sample.hpp", "sample_api.hip")
+OPERATOR_SOURCES = ("mx4.hip", "mx4.hpp", "mx4_block.hpp", "mx4_gemm.hip", "mx4_api.hip", "sample.hip",
+                    "sample.hpp", "sample_api.hip")
 
 
 def source_hashes(root: str = ROOT) -> dict:

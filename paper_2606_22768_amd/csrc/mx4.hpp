@@ -12,10 +12,11 @@
 // kernel moves whole fragments and none rearranges one: a matrix of R rows
 // and K columns lies in tiles of 64 rows x 128 columns, tile (r, k) at index
 // r * ceil(K / 128) + k, batch after batch.  A tile's codes are four
-// fragments of 16 rows, 1 KB each: lane l = (row % 16) + 16 * block holds
-// the 16 bytes of block `block` (0..3) of its row, low nibble first.  A
-// tile's scales are 64 dwords, one per lane, whose byte j belongs to
-// fragment j.  Rows and columns past the matrix are zero.
+// fragments of 32 rows x 64 columns, 1 KB each, fragment 2 p + h holding row
+// half p and column half h: lane l = (row % 32) + 32 * (block % 2) holds the
+// 16 bytes of one block of its row, low nibble first.  A tile's scales are
+// 64 dwords, one per lane, whose byte f belongs to fragment f.  Rows and
+// columns past the matrix are zero.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -32,6 +33,12 @@ inline int64_t mx4_tiles(int64_t batch, int64_t rows, int64_t cols) {
     return batch * mx4_row_tiles(rows) * mx4_col_tiles(cols);
 }
 
+// Whether every row of an array starts on a 16-byte boundary.
+inline bool mx4_rows_aligned(const void *x, bool bf16, int64_t batch_stride, int64_t row_stride) {
+    const int64_t es = bf16 ? 2 : 4;
+    return reinterpret_cast<uintptr_t>(x) % 16 == 0 && batch_stride * es % 16 == 0 && row_stride * es % 16 == 0;
+}
+
 // x[b][r][k] at b * batch_stride + r * row_stride + k * col_stride, one of
 // the last two strides 1.  False if a launch failed.
 bool mx4_quantize_launch(const void *x, bool bf16, int64_t batch, int64_t rows, int64_t cols, int64_t batch_stride,
@@ -44,5 +51,12 @@ bool mx4_dequantize_launch(const void *codes, const void *scales, int64_t batch,
 bool mx4_matmul_launch(const void *a_codes, const void *a_scales, const void *w_codes, const void *w_scales,
                        int64_t batch, int64_t m, int64_t n, int64_t k, void *out, bool bf16, int64_t batch_stride,
                        int64_t row_stride, hipStream_t stream);
+
+// The same product of x[b][i][k] at b * x_batch_stride + i * x_row_stride + k,
+// quantised on the way: for the few rows for which mx4_linear_fuses.
+bool mx4_linear_fuses(int64_t batch, int64_t m, int64_t n, int64_t k);
+bool mx4_linear_launch(const void *x, bool x_bf16, int64_t x_batch_stride, int64_t x_row_stride, const void *w_codes,
+                       const void *w_scales, int64_t batch, int64_t m, int64_t n, int64_t k, void *out, bool bf16,
+                       int64_t batch_stride, int64_t row_stride, hipStream_t stream);
 
 }  // namespace fgd

@@ -218,6 +218,13 @@ fgd_status fgd_mx4_linear(const void *x, int32_t x_dtype, int64_t x_batch_stride
         ranges_overlap(workspace, need, x, x_bytes) || ranges_overlap(workspace, need, w_codes, w.codes) ||
         ranges_overlap(workspace, need, w_scales, w.scales))
         return api_fail(FGD_ERR_INVALID_ARG, "x, the weights, the output and the workspace must not overlap");
+    if (fgd::mx4_linear_fuses(batch, tokens, n, k)) {
+        if (!fgd::mx4_linear_launch(x, x_dtype == FGD_BF16, x_batch_stride, x_row_stride, w_codes, w_scales, batch,
+                                    tokens, n, k, out, out_dtype == FGD_BF16, out_batch_stride, out_row_stride,
+                                    static_cast<hipStream_t>(stream)))
+            return api_fail(FGD_ERR_HIP, "4-bit layer launch failed");
+        return FGD_OK;
+    }
     uint8_t *codes = static_cast<uint8_t *>(workspace), *scales = codes + a.codes;
     if (!fgd::mx4_quantize_launch(x, x_dtype == FGD_BF16, batch, tokens, k, x_batch_stride, x_row_stride, 1, codes,
                                   scales, static_cast<hipStream_t>(stream)) ||

@@ -2,7 +2,11 @@
 // (the format and its layout: mx4.hpp).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "mx4.hpp"
+#include "mx4_block.hpp"
 
 namespace fgd {
 namespace {
@@ -10,12 +14,16 @@ namespace {
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int8v __attribute__((ext_vector_type(8)));
 typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
 
-// The operands' 4-bit format code, and which byte of the scale dwords.
-template <int SA, int SB>
-__device__ inline float4v mfma(int4v a, int4v b, float4v c, int sa, int sb) {
-    const int8v x = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, y = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, SA, sa, SB, sb);
+// 32 rows of w by 32 rows of a over 64 columns: fragments of 1 KB (lane l
+// holds row l % 32 of the block l / 32), scales the bytes SW and SA of each
+// lane's dwords.  Result: lane l holds row l % 32 of a and, in element i, row
+// 8 (i / 4) + 4 (l / 32) + i % 4 of w.
+template <int SW, int SA>
+__device__ inline float16v mfma(int4v w, int4v a, float16v c, int sw, int sa) {
+    const int8v x = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, y = {a[0], a[1], a[2], a[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, SW, sw, SA, sa);  // 4, 4: both 4-bit
 }
 
 __device__ inline uint16_t round_bf16(float v) {
@@ -24,257 +32,480 @@ __device__ inline uint16_t round_bf16(float v) {
     return static_cast<uint16_t>((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
 }
 
-__device__ inline void store(float *p, float v) { *p = v; }
-__device__ inline void store(uint16_t *p, float v) { *p = round_bf16(v); }
-
-// Four consecutive outputs at an address aligned to its element only.
+// Consecutive outputs at an address aligned to its element only.
 struct __attribute__((packed, aligned(4))) Four32 {
     float v[4];
 };
 struct __attribute__((packed, aligned(2))) Four16 {
     uint32_t v[2];
 };
-__device__ inline void store4(float *p, float4v v) {
-    *reinterpret_cast<Four32 *>(p) = Four32{{v[0], v[1], v[2], v[3]}};
+struct __attribute__((packed, aligned(2))) Eight16 {
+    uint32_t v[4];
+};
+
+// Four columns of a row.
+__device__ inline void store4(float *row, int64_t c, int64_t n, float4v v) {
+    if (c + 3 < n) {
+        *reinterpret_cast<Four32 *>(row + c) = Four32{{v[0], v[1], v[2], v[3]}};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < n) row[c + e] = v[e];
+    }
 }
-__device__ inline void store4(uint16_t *p, float4v v) {
-    *reinterpret_cast<Four16 *>(p) =
-        Four16{{round_bf16(v[0]) | static_cast<uint32_t>(round_bf16(v[1])) << 16,
-                round_bf16(v[2]) | static_cast<uint32_t>(round_bf16(v[3])) << 16}};
+__device__ inline void store4(uint16_t *row, int64_t c, int64_t n, float4v v) {
+    if (c + 3 < n) {
+        *reinterpret_cast<Four16 *>(row + c) =
+            Four16{{round_bf16(v[0]) | static_cast<uint32_t>(round_bf16(v[1])) << 16,
+                    round_bf16(v[2]) | static_cast<uint32_t>(round_bf16(v[3])) << 16}};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < n) row[c + e] = round_bf16(v[e]);
+    }
 }
 
-// Four waves, each 64 rows of w by 16 rows of a; fragments straight from
-// memory.
-template <typename T>
-__global__ __launch_bounds__(256) void product_kernel(const uint8_t *__restrict__ a_codes,
-                                                      const uint8_t *__restrict__ a_scales,
-                                                      const uint8_t *__restrict__ w_codes,
-                                                      const uint8_t *__restrict__ w_scales, int64_t m, int64_t n,
-                                                      int64_t kt, int64_t n_blocks, int64_t m_blocks,
-                                                      T *__restrict__ out, int64_t batch_stride, int64_t row_stride) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t nb = blockIdx.x % n_blocks, mb = blockIdx.x / n_blocks % m_blocks,
-                  b = blockIdx.x / n_blocks / m_blocks;
-    const int64_t a_tiles = (m + 63) / 64, w_tiles = (n + 63) / 64;
-    const int64_t wt = min(nb * 4 + wave, w_tiles - 1);  // a wave past the end repeats the last tile, unstored
-    const int sub = mb & 3;
-    const uint8_t *wc = w_codes + (b * w_tiles + wt) * kt * kMx4CodeBytes + lane * 16;
-    const uint8_t *ws = w_scales + (b * w_tiles + wt) * kt * kMx4ScaleBytes + lane * 4;
-    const uint8_t *ac = a_codes + (b * a_tiles + (mb >> 2)) * kt * kMx4CodeBytes + sub * 1024 + lane * 16;
-    const uint8_t *as = a_scales + (b * a_tiles + (mb >> 2)) * kt * kMx4ScaleBytes + lane * 4;
-    float4v acc[4] = {};
-    for (int64_t k = 0; k < kt; ++k) {
-        const int4v x = *reinterpret_cast<const int4v *>(ac + k * kMx4CodeBytes);
-        const int sx = *reinterpret_cast<const int *>(as + k * kMx4ScaleBytes) >> (8 * sub);
-        const int sw = *reinterpret_cast<const int *>(ws + k * kMx4ScaleBytes);
-        const uint8_t *p = wc + k * kMx4CodeBytes;
-        acc[0] = mfma<0, 0>(*reinterpret_cast<const int4v *>(p), x, acc[0], sw, sx);
-        acc[1] = mfma<1, 0>(*reinterpret_cast<const int4v *>(p + 1024), x, acc[1], sw, sx);
-        acc[2] = mfma<2, 0>(*reinterpret_cast<const int4v *>(p + 2048), x, acc[2], sw, sx);
-        acc[3] = mfma<3, 0>(*reinterpret_cast<const int4v *>(p + 3072), x, acc[3], sw, sx);
-    }
-    const int64_t i = mb * 16 + (lane & 15);
-    if (i >= m) return;
-    T *row = out + b * batch_stride + i * row_stride;
+// Stores one lane's part of a 32 x 32 result: columns c0 + 8 q + 4 (lane /
+// 32) + e of its row.  Two lanes of a bf16 row first exchange halves, so that
+// each stores eight consecutive columns.  (Stores of whole lines, by way of
+// LDS, measured no faster: 2048 x 128256 x 4096 to bf16 in 653 us for 629.)
+__device__ inline void store_rows(float *row, int64_t c0, int64_t n, bool in, int lane, float16v v) {
+    if (!in) return;
 #pragma unroll
-    for (int f = 0; f < 4; ++f)
+    for (int q = 0; q < 4; ++q)
+        store4(row, c0 + 8 * q + (lane >> 5) * 4, n, float4v{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
+}
+__device__ inline void store_rows(uint16_t *row, int64_t c0, int64_t n, bool in, int lane, float16v v) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t j = (nb * 4 + wave) * 64 + f * 16 + (lane >> 4) * 4 + e;
-            if (j < n) store(row + j, acc[f][e]);
+    for (int q = 0; q < 4; q += 2) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = round_bf16(v[4 * q + 2 * e]) | static_cast<uint32_t>(round_bf16(v[4 * q + 2 * e + 1])) << 16;
+        // w[0..1]: columns 4 (lane / 32) .. + 3, w[2..3]: those + 8.
+        const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        const int64_t c = c0 + 8 * q + (lane >> 5) * 8;
+        const uint32_t x[4] = {lo[0], hi[0], lo[1], hi[1]};
+        if (!in) continue;
+        if (c + 7 < n) {
+            *reinterpret_cast<Eight16 *>(row + c) = Eight16{{x[0], x[1], x[2], x[3]}};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < n) row[c + e] = static_cast<uint16_t>(x[e >> 1] >> (16 * (e & 1)));
         }
+    }
+}
+
+// --------------------------------------------------------------- few tokens
+//
+// A block multiplies NW fragments of 32 rows of w by NA fragments of 32 rows
+// of a; its waves share out the columns, tile by tile in turn, and add their
+// sums through LDS in the waves' order.  Every operand goes straight from
+// memory to registers: w is read once, and a comes from L2.
+template <int NA>
+__device__ inline void products(float16v (&acc)[1][NA], const int4v (&x)[1][2], const int4v (&y)[NA][2], int sw, int sa) {
+    acc[0][0] = mfma<0, 0>(x[0][0], y[0][0], acc[0][0], sw, sa);
+    if constexpr (NA == 2) acc[0][1] = mfma<0, 2>(x[0][0], y[1][0], acc[0][1], sw, sa);
+    acc[0][0] = mfma<1, 1>(x[0][1], y[0][1], acc[0][0], sw, sa);
+    if constexpr (NA == 2) acc[0][1] = mfma<1, 3>(x[0][1], y[1][1], acc[0][1], sw, sa);
+}
+template <int NA>
+__device__ inline void products(float16v (&acc)[2][NA], const int4v (&x)[2][2], const int4v (&y)[NA][2], int sw, int sa) {
+    acc[0][0] = mfma<0, 0>(x[0][0], y[0][0], acc[0][0], sw, sa);
+    acc[1][0] = mfma<2, 0>(x[1][0], y[0][0], acc[1][0], sw, sa);
+    if constexpr (NA == 2) {
+        acc[0][1] = mfma<0, 2>(x[0][0], y[1][0], acc[0][1], sw, sa);
+        acc[1][1] = mfma<2, 2>(x[1][0], y[1][0], acc[1][1], sw, sa);
+    }
+    acc[0][0] = mfma<1, 1>(x[0][1], y[0][1], acc[0][0], sw, sa);
+    acc[1][0] = mfma<3, 1>(x[1][1], y[0][1], acc[1][0], sw, sa);
+    if constexpr (NA == 2) {
+        acc[0][1] = mfma<1, 3>(x[0][1], y[1][1], acc[0][1], sw, sa);
+        acc[1][1] = mfma<3, 3>(x[1][1], y[1][1], acc[1][1], sw, sa);
+    }
+}
+
+#ifndef FGD_GRID
+#define FGD_GRID 512
+#endif
+// The left operand: in the 4-bit format, or (X: float, or uint16_t for bf16)
+// dense rows that the block quantises itself.
+struct Packed {
+    const uint8_t *codes, *scales;
+};
+template <typename X>
+struct Dense {
+    const X *x;
+    int64_t batch_stride, row_stride, cols;
+    bool vectors;  // rows on 16-byte boundaries
+};
+
+template <int NW, int NA, int WAVES, int AHEAD, typename T, typename Left>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(Left left, const uint8_t *__restrict__ w_codes,
+                                                         const uint8_t *__restrict__ w_scales, int64_t m, int64_t n,
+                                                         int kt, int64_t n_blocks, int64_t m_blocks,
+                                                         T *__restrict__ out, int64_t batch_stride,
+                                                         int64_t row_stride) {
+    constexpr bool kDense = !std::is_same<Left, Packed>::value;
+    static_assert(!kDense || NA == 1, "dense rows: of one fragment");
+    __shared__ float4v sums[WAVES][4 * NW * NA][64];
+    // Dense rows' blocks, block by block of the columns: one per thread.
+    __shared__ int4v x_codes[kDense ? 64 * WAVES : 1];
+    __shared__ uint8_t x_scales[kDense ? 64 * WAVES : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t w_tiles = (n + 63) / 64, items = n_blocks * m_blocks;
+    const int64_t b = blockIdx.y;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t nb = item % n_blocks, mb = item / n_blocks;
+        const int wh = NW == 2 ? 0 : nb & 1, ah = NA == 2 ? 0 : mb & 1;  // the half of a tile, where it is one
+        const int64_t wt = b * w_tiles + (NW == 2 ? nb : nb >> 1);
+        const uint8_t *wc = w_codes + wt * kt * kMx4CodeBytes + wh * 2048 + lane * 16;
+        const uint8_t *ws = w_scales + wt * kt * kMx4ScaleBytes + lane * 4;
+        const uint8_t *ac = nullptr, *as = nullptr;
+        if constexpr (!kDense) {
+            const int64_t at = b * ((m + 63) / 64) + (NA == 2 ? mb : mb >> 1);
+            ac = left.codes + at * kt * kMx4CodeBytes + ah * 2048 + lane * 16;
+            as = left.scales + at * kt * kMx4ScaleBytes + lane * 4;
+        }
+        // Rows past the last token are not loaded, but zero.
+        bool some[NA];
+#pragma unroll
+        for (int i = 0; i < NA; ++i) some[i] = (mb * NA + i) * 32 + (lane & 31) < m;
+        float16v acc[NW][NA] = {};
+        bool fresh = kDense && item == blockIdx.x;
+        for (int k0 = wave; k0 < kt || fresh; k0 += WAVES * AHEAD) {
+            // AHEAD tiles' loads go out before the first product waits.
+            int4v x[AHEAD][NW][2], y[AHEAD][NA][2];
+            int sw[AHEAD], sa[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int k = min(k0 + u * WAVES, kt - 1);  // past the last tile: that one again, times zero
+                const int64_t co = static_cast<int64_t>(k) * kMx4CodeBytes,
+                              so = static_cast<int64_t>(k) * kMx4ScaleBytes;
+                sw[u] = *reinterpret_cast<const int *>(ws + so) >> (16 * wh);
+#pragma unroll
+                for (int i = 0; i < 2 * NW; ++i)
+                    x[u][i / 2][i % 2] = *reinterpret_cast<const int4v *>(wc + co + i * 1024);
+                if constexpr (!kDense) {
+                    sa[u] = *reinterpret_cast<const int *>(as + so) >> (16 * ah);
+#pragma unroll
+                    for (int i = 0; i < 2 * NA; ++i) {
+                        y[u][i / 2][i % 2] = int4v{0, 0, 0, 0};
+                        if (some[i / 2] && k0 + u * WAVES < kt)
+                            y[u][i / 2][i % 2] = *reinterpret_cast<const int4v *>(ac + co + i * 1024);
+                    }
+                }
+            }
+            if constexpr (kDense) {
+                const int tokens = static_cast<int>(m);
+                if (fresh) {  // with the first weights on their way
+                    const int row = threadIdx.x % tokens, block = threadIdx.x / tokens;
+                    if (block < 4 * kt) {
+                        const int64_t c0 = 32 * static_cast<int64_t>(block);
+                        float v[32];
+                        load_block(left.x + b * left.batch_stride + row * left.row_stride + c0, left.cols - c0,
+                                   left.vectors, v);
+                        uint4 c;
+                        x_scales[threadIdx.x] = static_cast<uint8_t>(encode_block(v, c));
+                        x_codes[threadIdx.x] = int4v{static_cast<int>(c.x), static_cast<int>(c.y),
+                                                     static_cast<int>(c.z), static_cast<int>(c.w)};
+                    }
+                    __syncthreads();
+                    fresh = false;
+                }
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    sa[u] = 0;
+                    y[u][0][0] = y[u][0][1] = int4v{0, 0, 0, 0};
+                    if (some[0] && k0 + u * WAVES < kt) {
+                        const int at = (4 * (k0 + u * WAVES) + (lane >> 5)) * tokens + (lane & 31);
+                        y[u][0][0] = x_codes[at];
+                        y[u][0][1] = x_codes[at + 2 * tokens];
+                        sa[u] = x_scales[at] | x_scales[at + 2 * tokens] << 8;
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) products(acc, x[u], y[u], sw[u], sa[u]);
+        }
+        // Each wave leaves its sums in LDS, and adds up its share of the
+        // groups of four columns.
+#pragma unroll
+        for (int i = 0; i < NW * NA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float16v &v = acc[i / NA][i % NA];
+                sums[wave][4 * i + q][lane] = float4v{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            }
+        __syncthreads();
+#pragma unroll
+        for (int g = wave; g < 4 * NW * NA; g += WAVES) {
+            float4v v = sums[0][g][lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) v += sums[w][g][lane];
+            const int64_t i = (mb * NA + g / 4 % NA) * 32 + (lane & 31);
+            const int64_t c = (nb * NW + g / 4 / NA) * 32 + (g & 3) * 8 + (lane >> 5) * 4;
+            if (i < m) store4(out + b * batch_stride + i * row_stride, c, n, v);
+        }
+        if (item + gridDim.x < items) __syncthreads();  // before the sums' room is used again
+    }
+}
+
+// A tile of w (its fragments x) by a tile of a (y) over 128 columns.
+template <int NW, int NA>
+__device__ inline void outer(float16v (&acc)[NW][NA], int i, int j, const int4v *x, const int4v *y, int sx,
+                             int sy) {
+    acc[i][j] = mfma<0, 0>(x[0], y[0], acc[i][j], sx, sy);
+    acc[i + 1][j] = mfma<2, 0>(x[2], y[0], acc[i + 1][j], sx, sy);
+    acc[i][j + 1] = mfma<0, 2>(x[0], y[2], acc[i][j + 1], sx, sy);
+    acc[i + 1][j + 1] = mfma<2, 2>(x[2], y[2], acc[i + 1][j + 1], sx, sy);
+    acc[i][j] = mfma<1, 1>(x[1], y[1], acc[i][j], sx, sy);
+    acc[i + 1][j] = mfma<3, 1>(x[3], y[1], acc[i + 1][j], sx, sy);
+    acc[i][j + 1] = mfma<1, 3>(x[1], y[3], acc[i][j + 1], sx, sy);
+    acc[i + 1][j + 1] = mfma<3, 3>(x[3], y[3], acc[i + 1][j + 1], sx, sy);
+}
+
+// Waits until at most LOADS of this wave's loads are on their way and all
+// that it read from LDS has come, then for the block's other waves.
+template <int LOADS>
+__device__ inline void arrive() {
+    static_assert(LOADS < 64, "the counter's range");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((LOADS & 15) | 7 << 4 | (LOADS >> 4) << 14);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Orders a step's instructions: products with the reads of LDS and the loads
+// spread evenly between them, since a wave issues in order and would wait at
+// a full LDS queue with its matrix unit idle.
+template <int PRODUCTS, int READS, int LOADS>
+__device__ inline void interleave() {
+    constexpr int kOther = READS + LOADS;
+#pragma unroll
+    for (int i = 0, done = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        const int upto = (i + 1) * kOther / PRODUCTS;
+#pragma unroll
+        for (; done < upto; ++done) {
+            if (done < READS)
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            else
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+    }
 }
 
 // ------------------------------------------------------------ large products
 //
-// Four waves in a 2 x 2 square; each holds WN x WA tiles of 64 x 64 outputs
-// (rows of w by rows of a) in registers.
-
-// Tiles of one step of 128 columns, in registers on their way to LDS: a
-// thread moves 16 bytes of each tile's codes and one scale dword of each
-// operand.
-template <int N, int A>
-struct Stage {
-    int4v w[N], a[A];
-    int sw, sa;
-};
-
-template <int WN, int WA, typename T>
-__global__ __launch_bounds__(256, 1) void tiled_kernel(const uint8_t *__restrict__ a_codes,
-                                                       const uint8_t *__restrict__ a_scales,
-                                                       const uint8_t *__restrict__ w_codes,
-                                                       const uint8_t *__restrict__ w_scales, int64_t m, int64_t n,
-                                                       int kt, int64_t batch, int n_blocks, int a_blocks, int blocks_per_xcd,
-                                                       T *__restrict__ out, int64_t batch_stride,
-                                                       int64_t row_stride) {
-    constexpr int N = 2 * WN, A = 2 * WA;  // tiles of a block
-    constexpr int kStage = (N + A) * (kMx4CodeBytes + kMx4ScaleBytes), kSlots = 3;
+// GN x GA waves, each holding WN x WA tiles of 64 x 64 outputs (rows of w by
+// rows of a) in registers.
+template <int GN, int GA, int WN, int WA, typename T>
+__global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_kernel(
+    const uint8_t *__restrict__ a_codes, const uint8_t *__restrict__ a_scales, const uint8_t *__restrict__ w_codes,
+    const uint8_t *__restrict__ w_scales, int64_t m, int64_t n, int kt, int64_t batch, int n_blocks, int a_blocks,
+    int blocks_per_xcd, T *__restrict__ out, int64_t batch_stride, int64_t row_stride) {
+    constexpr int N = GN * WN, A = GA * WA, kThreads = 64 * GN * GA;  // tiles of a block
+    constexpr int kCodes = (N + A) * 256 / kThreads, kScales = ((N + A) * 64 + kThreads - 1) / kThreads;
+    constexpr int kLoads = kCodes + kScales, kSlots = 3;
+    // Every wave issues the same loads, so that it can count them: scales
+    // past the last tile's repeat its last ones, behind them.
+    constexpr int kStage = (N + A) * kMx4CodeBytes + kScales * kThreads * 4;
+    static_assert(kCodes * kThreads == (N + A) * 256, "whole chunks per thread");
     __shared__ __attribute__((aligned(16))) uint8_t lds[kSlots * kStage];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = wave & 1, wa = wave >> 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = wave % GN, wa = wave / GN;
     // Blocks go to the eight dies in turn; each die takes a contiguous range
-    // of tiles, the rows of a running fastest, so that a die's L2 serves one
-    // range of w to all of them.
+    // of the order below, in which 32 neighbours (a die's compute units) are
+    // 8 blocks of a by 4 of w: what its L2 serves to all of them is least.
     const int64_t id = static_cast<int64_t>(blockIdx.x & 7) * blocks_per_xcd + (blockIdx.x >> 3);
     const int64_t per_batch = static_cast<int64_t>(n_blocks) * a_blocks, b = id / per_batch;
-    const int nb = static_cast<int>(id % per_batch / a_blocks), ab = static_cast<int>(id % a_blocks);
-    const int64_t a_tiles = (m + 63) / 64, w_tiles = (n + 63) / 64;
     if (b >= batch) return;
+    const int in_batch = static_cast<int>(id % per_batch), strip = in_batch / (8 * n_blocks) * 8,
+              in_strip = in_batch % (8 * n_blocks), width = min(8, a_blocks - strip);
+    const int nb = in_strip / width, ab = strip + in_strip % width;
+    const int64_t a_tiles = (m + 63) / 64, w_tiles = (n + 63) / 64;
 
-    const uint8_t *wc[N], *ac[A];
-#pragma unroll
-    for (int j = 0; j < N; ++j)  // tiles past the end repeat the last one, unstored
-        wc[j] = w_codes + (b * w_tiles + min(static_cast<int64_t>(nb) * N + j, w_tiles - 1)) * kt * kMx4CodeBytes +
-                tid * 16;
-#pragma unroll
-    for (int j = 0; j < A; ++j)
-        ac[j] = a_codes + (b * a_tiles + min(static_cast<int64_t>(ab) * A + j, a_tiles - 1)) * kt * kMx4CodeBytes +
-                tid * 16;
-    const uint8_t *ws = w_scales +
-                        (b * w_tiles + min(static_cast<int64_t>(nb) * N + (wave & (N - 1)), w_tiles - 1)) * kt *
-                            kMx4ScaleBytes +
-                        lane * 4;
-    const uint8_t *as = a_scales +
-                        (b * a_tiles + min(static_cast<int64_t>(ab) * A + (wave & (A - 1)), a_tiles - 1)) * kt *
-                            kMx4ScaleBytes +
-                        lane * 4;
-
-    Stage<N, A> st;
-    auto fetch = [&](int k) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) st.w[j] = *reinterpret_cast<const int4v *>(wc[j] + static_cast<int64_t>(k) * kMx4CodeBytes);
-#pragma unroll
-        for (int j = 0; j < A; ++j) st.a[j] = *reinterpret_cast<const int4v *>(ac[j] + static_cast<int64_t>(k) * kMx4CodeBytes);
-        st.sw = *reinterpret_cast<const int *>(ws + static_cast<int64_t>(k) * kMx4ScaleBytes);
-        st.sa = *reinterpret_cast<const int *>(as + static_cast<int64_t>(k) * kMx4ScaleBytes);
+    // Tiles past the end repeat the last one, unstored.
+    auto tile_of = [&](int j) {
+        return j < N ? b * w_tiles + min(static_cast<int64_t>(nb) * N + j, w_tiles - 1)
+                     : b * a_tiles + min(static_cast<int64_t>(ab) * A + (j - N), a_tiles - 1);
     };
-    auto put = [&](int slot) {
-        uint8_t *p = lds + slot * kStage;
+    const uint8_t *code_src[kCodes], *scale_src[kScales];
 #pragma unroll
-        for (int j = 0; j < N; ++j) *reinterpret_cast<int4v *>(p + j * kMx4CodeBytes + tid * 16) = st.w[j];
-#pragma unroll
-        for (int j = 0; j < A; ++j) *reinterpret_cast<int4v *>(p + (N + j) * kMx4CodeBytes + tid * 16) = st.a[j];
-        uint8_t *q = p + (N + A) * kMx4CodeBytes;
-        if (wave < N) *reinterpret_cast<int *>(q + tid * 4) = st.sw;
-        if (wave < A) *reinterpret_cast<int *>(q + N * kMx4ScaleBytes + tid * 4) = st.sa;
-    };
-    auto w_frag = [&](int slot, int f) {
-        return *reinterpret_cast<const int4v *>(lds + slot * kStage + wn * WN * kMx4CodeBytes + f * 1024 + lane * 16);
-    };
-    auto a_frag = [&](int slot, int f) {
-        return *reinterpret_cast<const int4v *>(lds + slot * kStage + (N + wa * WA) * kMx4CodeBytes + f * 1024 +
-                                                lane * 16);
-    };
-    auto w_scale = [&](int slot, int t) {
-        return *reinterpret_cast<const int *>(lds + slot * kStage + (N + A) * kMx4CodeBytes +
-                                              (wn * WN + t) * kMx4ScaleBytes + lane * 4);
-    };
-    auto a_scale = [&](int slot, int t) {
-        return *reinterpret_cast<const int *>(lds + slot * kStage + (N + A) * kMx4CodeBytes +
-                                              (N + wa * WA + t) * kMx4ScaleBytes + lane * 4);
-    };
-
-    float4v acc[4 * WN][4 * WA] = {};
-    fetch(0);
-    put(0);
-    if (kt > 1) {
-        fetch(1);
-        put(1);
+    for (int i = 0; i < kCodes; ++i) {
+        const int c = i * kThreads + tid, j = c >> 8;
+        code_src[i] = (j < N ? w_codes : a_codes) + tile_of(j) * kt * kMx4CodeBytes + (c & 255) * 16;
     }
-    if (kt > 2) fetch(2);
-    int slot = 0;
-    for (int k = 0; k < kt; ++k) {
-        __syncthreads();
-        const int after = slot == 2 ? 0 : slot + 1, last = after == 2 ? 0 : after + 1;
-        int4v y[4 * WA];
-        int sy[WA];
 #pragma unroll
-        for (int f = 0; f < 4 * WA; ++f) y[f] = a_frag(slot, f);
+    for (int i = 0; i < kScales; ++i) {
+        const int c = min(i * kThreads + tid, (N + A) * 64 - 1), j = c >> 6;
+        scale_src[i] = (j < N ? w_scales : a_scales) + tile_of(j) * kt * kMx4ScaleBytes + (c & 63) * 4;
+    }
+    // Copies step k's tiles to a slot: 16 (or 4) bytes a lane, straight to LDS.
+    auto fetch = [&](int k, int slot) {
+        uint8_t *p = lds + slot * kStage, *q = p + (N + A) * kMx4CodeBytes;
 #pragma unroll
-        for (int t = 0; t < WA; ++t) sy[t] = a_scale(slot, t);
-        if (k + 2 < kt) put(last);
-        if (k + 3 < kt) fetch(k + 3);
+        for (int i = 0; i < kCodes; ++i)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void *)(code_src[i] + static_cast<int64_t>(k) * kMx4CodeBytes),
+                (__attribute__((address_space(3))) void *)(p + (i * kThreads + wave * 64) * 16), 16, 0, 0);
 #pragma unroll
-        for (int t = 0; t < WN; ++t) {
-            const int sx = w_scale(slot, t);
-            int4v x[4];
+        for (int i = 0; i < kScales; ++i)
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void *)(scale_src[i] +
+                                                                 static_cast<int64_t>(k) * kMx4ScaleBytes),
+                (__attribute__((address_space(3))) void *)(q + (i * kThreads + wave * 64) * 4), 4, 0, 0);
+    };
+    auto frag = [&](int slot, int tile, int f) {
+        return *reinterpret_cast<const int4v *>(lds + slot * kStage + tile * kMx4CodeBytes + f * 1024 + lane * 16);
+    };
+    auto scales = [&](int slot, int tile) {
+        return *reinterpret_cast<const int *>(lds + slot * kStage + (N + A) * kMx4CodeBytes + tile * kMx4ScaleBytes +
+                                              lane * 4);
+    };
+
+    float16v acc[2 * WN][2 * WA] = {};
+    // A step's operands in registers.
+    struct Operands {
+        int4v w[4 * WN], a[4 * WA];
+        int sw[WN], sa[WA];
+    } held[2];
+    auto read = [&](Operands &r, int slot) {
 #pragma unroll
-            for (int f = 0; f < 4; ++f) x[f] = w_frag(slot, 4 * t + f);
+        for (int t = 0; t < WA; ++t) r.sa[t] = scales(slot, N + wa * WA + t);
 #pragma unroll
-            for (int u = 0; u < WA; ++u)
+        for (int t = 0; t < WN; ++t) r.sw[t] = scales(slot, wn * WN + t);
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    auto *c = acc[4 * t];
-                    const int4v yy = y[4 * u + g];
-                    const int j = 4 * u + g;
-                    if (g == 0) {
-                        acc[4 * t + 0][j] = mfma<0, 0>(x[0], yy, acc[4 * t + 0][j], sx, sy[u]);
-                        acc[4 * t + 1][j] = mfma<1, 0>(x[1], yy, acc[4 * t + 1][j], sx, sy[u]);
-                        acc[4 * t + 2][j] = mfma<2, 0>(x[2], yy, acc[4 * t + 2][j], sx, sy[u]);
-                        acc[4 * t + 3][j] = mfma<3, 0>(x[3], yy, acc[4 * t + 3][j], sx, sy[u]);
-                    } else if (g == 1) {
-                        acc[4 * t + 0][j] = mfma<0, 1>(x[0], yy, acc[4 * t + 0][j], sx, sy[u]);
-                        acc[4 * t + 1][j] = mfma<1, 1>(x[1], yy, acc[4 * t + 1][j], sx, sy[u]);
-                        acc[4 * t + 2][j] = mfma<2, 1>(x[2], yy, acc[4 * t + 2][j], sx, sy[u]);
-                        acc[4 * t + 3][j] = mfma<3, 1>(x[3], yy, acc[4 * t + 3][j], sx, sy[u]);
-                    } else if (g == 2) {
-                        acc[4 * t + 0][j] = mfma<0, 2>(x[0], yy, acc[4 * t + 0][j], sx, sy[u]);
-                        acc[4 * t + 1][j] = mfma<1, 2>(x[1], yy, acc[4 * t + 1][j], sx, sy[u]);
-                        acc[4 * t + 2][j] = mfma<2, 2>(x[2], yy, acc[4 * t + 2][j], sx, sy[u]);
-                        acc[4 * t + 3][j] = mfma<3, 2>(x[3], yy, acc[4 * t + 3][j], sx, sy[u]);
-                    } else {
-                        acc[4 * t + 0][j] = mfma<0, 3>(x[0], yy, acc[4 * t + 0][j], sx, sy[u]);
-                        acc[4 * t + 1][j] = mfma<1, 3>(x[1], yy, acc[4 * t + 1][j], sx, sy[u]);
-                        acc[4 * t + 2][j] = mfma<2, 3>(x[2], yy, acc[4 * t + 2][j], sx, sy[u]);
-                        acc[4 * t + 3][j] = mfma<3, 3>(x[3], yy, acc[4 * t + 3][j], sx, sy[u]);
-                    }
-                    (void)c;
-                }
-        }
+        for (int f = 0; f < 4 * WA; ++f) r.a[f] = frag(slot, N + wa * WA, f);
+#pragma unroll
+        for (int f = 0; f < 4 * WN; ++f) r.w[f] = frag(slot, wn * WN, f);
+    };
+    auto multiply = [&](const Operands &r) {
+#pragma unroll
+        for (int t = 0; t < WN; ++t)
+#pragma unroll
+            for (int u = 0; u < WA; ++u) outer(acc, 2 * t, 2 * u, r.w + 4 * t, r.a + 4 * u, r.sw[t], r.sa[u]);
+        // Keeps the products on their side of the next barrier.
+#pragma unroll
+        for (int t = 0; t < 2 * WN; ++t)
+#pragma unroll
+            for (int u = 0; u < 2 * WA; ++u) asm volatile("" : "+v"(acc[t][u]));
+    };
+
+    // The ring of slots.  While step k multiplies, its own slot, already
+    // read, takes step k + kSlots, and the operands of step k + 1 are read
+    // from theirs; the barrier before says that step k is read and that step
+    // k + 1 has arrived everywhere.
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) fetch(min(i, kt - 1), i);
+    arrive<(kSlots - 1) * kLoads>();
+    read(held[0], 0);
+    int slot = 0, k = 0;
+    auto step = [&](int p) {
+        const int after = slot == kSlots - 1 ? 0 : slot + 1;
+        arrive<(kSlots - 2) * kLoads>();
+        __builtin_amdgcn_sched_barrier(0);
+        // Past the last step these read and load tiles that nothing uses:
+        // a branch would cost the registers that hold the result.
+        read(held[p ^ 1], after);
+        fetch(min(k + kSlots, kt - 1), slot);
+        multiply(held[p]);
+        interleave<8 * WN * WA, 5 * (WN + WA), kLoads>();
+        __builtin_amdgcn_sched_barrier(0);
         slot = after;
+        ++k;
+    };
+    while (k + 1 < kt) {
+        step(0);
+        step(1);
     }
-    const int64_t n0 = (static_cast<int64_t>(nb) * N + wn * WN) * 64 + (lane >> 4) * 4;
-    const int64_t m0 = (static_cast<int64_t>(ab) * A + wa * WA) * 64 + (lane & 15);
+    if (k < kt) step(0);
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);  // vmcnt(0): nothing may still be on its way to this block's LDS
+    const int64_t n0 = (static_cast<int64_t>(nb) * N + wn * WN) * 64;
+    const int64_t m0 = (static_cast<int64_t>(ab) * A + wa * WA) * 64 + (lane & 31);
 #pragma unroll
-    for (int j = 0; j < 4 * WA; ++j) {
-        const int64_t i = m0 + j * 16;
-        if (i < m) {
-            T *row = out + b * batch_stride + i * row_stride;
+    for (int j = 0; j < 2 * WA; ++j) {
+        const int64_t i = m0 + j * 32;
+        T *row = out + b * batch_stride + i * row_stride;
 #pragma unroll
-            for (int f = 0; f < 4 * WN; ++f) {
-                const int64_t c = n0 + f * 16;
-                if (c + 3 < n) {
-                    store4(row + c, acc[f][j]);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (c + e < n) store(row + c + e, acc[f][j][e]);
-                }
-            }
-        }
+        for (int f = 0; f < 2 * WN; ++f) store_rows(row, n0 + f * 32, n, i < m, lane, acc[f][j]);
     }
 }
 
-template <int WN, int WA, typename T>
+template <int GN, int GA, int WN, int WA, typename T>
 bool launch_tiled(const uint8_t *ac, const uint8_t *as, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m,
                   int64_t n, int64_t kt, T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
-    const int64_t nb = (mx4_row_tiles(n) + 2 * WN - 1) / (2 * WN), ab = (mx4_row_tiles(m) + 2 * WA - 1) / (2 * WA);
+    const int64_t nb = (mx4_row_tiles(n) + GN * WN - 1) / (GN * WN), ab = (mx4_row_tiles(m) + GA * WA - 1) / (GA * WA);
     const int64_t per = (batch * nb * ab + 7) / 8;
-    if (per * 8 > INT32_MAX || kt > INT32_MAX) return false;
-    tiled_kernel<WN, WA, T><<<dim3(static_cast<unsigned>(per * 8), 1), 256, 0, stream>>>(
-        ac, as, wc, ws, m, n, static_cast<int>(kt), batch, static_cast<int>(nb), static_cast<int>(ab), static_cast<int>(per),
-        out, batch_stride, row_stride);
+    if (nb * ab > INT32_MAX / 8 || per * 8 > INT32_MAX || kt > INT32_MAX) return false;
+    tiled_kernel<GN, GA, WN, WA, T><<<static_cast<unsigned>(per * 8), 64 * GN * GA, 0, stream>>>(
+        ac, as, wc, ws, m, n, static_cast<int>(kt), batch, static_cast<int>(nb), static_cast<int>(ab),
+        static_cast<int>(per), out, batch_stride, row_stride);
     return hipGetLastError() == hipSuccess;
+}
+
+template <int NW, int NA, int WAVES, int AHEAD, typename T, typename Left>
+bool launch_few(Left left, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m, int64_t n, int64_t kt,
+                T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
+    const int64_t nb = (n + 32 * NW - 1) / (32 * NW), mb = (m + 32 * NA - 1) / (32 * NA);
+    if (nb * mb > INT32_MAX || batch > 65535 || kt > INT32_MAX / 64) return false;
+    const int64_t most = std::is_same<Left, Packed>::value ? nb * mb : std::max<int64_t>(1, FGD_GRID / batch);
+    const dim3 grid(static_cast<unsigned>(std::min(nb * mb, most)), static_cast<unsigned>(batch));
+    few_kernel<NW, NA, WAVES, AHEAD, T, Left><<<grid, 64 * WAVES, 0, stream>>>(
+        left, wc, ws, m, n, static_cast<int>(kt), nb, mb, out, batch_stride, row_stride);
+    return hipGetLastError() == hipSuccess;
+}
+
+// Which kernel a product takes.
+enum Shape { kFew1x1, kFew1x1Deep, kFew1x2, kFew2x2, kTiled128, kTiled256 };
+
+Shape shape_of(int64_t batch, int64_t m, int64_t n, int64_t kt) {
+    constexpr int64_t kCus = 256;
+    auto blocks = [&](int64_t rows, int64_t cols) { return batch * ((m + rows - 1) / rows) * ((n + cols - 1) / cols); };
+    const int64_t small = blocks(128, 128), large = blocks(256, 256);
+    if (m > 32 && small >= kCus && kt > 0)
+        // Steps of the fullest compute unit: one of a 256 x 256 block costs
+        // 3.3 times one of a 128 x 128 block (1.1 and 0.33 us, the card full).
+        return 10 * ((small + kCus - 1) / kCus) >= 33 * ((large + kCus - 1) / kCus) ? kTiled256 : kTiled128;
+    // Below that a compute unit's block is the smaller, the fewer there are,
+    // and its waves share out the columns.  Eight waves for four: 5.2 us for
+    // 5.9 at 1 x 2048 x 8192, but 31 for 23 at 1 x 128256 x 2048.  At 256 x
+    // 8192 x 8192 these take 22 us and 128 x 128 tiles 30; at 512 x 8192 x
+    // 8192, 39 and 34.
+    if (blocks(32, 32) <= kCus) return kFew1x1Deep;
+    if (m <= 32) return kFew1x1;
+    return blocks(64, 32) <= kCus ? kFew1x2 : kFew2x2;
 }
 
 template <typename T>
-bool launch(const uint8_t *ac, const uint8_t *as, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m,
-            int64_t n, int64_t kt, T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
-    if (m > 64) return launch_tiled<2, 2>(ac, as, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
-    const int64_t nb = (mx4_row_tiles(n) + 3) / 4, mb = (m + 15) / 16, blocks = batch * nb * mb;
-    if (blocks > INT32_MAX) return false;
-    product_kernel<<<static_cast<int>(blocks), 256, 0, stream>>>(ac, as, wc, ws, m, n, kt, nb, mb, out, batch_stride,
-                                                                 row_stride);
-    return hipGetLastError() == hipSuccess;
+bool launch(Packed a, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m, int64_t n, int64_t kt, T *out,
+            int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
+    switch (shape_of(batch, m, n, kt)) {
+        case kFew1x1:
+            return launch_few<1, 1, 4, 4>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew1x1Deep:
+            return launch_few<1, 1, 8, 4>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew1x2:
+            return launch_few<1, 2, 8, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew2x2:
+            return launch_few<2, 2, 8, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kTiled128:
+            return launch_tiled<2, 2, 1, 1>(a.codes, a.scales, wc, ws, batch, m, n, kt, out, batch_stride, row_stride,
+                                            stream);
+        default:
+            return launch_tiled<2, 4, 2, 1>(a.codes, a.scales, wc, ws, batch, m, n, kt, out, batch_stride, row_stride,
+                                            stream);
+    }
+}
+
+template <typename T, typename X>
+bool launch_dense(Dense<X> x, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m, int64_t n, int64_t kt,
+                  T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
+    if (shape_of(batch, m, n, kt) == kFew1x1)
+        return launch_few<1, 1, 4, 4>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+    return launch_few<1, 1, 8, 4>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
 }
 
 }  // namespace
@@ -285,10 +516,34 @@ bool mx4_matmul_launch(const void *a_codes, const void *a_scales, const void *w_
     if (batch == 0 || m == 0 || n == 0) return true;
     const int64_t kt = mx4_col_tiles(k);
     auto u = [](const void *p) { return static_cast<const uint8_t *>(p); };
-    return bf16 ? launch(u(a_codes), u(a_scales), u(w_codes), u(w_scales), batch, m, n, kt,
-                         static_cast<uint16_t *>(out), batch_stride, row_stride, stream)
-                : launch(u(a_codes), u(a_scales), u(w_codes), u(w_scales), batch, m, n, kt, static_cast<float *>(out),
-                         batch_stride, row_stride, stream);
+    const Packed a = {u(a_codes), u(a_scales)};
+    return bf16 ? launch(a, u(w_codes), u(w_scales), batch, m, n, kt, static_cast<uint16_t *>(out), batch_stride,
+                         row_stride, stream)
+                : launch(a, u(w_codes), u(w_scales), batch, m, n, kt, static_cast<float *>(out), batch_stride,
+                         row_stride, stream);
+}
+
+bool mx4_linear_fuses(int64_t batch, int64_t m, int64_t n, int64_t k) {
+    if (batch == 0 || m == 0 || n == 0 || k == 0 || m > 32) return false;
+    const int64_t kt = mx4_col_tiles(k);
+    const Shape shape = shape_of(batch, m, n, kt);
+    return (shape == kFew1x1 && m * 4 * kt <= 256) || (shape == kFew1x1Deep && m * 4 * kt <= 512);
+}
+
+bool mx4_linear_launch(const void *x, bool x_bf16, int64_t x_batch_stride, int64_t x_row_stride, const void *w_codes,
+                       const void *w_scales, int64_t batch, int64_t m, int64_t n, int64_t k, void *out, bool bf16,
+                       int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
+    const int64_t kt = mx4_col_tiles(k);
+    auto *wc = static_cast<const uint8_t *>(w_codes), *ws = static_cast<const uint8_t *>(w_scales);
+    auto go = [&](auto dense) {
+        return bf16 ? launch_dense(dense, wc, ws, batch, m, n, kt, static_cast<uint16_t *>(out), batch_stride,
+                                   row_stride, stream)
+                    : launch_dense(dense, wc, ws, batch, m, n, kt, static_cast<float *>(out), batch_stride, row_stride,
+                                   stream);
+    };
+    const bool vectors = mx4_rows_aligned(x, x_bf16, x_batch_stride, x_row_stride);
+    return x_bf16 ? go(Dense<uint16_t>{static_cast<const uint16_t *>(x), x_batch_stride, x_row_stride, k, vectors})
+                  : go(Dense<float>{static_cast<const float *>(x), x_batch_stride, x_row_stride, k, vectors});
 }
 
 }  // namespace fgd

@@ -103,7 +103,7 @@ def test_every_binade_and_tie(env):
     q = fgd.mx4_quantize(_tensor(torch, x, "f32"))
     assert np.array_equal(_host(fgd.mx4_dequantize(q)), ref.mx4_values(x))
     s = q.scales.cpu().numpy().reshape(-1, 64, 4)  # [row tile][lane][fragment]: one column tile
-    got = np.array([s[r // 64, r % 16, (r % 64) // 16] for r in range(x.shape[0])])
+    got = np.array([s[r // 64, r % 32, 2 * (r % 64 // 32)] for r in range(x.shape[0])])
     assert np.array_equal(got, ref.mx4_scale_bytes(x)[:, 0])
 
 
@@ -137,7 +137,9 @@ def _check_product(got, a, w):
 
 PRODUCTS = [(1, 1, 1), (1, 5, 33), (1, 128, 256), (2, 64, 1000), (3, 257, 129), (16, 300, 96), (17, 65, 640),
             (31, 1000, 224), (64, 64, 128), (65, 33, 300), (100, 513, 2048), (129, 255, 1024), (256, 256, 256),
-            (257, 300, 520), (300, 1030, 385), (1, 700, 9000), (40, 90, 8200)]
+            (257, 300, 520), (300, 1030, 385), (1, 700, 9000), (40, 90, 8200),
+            (1, 9000, 2048), (4, 9000, 2048), (5, 9000, 2048), (30, 9000, 100), (2, 9000, 8192), (48, 8200, 300),
+            (70, 4200, 1100), (300, 2100, 700), (520, 2049, 1153)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
