@@ -454,8 +454,7 @@ fgd_status fgd_mx4_quantize(const void *x, int32_t dtype, int32_t batch, int64_t
 
 /* Writes the values that codes and scales stand for to out, rows contiguous
  * (element (b, r, k) at b * batch_stride + r * row_stride + k).  Exact in
- * either dtype, but for bf16 values below its smallest normal number, which
- * round to its denormals.  Enqueued on `stream`. */
+ * either dtype.  Enqueued on `stream`. */
 fgd_status fgd_mx4_dequantize(const void *codes, const void *scales, int32_t batch, int64_t rows, int64_t cols,
                               void *out, int32_t dtype, int64_t batch_stride, int64_t row_stride, void *stream);
 

@@ -33,12 +33,6 @@ inline int64_t mx4_tiles(int64_t batch, int64_t rows, int64_t cols) {
     return batch * mx4_row_tiles(rows) * mx4_col_tiles(cols);
 }
 
-// Whether every row of an array starts on a 16-byte boundary.
-inline bool mx4_rows_aligned(const void *x, bool bf16, int64_t batch_stride, int64_t row_stride) {
-    const int64_t es = bf16 ? 2 : 4;
-    return reinterpret_cast<uintptr_t>(x) % 16 == 0 && batch_stride * es % 16 == 0 && row_stride * es % 16 == 0;
-}
-
 // x[b][r][k] at b * batch_stride + r * row_stride + k * col_stride, one of
 // the last two strides 1.  False if a launch failed.
 bool mx4_quantize_launch(const void *x, bool bf16, int64_t batch, int64_t rows, int64_t cols, int64_t batch_stride,

@@ -14,30 +14,28 @@ __device__ inline float widen<float>(float v) { return v; }
 template <>
 __device__ inline float widen<uint16_t>(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
 
-// `valid` (at most 32) values from src, zeros behind them; src is on a
-// 16-byte boundary where `vectors`.
-__device__ inline void load_block(const float *src, int64_t valid, bool vectors, float (&v)[32]) {
-    if (vectors && valid >= 32) {
+// Sixteen bytes of elements at an address aligned to its element only.
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+    uint32_t w[4];
+};
+
+// `valid` (32 at most) values from src, zeros behind them.
+template <typename T>
+__device__ inline void load_block(const T *src, int64_t valid, float (&v)[32]) {
+    constexpr int kPer = 16 / sizeof(T);
+    if (valid >= 32) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 f = reinterpret_cast<const float4 *>(src)[i];
-            v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = i < valid ? src[i] : 0.0f;
-    }
-}
-__device__ inline void load_block(const uint16_t *src, int64_t valid, bool vectors, float (&v)[32]) {
-    if (vectors && valid >= 32) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 u = reinterpret_cast<const uint4 *>(src)[i];
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        for (int i = 0; i < 32 / kPer; ++i) {
+            const Pack<T> u = reinterpret_cast<const Pack<T> *>(src)[i];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-                v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                if constexpr (sizeof(T) == 4) {
+                    v[4 * i + j] = __uint_as_float(u.w[j]);
+                } else {
+                    v[8 * i + 2 * j] = __uint_as_float(u.w[j] << 16);
+                    v[8 * i + 2 * j + 1] = __uint_as_float(u.w[j] & 0xffff0000u);
+                }
             }
         }
     } else {

@@ -127,9 +127,6 @@ __device__ inline void products(float16v (&acc)[2][NA], const int4v (&x)[2][2], 
     }
 }
 
-#ifndef FGD_GRID
-#define FGD_GRID 512
-#endif
 // The left operand: in the 4-bit format, or (X: float, or uint16_t for bf16)
 // dense rows that the block quantises itself.
 struct Packed {
@@ -139,7 +136,6 @@ template <typename X>
 struct Dense {
     const X *x;
     int64_t batch_stride, row_stride, cols;
-    bool vectors;  // rows on 16-byte boundaries
 };
 
 template <int NW, int NA, int WAVES, int AHEAD, typename T, typename Left>
@@ -206,7 +202,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Left left, const uint8_
                         const int64_t c0 = 32 * static_cast<int64_t>(block);
                         float v[32];
                         load_block(left.x + b * left.batch_stride + row * left.row_stride + c0, left.cols - c0,
-                                   left.vectors, v);
+                                   v);
                         uint4 c;
                         x_scales[threadIdx.x] = static_cast<uint8_t>(encode_block(v, c));
                         x_codes[threadIdx.x] = int4v{static_cast<int>(c.x), static_cast<int>(c.y),
@@ -451,7 +447,10 @@ bool launch_few(Left left, const uint8_t *wc, const uint8_t *ws, int64_t batch, 
                 T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
     const int64_t nb = (n + 32 * NW - 1) / (32 * NW), mb = (m + 32 * NA - 1) / (32 * NA);
     if (nb * mb > INT32_MAX || batch > 65535 || kt > INT32_MAX / 64) return false;
-    const int64_t most = std::is_same<Left, Packed>::value ? nb * mb : std::max<int64_t>(1, FGD_GRID / batch);
+    // Dense rows are quantised once a block, so there are two blocks a compute
+    // unit, which go round (768 blocks: 34 us at 1 x 128256 x 2048, 512: 28,
+    // 256: 36).
+    const int64_t most = std::is_same<Left, Packed>::value ? nb * mb : std::max<int64_t>(1, 512 / batch);
     const dim3 grid(static_cast<unsigned>(std::min(nb * mb, most)), static_cast<unsigned>(batch));
     few_kernel<NW, NA, WAVES, AHEAD, T, Left><<<grid, 64 * WAVES, 0, stream>>>(
         left, wc, ws, m, n, static_cast<int>(kt), nb, mb, out, batch_stride, row_stride);
@@ -541,9 +540,8 @@ bool mx4_linear_launch(const void *x, bool x_bf16, int64_t x_batch_stride, int64
                     : launch_dense(dense, wc, ws, batch, m, n, kt, static_cast<float *>(out), batch_stride, row_stride,
                                    stream);
     };
-    const bool vectors = mx4_rows_aligned(x, x_bf16, x_batch_stride, x_row_stride);
-    return x_bf16 ? go(Dense<uint16_t>{static_cast<const uint16_t *>(x), x_batch_stride, x_row_stride, k, vectors})
-                  : go(Dense<float>{static_cast<const float *>(x), x_batch_stride, x_row_stride, k, vectors});
+    return x_bf16 ? go(Dense<uint16_t>{static_cast<const uint16_t *>(x), x_batch_stride, x_row_stride, k})
+                  : go(Dense<float>{static_cast<const float *>(x), x_batch_stride, x_row_stride, k});
 }
 
 }  // namespace fgd
