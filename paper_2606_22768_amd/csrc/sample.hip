@@ -12,28 +12,36 @@
 // first among equal ones.  Top-k, top-p and min-p each keep a prefix of that
 // order, so their intersection is the shortest of the three and its mass the
 // least of theirs; the drawn token is the one whose span of mass holds
-// floor(u mass).  Both searches (where top-k or top-p cuts, and the draw)
-// are for the group of equal logits at a given count or mass of the order,
-// found by radix descent over the logits' order-preserving keys.
+// floor(u mass).  So a row is sampled by finding places in the order at a
+// given count or mass, without sorting it:
+//   1. the row's maximum;
+//   2. a histogram of masses (and, for top-k, counts) over bins of t, each
+//      1/64 wide: 2048 bins reach the smallest mass;
+//   3. of the few bins in which a cut or the draw can fall (a cut that is
+//      known to a bin gives a range for the next), the tokens, collected,
+//      sorted and summed up: these give the exact places.
+// Where those bins hold more than the room (thousands of nearly equal
+// tokens), the row is searched by radix descent over its logits' bits
+// instead, which needs no room and takes many more passes.
+//
+// Many rows: a block per row.  Fewer: a row's slices on several blocks, a
+// kernel for each step, histogram and tokens in the workspace; the block of a
+// row that ends last finds its token.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "sample.hpp"
 
 namespace fgd {
 namespace {
 
-constexpr int kThreads = 1024, kBins = 2048, kBinBits = 11;
+typedef unsigned long long u64;
 
-struct Shared {
-    uint32_t count[kBins];
-    unsigned long long mass[kBins];
-    unsigned long long wave_count[kThreads / 64], wave_mass[kThreads / 64];
-    // The bin found by a search, and what stands before it.
-    uint32_t bin, bin_count;
-    unsigned long long bin_mass, above_count, above_mass;
-    float wave_max[kThreads / 64];
-    int wave_nan[kThreads / 64], index;
-};
+constexpr int kBins = 2048, kBinBits = 11;
+constexpr int kRoom = 4096;          // tokens that a row's search can collect
+constexpr int kMostSlices = 64;      // of a row
+constexpr float kPerOctave = 64.0f;  // bins per factor of two of weight
 
 __device__ inline float value(float v) { return v; }
 __device__ inline float value(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
@@ -43,215 +51,645 @@ __device__ inline uint32_t key_of(float z) {
     const uint32_t b = __float_as_uint(z + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ inline float logit_of(uint32_t key) {
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
 
-__device__ inline float weight(float z, float top, float c) {
+// log2 of a token's weight; the largest logit's is 0, an infinite one's too.
+// NaN (an infinite difference times c = 0) stands for no weight.
+__device__ inline float scaled(float z, float top, float c) {
 #pragma clang fp contract(off)
-    const float t = z == top ? 0.0f : (z - top) * c;
-    return z == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(fmaxf(t, -126.0f));
+    return z == top ? 0.0f : (z - top) * c;
 }
-
+__device__ inline float weight(float t) { return __builtin_amdgcn_exp2f(fmaxf(t, -126.0f)); }
 __device__ inline uint32_t mass_of(float w) { return static_cast<uint32_t>(fmaf(w, 0x1p31f, 0.5f)); }
-
-// f(index, logit) for every element of a row, by the whole block.
-template <typename T, typename F>
-__device__ inline void scan_row(const T *row, int vocab, F f) {
-    for (int i = threadIdx.x; i < vocab; i += kThreads) f(i, value(row[i]));
+// The bin of a token that has mass (t >= -32).
+__device__ inline uint32_t bin_of(float t) {
+    return min(static_cast<uint32_t>(-kPerOctave * t), static_cast<uint32_t>(kBins - 1));
 }
 
-__device__ inline unsigned long long wave_sum(unsigned long long v) {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
-// Finds the first bin, from the highest, at whose end the measure (counts,
-// or masses) exceeds `target`; the histogram's total does.  Each thread owns
-// two bins.
-__device__ void find_bin(Shared &s, bool by_mass, unsigned long long target) {
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const int hi = kBins - 1 - 2 * t, lo = hi - 1;
-    unsigned long long c = s.count[hi] + static_cast<unsigned long long>(s.count[lo]), m = s.mass[hi] + s.mass[lo];
-    unsigned long long ci = c, mi = m;  // inclusive sums within the wave
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned long long cu = __shfl_up(ci, o), mu = __shfl_up(mi, o);
-        if (lane >= o) ci += cu, mi += mu;
+// f(index, logit) for the elements [lo, hi) of a row, by a block of TH threads.
+template <int TH, typename T, typename F>
+__device__ inline void scan_row(const T *row, int lo, int hi, F f) {
+    constexpr int kPer = 16 / sizeof(T), kAhead = 4;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + lo);
+    const int head = min(hi - lo, static_cast<int>((16 - (at & 15)) & 15) / static_cast<int>(sizeof(T)));
+    const int vectors = (hi - lo - head) / kPer, first = lo + head, tail = first + vectors * kPer;
+    const uint4 *v = reinterpret_cast<const uint4 *>(row + first);
+    auto each = [&](int i, uint4 u) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 4) {
+                f(first + i * 4 + j, __uint_as_float(w[j]));
+            } else {
+                f(first + i * 8 + 2 * j, __uint_as_float(w[j] << 16));
+                f(first + i * 8 + 2 * j + 1, __uint_as_float(w[j] & 0xffff0000u));
+            }
+        }
+    };
+    int i = threadIdx.x;
+    for (; i + (kAhead - 1) * TH < vectors; i += kAhead * TH) {
+        uint4 u[kAhead];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) u[a] = v[i + a * TH];
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) each(i + a * TH, u[a]);
     }
-    if (lane == 63) s.wave_count[wave] = ci, s.wave_mass[wave] = mi;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) ci += s.wave_count[w], mi += s.wave_mass[w];
-    unsigned long long ce = ci - c, me = mi - m;  // before this thread's bins
-    const unsigned long long before = by_mass ? me : ce, through = by_mass ? mi : ci;
-    if (before <= target && target < through) {
-        const unsigned long long first = by_mass ? s.mass[hi] : s.count[hi];
-        const int bin = target < before + first ? hi : lo;
-        if (bin == lo) ce += s.count[hi], me += s.mass[hi];
-        s.bin = bin;
-        s.bin_count = s.count[bin];
-        s.bin_mass = s.mass[bin];
-        s.above_count = ce;
-        s.above_mass = me;
-    }
-    __syncthreads();
+    for (; i < vectors; i += TH) each(i, v[i]);
+    const int rest = static_cast<int>(threadIdx.x);
+    if (rest < head)
+        f(lo + rest, value(row[lo + rest]));
+    else if (tail + rest - head < hi)
+        f(tail + rest - head, value(row[tail + rest - head]));
 }
 
-struct Group {  // the tokens of one logit in the order
-    uint32_t key, count;
-    unsigned long long above_count, above_mass, mass;  // mass: of one token
+// A row's settings, made definite.
+struct Settings {
+    float c, top_p, min_p;
+    int k;  // 1..vocab
 };
 
-template <typename T>
-__device__ Group find_group(Shared &s, const T *row, int vocab, float top, float c, bool by_mass,
-                            unsigned long long target) {
-    uint32_t prefix = 0;
-    unsigned long long above_count = 0, above_mass = 0;
+__device__ inline Settings settings_of(const SampleSettings &set, int64_t r, int vocab) {
+    Settings s;
+    const float temperature = set.temperature_rows ? set.temperature_rows[r] : set.temperature;
+    s.c = 1.0f / temperature;
+    s.c = s.c * 1.44269504088896340736f;
+    const bool greedy = !(temperature > 0.0f) || s.c == __builtin_inff();
+    if (greedy) s.c = 1.0f;
+    s.k = greedy ? 1 : set.top_k_rows ? set.top_k_rows[r] : set.top_k;
+    if (s.k <= 0 || s.k > vocab) s.k = vocab;
+    s.top_p = set.top_p_rows ? set.top_p_rows[r] : set.top_p;
+    s.min_p = set.min_p_rows ? set.min_p_rows[r] : set.min_p;
+    if (s.min_p > 1.0f) s.min_p = 1.0f;
+    return s;
+}
+
+// The mass that top-p asks for, of a total.
+__device__ inline u64 nucleus(float top_p, u64 total) {
+    if (!(top_p < 1.0f)) return total;
+    const double want = ceil(static_cast<double>(top_p) * static_cast<double>(total));
+    return min(want >= 1.0 ? static_cast<u64>(want) : u64{1}, total);
+}
+// The place of the draw, of a total of at least 1.
+__device__ inline u64 place(float u, u64 total) {
+    const double at = static_cast<double>(u) * static_cast<double>(total);
+    return min(at > 0.0 ? static_cast<u64>(at) : u64{0}, total - 1);
+}
+
+template <int TH>
+struct Shared {
+    u64 mass[kBins + 1];        // a histogram, then the sums before each bin; the total
+    uint32_t count[kBins + 1];
+    u64 list[kRoom];            // key, then ~index: the larger is the earlier in the order
+    u64 wave_a[TH / 64], wave_b[TH / 64];
+    u64 found_mass, found_count, total;
+    uint32_t found[2], listed, last;
+    float wave_max[TH / 64];
+};
+
+// The largest value of the block's, NaN if one is.
+template <int TH>
+__device__ inline float block_max(Shared<TH> &s, float best, bool bad) {
+    for (int o = 32; o; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
+    if (__any(bad)) best = __builtin_nanf("");
+    if ((threadIdx.x & 63) == 0) s.wave_max[threadIdx.x >> 6] = best;
+    __syncthreads();
+    best = s.wave_max[0];
+    for (int w = 1; w < TH / 64; ++w) {
+        const float v = s.wave_max[w];
+        best = v != v || best != best ? __builtin_nanf("") : fmaxf(best, v);
+    }
+    __syncthreads();
+    return best;
+}
+
+// Sums of a and b over the threads before this one; the totals in ta, tb.
+template <int TH>
+__device__ inline void scan_threads(Shared<TH> &s, u64 &a, u64 &b, u64 &ta, u64 &tb) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 ia = a, ib = b;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const u64 ua = __shfl_up(ia, o), ub = __shfl_up(ib, o);
+        if (lane >= o) ia += ua, ib += ub;
+    }
+    if (lane == 63) s.wave_a[wave] = ia, s.wave_b[wave] = ib;
+    __syncthreads();
+    a = ia - a, b = ib - b;
+    ta = tb = 0;
+    for (int w = 0; w < TH / 64; ++w) {
+        if (w == wave) a += ta, b += tb;
+        ta += s.wave_a[w], tb += s.wave_b[w];
+    }
+    __syncthreads();
+}
+
+template <int TH>
+__device__ inline void clear_bins(Shared<TH> &s) {
+    for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = 0, s.count[i] = 0;
+    __syncthreads();
+}
+
+// Turns the histogram into the sums before each bin.
+template <int TH>
+__device__ inline void scan_bins(Shared<TH> &s) {
+    constexpr int kOwn = kBins / TH;
+    u64 m[kOwn], a = 0, b = 0, ta, tb;
+    uint32_t c[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        m[i] = s.mass[threadIdx.x * kOwn + i], c[i] = s.count[threadIdx.x * kOwn + i];
+        a += m[i], b += c[i];
+    }
+    scan_threads(s, a, b, ta, tb);
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        s.mass[threadIdx.x * kOwn + i] = a, s.count[threadIdx.x * kOwn + i] = static_cast<uint32_t>(b);
+        a += m[i], b += c[i];
+    }
+    if (threadIdx.x == 0) s.mass[kBins] = ta, s.count[kBins] = static_cast<uint32_t>(tb);
+    __syncthreads();
+}
+
+// The bins that hold the places x0 and x1 of mass (below the total).
+template <int TH>
+__device__ inline void bins_at(Shared<TH> &s, u64 x0, u64 x1, uint32_t &b0, uint32_t &b1) {
+    for (int bin = threadIdx.x; bin < kBins; bin += TH) {
+        const u64 lo = s.mass[bin], hi = s.mass[bin + 1];
+        if (lo <= x0 && x0 < hi) s.found[0] = bin;
+        if (lo <= x1 && x1 < hi) s.found[1] = bin;
+    }
+    __syncthreads();
+    b0 = s.found[0], b1 = s.found[1];
+    __syncthreads();
+}
+
+// The bins that a row's search needs: three ranges, from .. from + span.
+struct Wanted {
+    uint32_t from[3], span[3];
+    __device__ bool has(uint32_t bin) const {
+        return bin - from[0] <= span[0] || bin - from[1] <= span[1] || bin - from[2] <= span[2];
+    }
+};
+
+// From the summed histogram.  A step's total, with which the next one works,
+// is known to a range lo..hi: of top-k's cut its bin is wanted, of top-p's
+// and the draw's the bins from one end's to the other's.  kept: the mass
+// that min-p keeps.
+template <int TH>
+__device__ inline Wanted wanted_bins(Shared<TH> &s, const Settings &set, float u, u64 kept) {
+    Wanted w;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w.from[i] = kBins, w.span[i] = 0;  // none
+    u64 lo = s.mass[kBins], hi = lo;
+    const uint32_t k = static_cast<uint32_t>(set.k);
+    uint32_t b0, b1;
+    if (k < s.count[kBins]) {
+        for (int bin = threadIdx.x; bin < kBins; bin += TH)
+            if (s.count[bin] < k && k <= s.count[bin + 1]) s.found[0] = bin;
+        __syncthreads();
+        b0 = s.found[0];
+        __syncthreads();
+        w.from[0] = b0;
+        lo = s.mass[b0], hi = s.mass[b0 + 1];
+    }
+    if (set.top_p < 1.0f) {
+        const u64 p0 = max(nucleus(set.top_p, lo), u64{1}), p1 = nucleus(set.top_p, hi);
+        bins_at(s, p0 - 1, p1 - 1, b0, b1);
+        w.from[1] = b0, w.span[1] = b1 - b0;
+        lo = p0, hi = min(hi, s.mass[b1 + 1]);
+    }
+    lo = max(min(lo, kept), u64{1}), hi = min(hi, kept);
+    bins_at(s, place(u, lo), place(u, hi), b0, b1);
+    w.from[2] = b0, w.span[2] = b1 - b0;
+    return w;
+}
+
+// Sorts list[0, n), n a power of two, from the largest.
+template <int TH>
+__device__ inline void sort_list(u64 *list, int n) {
+    for (int size = 2; size <= n; size <<= 1)
+        for (int step = size >> 1; step; step >>= 1) {
+            for (int i = threadIdx.x; i < n / 2; i += TH) {
+                const int a = 2 * i - (i & (step - 1)), b = a + step;
+                const u64 x = list[a], y = list[b];
+                if ((x < y) == ((a & size) == 0)) list[a] = y, list[b] = x;
+            }
+            __syncthreads();
+        }
+}
+
+// Finds the token among those collected, which are all of the wanted bins'.
+template <int TH>
+__device__ inline void finish(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
+                              int32_t *token, float *prob) {
+    int n = 1;
+    while (n < listed) n <<= 1;
+    for (int i = listed + threadIdx.x; i < n; i += TH) s.list[i] = 0;
+    __syncthreads();
+    sort_list<TH>(s.list, n);
+    const int own = (n + TH - 1) / TH, base = threadIdx.x * own, end = min(base + own, listed);
+    auto t_at = [&](int i) { return scaled(logit_of(static_cast<uint32_t>(s.list[i] >> 32)), top, set.c); };
+    u64 sum = 0, none = 0, t0, t1;
+    for (int i = base; i < end; ++i) sum += mass_of(weight(t_at(i)));
+    scan_threads(s, sum, none, t0, t1);
+    // A bin's sums become those to add to a place in the list.
+    u64 at = sum;
+    for (int i = base; i < end; ++i) {
+        const float t = t_at(i);
+        const uint32_t bin = bin_of(t);
+        if (i == 0 || bin_of(t_at(i - 1)) != bin) s.mass[bin] -= at, s.count[bin] -= i;
+        at += mass_of(weight(t));
+    }
+    u64 total = s.mass[kBins];
+    __syncthreads();
+    if (static_cast<uint32_t>(set.k) < s.count[kBins]) {
+        at = sum;
+        for (int i = base; i < end; ++i) {
+            const float t = t_at(i);
+            const uint32_t bin = bin_of(t), m = mass_of(weight(t));
+            at += m;
+            if (s.count[bin] + i == static_cast<uint32_t>(set.k) - 1) s.total = s.mass[bin] + at;
+        }
+        __syncthreads();
+        total = s.total;
+        __syncthreads();
+    }
+    const u64 limit = nucleus(set.top_p, total);
+    if (limit < total) {
+        at = sum;
+        for (int i = base; i < end; ++i) {
+            const float t = t_at(i);
+            const uint32_t bin = bin_of(t), m = mass_of(weight(t));
+            const u64 before = s.mass[bin] + at;
+            if (before < limit && limit <= before + m) s.total = before + m;
+            at += m;
+        }
+        __syncthreads();
+        total = s.total;
+    }
+    total = min(total, kept);
+    const u64 target = place(u, total);
+    at = sum;
+    for (int i = base; i < end; ++i) {
+        const float t = t_at(i);
+        const uint32_t bin = bin_of(t), m = mass_of(weight(t));
+        const u64 before = s.mass[bin] + at;
+        if (before <= target && target < before + m) {
+            *token = static_cast<int32_t>(~static_cast<uint32_t>(s.list[i]));
+            if (prob) *prob = static_cast<float>(m) / static_cast<float>(total);
+        }
+        at += m;
+    }
+}
+
+// ------------------------------------------------------- by radix descent
+
+struct Group {  // the tokens of one logit in the order
+    uint32_t key;
+    u64 above_count, above_mass, mass;  // mass: of one token
+};
+
+// The first bin, from the highest, through which the measure exceeds
+// `target`.
+template <int TH>
+__device__ inline void find_bin(Shared<TH> &s, bool by_mass, u64 target) {
+    constexpr int kOwn = kBins / TH;
+    u64 a = 0, b = 0, ta, tb;
+    for (int i = 0; i < kOwn; ++i) {
+        const int bin = kBins - 1 - (threadIdx.x * kOwn + i);
+        a += s.count[bin], b += s.mass[bin];
+    }
+    scan_threads(s, a, b, ta, tb);
+    for (int i = 0; i < kOwn; ++i) {
+        const int bin = kBins - 1 - (threadIdx.x * kOwn + i);
+        const u64 before = by_mass ? b : a, own = by_mass ? s.mass[bin] : s.count[bin];
+        if (before <= target && target < before + own) s.found[0] = bin, s.found_count = a, s.found_mass = b;
+        a += s.count[bin], b += s.mass[bin];
+    }
+    __syncthreads();
+}
+
+template <int TH, typename T>
+__device__ Group find_group(Shared<TH> &s, const T *row, int vocab, float top, float c, bool by_mass, u64 target) {
+    Group g = {0, 0, 0, 0};
     const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
     for (int level = 0; level < 3; ++level) {
         const int shift = shifts[level];
         const uint32_t mask = (1u << bits[level]) - 1;
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0, s.mass[i] = 0;
-        __syncthreads();
-        scan_row(row, vocab, [&](int, float z) {
+        clear_bins(s);
+        scan_row<TH>(row, 0, vocab, [&](int, float z) {
             const uint32_t key = key_of(z);
-            if (level && (key >> (shift + bits[level])) != prefix) return;
-            const uint32_t bin = (key >> shift) & mask;
+            if (level && (key >> (shift + bits[level])) != g.key) return;
+            const uint32_t bin = (key >> shift) & mask, m = mass_of(weight(scaled(z, top, c)));
+            if (!m) return;  // no place falls on it
             atomicAdd(&s.count[bin], 1u);
-            const uint32_t m = mass_of(weight(z, top, c));
-            if (m) atomicAdd(&s.mass[bin], static_cast<unsigned long long>(m));
+            atomicAdd(&s.mass[bin], static_cast<u64>(m));
         });
         __syncthreads();
         find_bin(s, by_mass, target);
-        const unsigned long long at = by_mass ? s.above_mass : s.above_count;
-        target -= at;
-        above_count += s.above_count;
-        above_mass += s.above_mass;
-        prefix = prefix << bits[level] | s.bin;
+        const uint32_t bin = s.found[0];
+        target -= by_mass ? s.found_mass : s.found_count;
+        g.above_count += s.found_count;
+        g.above_mass += s.found_mass;
+        g.key = g.key << bits[level] | bin;
+        g.mass = s.mass[bin] / s.count[bin];
         __syncthreads();
     }
-    Group g;
-    g.key = prefix;
-    g.count = s.bin_count;
-    g.mass = s.bin_mass / s.bin_count;
-    g.above_count = above_count;
-    g.above_mass = above_mass;
-    __syncthreads();
     return g;
 }
 
-// The index of the n-th token of key `key`, by radix descent over indices.
-template <typename T>
-__device__ int find_index(Shared &s, const T *row, int vocab, uint32_t key, uint32_t n) {
+// The index of the n-th token of key `key`.
+template <int TH, typename T>
+__device__ int find_index(Shared<TH> &s, const T *row, int vocab, uint32_t key, u64 n) {
     uint32_t prefix = 0;
-    const int shifts[3] = {22, 11, 0};
-    for (int level = 0; level < 3; ++level) {
-        const int shift = shifts[level];
-        for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0, s.mass[i] = 0;
-        __syncthreads();
-        scan_row(row, vocab, [&](int i, float z) {
+    for (int shift = 22; shift >= 0; shift -= kBinBits) {
+        clear_bins(s);
+        scan_row<TH>(row, 0, vocab, [&](int i, float z) {
             const uint32_t r = ~static_cast<uint32_t>(i);  // find_bin counts from the highest bin
-            if (key_of(z) != key || (level && (r >> (shift + kBinBits)) != prefix)) return;
+            if (key_of(z) != key || (shift < 22 && (r >> (shift + kBinBits)) != prefix)) return;
             atomicAdd(&s.count[(r >> shift) & (kBins - 1)], 1u);
         });
         __syncthreads();
         find_bin(s, false, n);
-        n -= static_cast<uint32_t>(s.above_count);
-        prefix = prefix << kBinBits | s.bin;
+        n -= s.found_count;
+        prefix = prefix << kBinBits | s.found[0];
         __syncthreads();
     }
-    return static_cast<int>(~prefix & 0xffffffffu);
+    return static_cast<int>(~prefix);
 }
 
+// all, counted: the mass and number of the tokens that have mass.
+template <int TH, typename T>
+__device__ __noinline__ void search_row(Shared<TH> &s, const T *row, int vocab, const Settings &set, float u, u64 all,
+                                        u64 counted, u64 kept, float top, int32_t *token, float *prob) {
+    u64 total = all;
+    if (static_cast<u64>(set.k) < counted) {
+        const Group g = find_group(s, row, vocab, top, set.c, false, set.k - 1);
+        total = g.above_mass + (set.k - g.above_count) * g.mass;
+    }
+    const u64 limit = nucleus(set.top_p, total);
+    if (limit < total) {
+        const Group g = find_group(s, row, vocab, top, set.c, true, limit - 1);
+        total = g.above_mass + ((limit - 1 - g.above_mass) / g.mass + 1) * g.mass;
+    }
+    total = min(total, kept);
+    const u64 target = place(u, total);
+    const Group g = find_group(s, row, vocab, top, set.c, true, target);
+    const int index = find_index(s, row, vocab, g.key, (target - g.above_mass) / g.mass);
+    if (threadIdx.x == 0) {
+        *token = index;
+        if (prob) *prob = static_cast<float>(g.mass) / static_cast<float>(total);
+    }
+    __syncthreads();
+}
+
+// ------------------------------------------------------------------ steps
+
+template <int TH, typename T>
+__device__ inline float slice_max(Shared<TH> &s, const T *row, int lo, int hi) {
+    float best = -__builtin_inff();
+    bool bad = false;
+    scan_row<TH>(row, lo, hi, [&](int, float z) {
+        bad |= z != z;
+        best = fmaxf(best, z);
+    });
+    return block_max(s, best, bad);
+}
+
+// Adds [lo, hi) to the histogram; returns this thread's mass of what min-p
+// keeps (min_p > 0).
+template <int TH, typename T>
+__device__ inline u64 slice_histogram(Shared<TH> &s, const T *row, int lo, int hi, float top, const Settings &set,
+                                      bool counts) {
+    u64 kept = 0;
+    const bool floors = set.min_p > 0.0f;
+    scan_row<TH>(row, lo, hi, [&](int, float z) {
+        const float t = scaled(z, top, set.c), w = weight(t);
+        const uint32_t m = mass_of(w);
+        if (!m) return;
+        const uint32_t bin = bin_of(t);
+        atomicAdd(&s.mass[bin], static_cast<u64>(m));
+        if (counts) atomicAdd(&s.count[bin], 1u);
+        if (floors && w >= set.min_p) kept += m;
+    });
+    return kept;
+}
+
+// Calls add(key and ~index) for the tokens of [lo, hi) in wanted bins.
+template <int TH, typename T, typename F>
+__device__ inline void slice_collect(const T *row, int lo, int hi, float top, const Settings &set, const Wanted &w,
+                                     F add) {
+    scan_row<TH>(row, lo, hi, [&](int i, float z) {
+        const float t = scaled(z, top, set.c);
+        if (t >= -32.0f && w.has(bin_of(t)) && mass_of(weight(t)))
+            add(static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i));
+    });
+}
+
+// -------------------------------------------------------------- block a row
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(const T *__restrict__ logits, int64_t rows, int vocab,
-                                                          int64_t ldk, const float *__restrict__ uniform,
-                                                          SampleSettings set, int32_t *__restrict__ tokens,
-                                                          float *__restrict__ probs) {
-    __shared__ Shared s;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ __launch_bounds__(1024, 8) void sample_rows_kernel(const T *__restrict__ logits, int64_t rows, int vocab,
+                                                              int64_t ldk, const float *__restrict__ uniform,
+                                                              SampleSettings settings, int32_t *__restrict__ tokens,
+                                                              float *__restrict__ probs) {
+    constexpr int TH = 1024;
+    __shared__ Shared<TH> s;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ldk;
-        float best = -__builtin_inff();
-        int bad = 0;
-        scan_row(row, vocab, [&](int, float z) {
-            bad |= z != z;
-            best = fmaxf(best, z);
-        });
-        for (int o = 32; o; o >>= 1) best = fmaxf(best, __shfl_xor(best, o)), bad |= __shfl_xor(bad, o);
-        if (lane == 0) s.wave_max[wave] = best, s.wave_nan[wave] = bad;
-        __syncthreads();
-        for (int w = 0; w < kThreads / 64; ++w) best = fmaxf(best, s.wave_max[w]), bad |= s.wave_nan[w];
-        __syncthreads();
-        if (bad || best == -__builtin_inff()) {
+        const float top = slice_max(s, row, 0, vocab);
+        if (!(top > -__builtin_inff())) {
             if (threadIdx.x == 0) {
                 tokens[r] = -1;
-                if (probs) probs[r] = bad ? __builtin_nanf("") : 0.0f;
+                if (probs) probs[r] = top != top ? top : 0.0f;
             }
             continue;
         }
-        const float temperature = set.temperature_rows ? set.temperature_rows[r] : set.temperature;
-        float c = 1.0f / temperature;
-        c = c * 1.44269504088896340736f;
-        const bool greedy = !(temperature > 0.0f) || c == __builtin_inff();
-        if (greedy) c = 1.0f;
-        int k = greedy ? 1 : set.top_k_rows ? set.top_k_rows[r] : set.top_k;
-        if (k <= 0 || k > vocab) k = vocab;
-        const float top_p = set.top_p_rows ? set.top_p_rows[r] : set.top_p;
-        float min_p = set.min_p_rows ? set.min_p_rows[r] : set.min_p;
-        if (min_p > 1.0f) min_p = 1.0f;
-
-        // Masses of everything, and of what min-p keeps.
-        unsigned long long all = 0, kept = 0;
-        scan_row(row, vocab, [&](int, float z) {
-            const float w = weight(z, best, c);
-            const unsigned long long m = mass_of(w);
-            all += m;
-            if (!(w < min_p)) kept += m;
+        const Settings set = settings_of(settings, r, vocab);
+        const float u = uniform[r];
+        clear_bins(s);
+        u64 kept = slice_histogram(s, row, 0, vocab, top, set, set.k < vocab), none = 0, t0, t1;
+        __syncthreads();
+        scan_bins(s);
+        const u64 all = s.mass[kBins], counted = set.k < vocab ? s.count[kBins] : 0;
+        if (set.min_p > 0.0f) {
+            scan_threads(s, kept, none, t0, t1);
+            kept = t0;
+        } else {
+            kept = all;
+        }
+        const Wanted w = wanted_bins(s, set, u, kept);
+        if (threadIdx.x == 0) s.listed = 0;
+        __syncthreads();
+        slice_collect<TH>(row, 0, vocab, top, set, w, [&](u64 v) {
+            const uint32_t at = atomicAdd(&s.listed, 1u);
+            if (at < kRoom) s.list[at] = v;
         });
-        all = wave_sum(all), kept = wave_sum(kept);
-        if (lane == 0) s.wave_count[wave] = all, s.wave_mass[wave] = kept;
         __syncthreads();
-        all = kept = 0;
-        for (int w = 0; w < kThreads / 64; ++w) all += s.wave_count[w], kept += s.wave_mass[w];
-        __syncthreads();
-
-        unsigned long long total = all;
-        if (k < vocab) {
-            const Group g = find_group(s, row, vocab, best, c, false, k - 1);
-            total = g.above_mass + (k - g.above_count) * g.mass;
-        }
-        if (top_p < 1.0f) {
-            const double want = ceil(static_cast<double>(top_p) * static_cast<double>(total));
-            const unsigned long long limit = want >= 1.0 ? static_cast<unsigned long long>(want) : 1;
-            if (limit < total) {
-                const Group g = find_group(s, row, vocab, best, c, true, limit - 1);
-                total = g.above_mass + ((limit - 1 - g.above_mass) / g.mass + 1) * g.mass;
-            }
-        }
-        total = min(total, kept);
-        const double at = static_cast<double>(uniform[r]) * static_cast<double>(total);
-        unsigned long long target = at > 0.0 ? static_cast<unsigned long long>(at) : 0;
-        target = min(target, total - 1);
-        const Group g = find_group(s, row, vocab, best, c, true, target);
-        const int index = find_index(s, row, vocab, g.key, static_cast<uint32_t>((target - g.above_mass) / g.mass));
-        if (threadIdx.x == 0) {
-            tokens[r] = index;
-            if (probs) probs[r] = static_cast<float>(g.mass) / static_cast<float>(total);
-        }
+        const uint32_t listed = s.listed;
+        float *prob = probs ? probs + r : nullptr;
+        if (listed <= kRoom)
+            finish(s, set, u, kept, top, listed, tokens + r, prob);
+        else
+            search_row(s, row, vocab, set, u, all, counted, kept, top, tokens + r, prob);
         __syncthreads();
     }
+}
+
+// ------------------------------------------------------- several blocks a row
+
+struct RowSpace {
+    u64 mass[kBins], list[kRoom], kept;
+    uint32_t count[kBins], listed, done;
+    float top[kMostSlices];
+};
+
+constexpr int kSliceThreads = 512;
+
+__device__ inline float row_top(const RowSpace &space, int slices) {
+    float best = space.top[0];
+    for (int i = 1; i < slices; ++i) {
+        const float v = space.top[i];
+        best = v != v || best != best ? __builtin_nanf("") : fmaxf(best, v);
+    }
+    return best;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSliceThreads) void slice_max_kernel(const T *__restrict__ logits, int vocab, int64_t ldk,
+                                                                  int slice, RowSpace *__restrict__ spaces) {
+    __shared__ Shared<kSliceThreads> s;
+    const int64_t r = blockIdx.y;
+    RowSpace &space = spaces[r];
+    const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
+    for (int i = blockIdx.x * kSliceThreads + threadIdx.x; i < kBins; i += gridDim.x * kSliceThreads)
+        space.mass[i] = 0, space.count[i] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) space.kept = 0, space.listed = 0, space.done = 0;
+    const float top = slice_max(s, logits + r * ldk, lo, hi);
+    if (threadIdx.x == 0) space.top[blockIdx.x] = top;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSliceThreads) void slice_histogram_kernel(const T *__restrict__ logits, int vocab,
+                                                                        int64_t ldk, int slice,
+                                                                        SampleSettings settings,
+                                                                        RowSpace *__restrict__ spaces) {
+    constexpr int TH = kSliceThreads;
+    __shared__ Shared<TH> s;
+    const int64_t r = blockIdx.y;
+    RowSpace &space = spaces[r];
+    const float top = row_top(space, gridDim.x);
+    if (!(top > -__builtin_inff())) return;
+    const Settings set = settings_of(settings, r, vocab);
+    const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
+    clear_bins(s);
+    u64 kept = slice_histogram(s, logits + r * ldk, lo, hi, top, set, set.k < vocab), none = 0, t0, t1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += TH) {
+        if (s.mass[i]) atomicAdd(&space.mass[i], s.mass[i]);
+        if (s.count[i]) atomicAdd(&space.count[i], s.count[i]);
+    }
+    if (set.min_p > 0.0f) {
+        scan_threads(s, kept, none, t0, t1);
+        if (threadIdx.x == 0 && t0) atomicAdd(&space.kept, t0);
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSliceThreads) void slice_token_kernel(const T *__restrict__ logits, int vocab,
+                                                                    int64_t ldk, int slice,
+                                                                    const float *__restrict__ uniform,
+                                                                    SampleSettings settings,
+                                                                    RowSpace *__restrict__ spaces,
+                                                                    int32_t *__restrict__ tokens,
+                                                                    float *__restrict__ probs) {
+    constexpr int TH = kSliceThreads;
+    __shared__ Shared<TH> s;
+    const int64_t r = blockIdx.y;
+    const T *row = logits + r * ldk;
+    RowSpace &space = spaces[r];
+    const float top = row_top(space, gridDim.x);
+    if (!(top > -__builtin_inff())) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) {
+            tokens[r] = -1;
+            if (probs) probs[r] = top != top ? top : 0.0f;
+        }
+        return;
+    }
+    const Settings set = settings_of(settings, r, vocab);
+    const float u = uniform[r];
+    for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = space.mass[i], s.count[i] = space.count[i];
+    __syncthreads();
+    scan_bins(s);
+    const u64 all = s.mass[kBins], counted = set.k < vocab ? s.count[kBins] : 0;
+    const u64 kept = set.min_p > 0.0f ? space.kept : all;
+    const Wanted w = wanted_bins(s, set, u, kept);
+    const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
+    slice_collect<TH>(row, lo, hi, top, set, w, [&](u64 v) {
+        const uint32_t at = atomicAdd(&space.listed, 1u);
+        if (at < kRoom) space.list[at] = v;
+    });
+    // The last of the row's blocks finds the token: what the others wrote is
+    // seen by it, since each fences before it counts itself.
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) s.last = atomicAdd(&space.done, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!s.last) return;
+    __threadfence();
+    const uint32_t listed = __hip_atomic_load(&space.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    float *prob = probs ? probs + r : nullptr;
+    if (listed <= kRoom) {
+        for (int i = threadIdx.x; i < static_cast<int>(listed); i += TH)
+            s.list[i] = __hip_atomic_load(&space.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        finish(s, set, u, kept, top, listed, tokens + r, prob);
+    } else {
+        search_row(s, row, vocab, set, u, all, counted, kept, top, tokens + r, prob);
+    }
+}
+
+// Blocks per row: about two a compute unit in all, of 2048 tokens at least;
+// 1: a block per row.
+int slices_of(int64_t rows, int32_t vocab) {
+    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / rows, vocab / 2048, kMostSlices})));
+}
+
+template <typename T>
+bool launch(const T *logits, int64_t rows, int32_t vocab, int64_t ldk, const float *uniform,
+            const SampleSettings &settings, int32_t *tokens, float *probs, void *workspace, hipStream_t stream) {
+    const int slices = slices_of(rows, vocab);
+    if (slices == 1) {
+        sample_rows_kernel<<<static_cast<unsigned>(std::min<int64_t>(rows, 512)), 1024, 0, stream>>>(
+            logits, rows, vocab, ldk, uniform, settings, tokens, probs);
+        return hipGetLastError() == hipSuccess;
+    }
+    const int slice = ((vocab + slices - 1) / slices + 7) / 8 * 8;  // whole vectors
+    const dim3 grid((vocab + slice - 1) / slice, static_cast<unsigned>(rows));
+    auto *spaces = static_cast<RowSpace *>(workspace);
+    slice_max_kernel<<<grid, kSliceThreads, 0, stream>>>(logits, vocab, ldk, slice, spaces);
+    slice_histogram_kernel<<<grid, kSliceThreads, 0, stream>>>(logits, vocab, ldk, slice, settings, spaces);
+    slice_token_kernel<<<grid, kSliceThreads, 0, stream>>>(logits, vocab, ldk, slice, uniform, settings, spaces, tokens,
+                                                           probs);
+    return hipGetLastError() == hipSuccess;
 }
 
 }  // namespace
 
+int64_t sample_workspace_bytes(int64_t rows, int32_t vocab) {
+    return rows > 0 && slices_of(rows, vocab) > 1 ? rows * static_cast<int64_t>(sizeof(RowSpace)) : 0;
+}
+
 bool sample_launch(const void *logits, bool bf16, int64_t rows, int32_t vocab, int64_t ldk, const float *uniform,
-                   const SampleSettings &settings, int32_t *tokens, float *probs, hipStream_t stream) {
+                   const SampleSettings &settings, int32_t *tokens, float *probs, void *workspace,
+                   hipStream_t stream) {
     if (rows == 0) return true;
-    const int grid = static_cast<int>(rows < 4096 ? rows : 4096);
-    if (bf16)
-        sample_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const uint16_t *>(logits), rows, vocab, ldk, uniform,
-                                                     settings, tokens, probs);
-    else
-        sample_kernel<<<grid, kThreads, 0, stream>>>(static_cast<const float *>(logits), rows, vocab, ldk, uniform,
-                                                     settings, tokens, probs);
-    return hipGetLastError() == hipSuccess;
+    return bf16 ? launch(static_cast<const uint16_t *>(logits), rows, vocab, ldk, uniform, settings, tokens, probs,
+                         workspace, stream)
+                : launch(static_cast<const float *>(logits), rows, vocab, ldk, uniform, settings, tokens, probs,
+                         workspace, stream);
 }
 
 }  // namespace fgd

@@ -15,9 +15,13 @@ struct SampleSettings {
     int32_t top_k;
 };
 
+// Device workspace of a call.
+int64_t sample_workspace_bytes(int64_t rows, int32_t vocab);
+
 // Samples one token per row of `logits` ([rows][ldk], element-aligned rows
 // of `vocab` logits); probs may be NULL.  False if a launch failed.
 bool sample_launch(const void *logits, bool bf16, int64_t rows, int32_t vocab, int64_t ldk, const float *uniform,
-                   const SampleSettings &settings, int32_t *tokens, float *probs, hipStream_t stream);
+                   const SampleSettings &settings, int32_t *tokens, float *probs, void *workspace,
+                   hipStream_t stream);
 
 }  // namespace fgd

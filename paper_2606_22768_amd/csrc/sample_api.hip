@@ -39,7 +39,7 @@ fgd_status fgd_sample_workspace_size(int32_t dtype, int64_t num_rows, int64_t vo
     fgd::api_clear();
     if (!bytes) return api_fail(FGD_ERR_INVALID_ARG, "NULL bytes");
     if (fgd_status st = check_sizes(dtype, num_rows, vocab)) return st;
-    *bytes = 0;
+    *bytes = fgd::sample_workspace_bytes(num_rows, static_cast<int32_t>(vocab));
     return FGD_OK;
 }
 
@@ -84,7 +84,7 @@ fgd_status fgd_sample(const void *logits, int32_t dtype, int64_t num_rows, int64
                                    settings->top_k_rows,       settings->temperature, settings->top_p,
                                    settings->min_p,            settings->top_k};
     if (!fgd::sample_launch(logits, dtype == FGD_BF16, num_rows, static_cast<int32_t>(vocab), ldk, uniform, s,
-                            tokens_out, probs_out, static_cast<hipStream_t>(stream)))
+                            tokens_out, probs_out, workspace, static_cast<hipStream_t>(stream)))
         return api_fail(FGD_ERR_HIP, "sampling launch failed");
     return FGD_OK;
 }
