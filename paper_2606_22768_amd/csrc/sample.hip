@@ -548,13 +548,14 @@ struct RowSpace {
 
 constexpr int kSliceThreads = 512;
 
+// The row's largest logit, NaN if one is; every wave by itself.
 __device__ inline float row_top(const RowSpace &space, int slices) {
-    float best = space.top[0];
-    for (int i = 1; i < slices; ++i) {
-        const float v = space.top[i];
-        best = v != v || best != best ? __builtin_nanf("") : fmaxf(best, v);
-    }
-    return best;
+    static_assert(kMostSlices <= 64, "a lane each");
+    const int lane = threadIdx.x & 63;
+    float best = lane < slices ? space.top[lane] : -__builtin_inff();
+    const bool bad = __any(best != best);
+    for (int o = 32; o; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
+    return bad ? __builtin_nanf("") : best;
 }
 
 template <typename T>
@@ -580,9 +581,9 @@ __global__ __launch_bounds__(kSliceThreads) void slice_histogram_kernel(const T 
     __shared__ Shared<TH> s;
     const int64_t r = blockIdx.y;
     RowSpace &space = spaces[r];
+    const Settings set = settings_of(settings, r, vocab);
     const float top = row_top(space, gridDim.x);
     if (!(top > -__builtin_inff())) return;
-    const Settings set = settings_of(settings, r, vocab);
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
     clear_bins(s);
     u64 kept = slice_histogram(s, logits + r * ldk, lo, hi, top, set, set.k < vocab), none = 0, t0, t1;
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(kSliceThreads) void slice_histogram_kernel(const T 
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSliceThreads) void slice_token_kernel(const T *__restrict__ logits, int vocab,
+__global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *__restrict__ logits, int vocab,
                                                                     int64_t ldk, int slice,
                                                                     const float *__restrict__ uniform,
                                                                     SampleSettings settings,
@@ -610,6 +611,10 @@ __global__ __launch_bounds__(kSliceThreads) void slice_token_kernel(const T *__r
     const int64_t r = blockIdx.y;
     const T *row = logits + r * ldk;
     RowSpace &space = spaces[r];
+    const Settings set = settings_of(settings, r, vocab);
+    const float u = uniform[r];
+    const u64 floored = space.kept;
+    for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = space.mass[i], s.count[i] = space.count[i];
     const float top = row_top(space, gridDim.x);
     if (!(top > -__builtin_inff())) {
         if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -618,27 +623,26 @@ __global__ __launch_bounds__(kSliceThreads) void slice_token_kernel(const T *__r
         }
         return;
     }
-    const Settings set = settings_of(settings, r, vocab);
-    const float u = uniform[r];
-    for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = space.mass[i], s.count[i] = space.count[i];
     __syncthreads();
     scan_bins(s);
     const u64 all = s.mass[kBins], counted = set.k < vocab ? s.count[kBins] : 0;
-    const u64 kept = set.min_p > 0.0f ? space.kept : all;
+    const u64 kept = set.min_p > 0.0f ? floored : all;
     const Wanted w = wanted_bins(s, set, u, kept);
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
     slice_collect<TH>(row, lo, hi, top, set, w, [&](u64 v) {
         const uint32_t at = atomicAdd(&space.listed, 1u);
-        if (at < kRoom) space.list[at] = v;
+        if (at < kRoom) __hip_atomic_store(&space.list[at], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     });
-    // The last of the row's blocks finds the token: what the others wrote is
-    // seen by it, since each fences before it counts itself.
-    __threadfence();
+    // The last of the row's blocks finds the token.  The tokens are stored
+    // and read at the device's scope, past the dies' own L2s, and a wave
+    // counts its block only when its stores are acknowledged; a fence would
+    // write back and invalidate whole L2s (25 us of a 64-row call).
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);  // vmcnt(0)
     __syncthreads();
     if (threadIdx.x == 0) s.last = atomicAdd(&space.done, 1u) == gridDim.x - 1;
     __syncthreads();
     if (!s.last) return;
-    __threadfence();
     const uint32_t listed = __hip_atomic_load(&space.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     float *prob = probs ? probs + r : nullptr;
     if (listed <= kRoom) {
