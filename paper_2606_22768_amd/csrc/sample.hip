@@ -55,12 +55,14 @@ __device__ inline float logit_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-// log2 of a token's weight; the largest logit's is 0, an infinite one's too.
-// NaN (an infinite difference times c = 0) stands for no weight.
+// log2 of a token's weight; the largest logit's is 0.  NaN (an infinite
+// difference times c = 0) stands for no weight.
 __device__ inline float scaled(float z, float top, float c) {
 #pragma clang fp contract(off)
-    return z == top ? 0.0f : (z - top) * c;
+    return (z - top) * c;
 }
+// The same where the largest logit may be infinite.
+__device__ inline float scaled_any(float z, float top, float c) { return z == top ? 0.0f : scaled(z, top, c); }
 __device__ inline float weight(float t) { return __builtin_amdgcn_exp2f(fmaxf(t, -126.0f)); }
 __device__ inline uint32_t mass_of(float w) { return static_cast<uint32_t>(fmaf(w, 0x1p31f, 0.5f)); }
 // The bin of a token that has mass (t >= -32).
@@ -104,6 +106,11 @@ __device__ inline void scan_row(const T *row, int lo, int hi, F f) {
         f(tail + rest - head, value(row[tail + rest - head]));
 }
 
+// A value that is the same in a wave, in a scalar register.
+__device__ inline float uniform_value(float v) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
 // A row's settings, made definite.
 struct Settings {
     float c, top_p, min_p;
@@ -122,6 +129,8 @@ __device__ inline Settings settings_of(const SampleSettings &set, int64_t r, int
     s.top_p = set.top_p_rows ? set.top_p_rows[r] : set.top_p;
     s.min_p = set.min_p_rows ? set.min_p_rows[r] : set.min_p;
     if (s.min_p > 1.0f) s.min_p = 1.0f;
+    s.c = uniform_value(s.c), s.top_p = uniform_value(s.top_p), s.min_p = uniform_value(s.min_p);
+    s.k = __builtin_amdgcn_readfirstlane(s.k);
     return s;
 }
 
@@ -161,7 +170,7 @@ __device__ inline float block_max(Shared<TH> &s, float best, bool bad) {
         best = v != v || best != best ? __builtin_nanf("") : fmaxf(best, v);
     }
     __syncthreads();
-    return best;
+    return uniform_value(best);
 }
 
 // Sums of a and b over the threads before this one; the totals in ta, tb.
@@ -225,11 +234,17 @@ __device__ inline void bins_at(Shared<TH> &s, u64 x0, u64 x1, uint32_t &b0, uint
     __syncthreads();
 }
 
-// The bins that a row's search needs: three ranges, from .. from + span.
+// The bins that a row's search needs, as three ranges lo < t <= hi.
 struct Wanted {
-    uint32_t from[3], span[3];
-    __device__ bool has(uint32_t bin) const {
-        return bin - from[0] <= span[0] || bin - from[1] <= span[1] || bin - from[2] <= span[2];
+    float lo[3], hi[3];
+    __device__ void set(int i, uint32_t first, uint32_t last) {
+        hi[i] = uniform_value(static_cast<float>(first) * (-1.0f / kPerOctave));
+        // The last bin ends with the smallest mass, at t = -32.
+        lo[i] = last == kBins - 1 ? -32.000004f
+                                  : uniform_value(static_cast<float>(last + 1) * (-1.0f / kPerOctave));
+    }
+    __device__ bool has(float t) const {
+        return (t > lo[0] && t <= hi[0]) || (t > lo[1] && t <= hi[1]) || (t > lo[2] && t <= hi[2]);
     }
 };
 
@@ -241,7 +256,7 @@ template <int TH>
 __device__ inline Wanted wanted_bins(Shared<TH> &s, const Settings &set, float u, u64 kept) {
     Wanted w;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) w.from[i] = kBins, w.span[i] = 0;  // none
+    for (int i = 0; i < 3; ++i) w.lo[i] = w.hi[i] = 1.0f;  // none
     u64 lo = s.mass[kBins], hi = lo;
     const uint32_t k = static_cast<uint32_t>(set.k);
     uint32_t b0, b1;
@@ -251,18 +266,18 @@ __device__ inline Wanted wanted_bins(Shared<TH> &s, const Settings &set, float u
         __syncthreads();
         b0 = s.found[0];
         __syncthreads();
-        w.from[0] = b0;
+        w.set(0, b0, b0);
         lo = s.mass[b0], hi = s.mass[b0 + 1];
     }
     if (set.top_p < 1.0f) {
         const u64 p0 = max(nucleus(set.top_p, lo), u64{1}), p1 = nucleus(set.top_p, hi);
         bins_at(s, p0 - 1, p1 - 1, b0, b1);
-        w.from[1] = b0, w.span[1] = b1 - b0;
+        w.set(1, b0, b1);
         lo = p0, hi = min(hi, s.mass[b1 + 1]);
     }
     lo = max(min(lo, kept), u64{1}), hi = min(hi, kept);
     bins_at(s, place(u, lo), place(u, hi), b0, b1);
-    w.from[2] = b0, w.span[2] = b1 - b0;
+    w.set(2, b0, b1);
     return w;
 }
 
@@ -382,7 +397,7 @@ __device__ Group find_group(Shared<TH> &s, const T *row, int vocab, float top, f
         scan_row<TH>(row, 0, vocab, [&](int, float z) {
             const uint32_t key = key_of(z);
             if (level && (key >> (shift + bits[level])) != g.key) return;
-            const uint32_t bin = (key >> shift) & mask, m = mass_of(weight(scaled(z, top, c)));
+            const uint32_t bin = (key >> shift) & mask, m = mass_of(weight(scaled_any(z, top, c)));
             if (!m) return;  // no place falls on it
             atomicAdd(&s.count[bin], 1u);
             atomicAdd(&s.mass[bin], static_cast<u64>(m));
@@ -420,12 +435,20 @@ __device__ int find_index(Shared<TH> &s, const T *row, int vocab, uint32_t key, 
     return static_cast<int>(~prefix);
 }
 
-// all, counted: the mass and number of the tokens that have mass.
 template <int TH, typename T>
-__device__ __noinline__ void search_row(Shared<TH> &s, const T *row, int vocab, const Settings &set, float u, u64 all,
-                                        u64 counted, u64 kept, float top, int32_t *token, float *prob) {
-    u64 total = all;
-    if (static_cast<u64>(set.k) < counted) {
+__device__ __noinline__ void search_row(Shared<TH> &s, const T *row, int vocab, Settings set, float u, float top,
+                                        int32_t *token, float *prob) {
+    u64 total = 0, kept = 0, counted = 0, none = 0, t0, t1;
+    scan_row<TH>(row, 0, vocab, [&](int, float z) {
+        const float w = weight(scaled_any(z, top, set.c));
+        const uint32_t m = mass_of(w);
+        total += m, counted += m != 0;
+        if (!(w < set.min_p)) kept += m;
+    });
+    scan_threads(s, total, kept, t0, t1);
+    total = t0, kept = t1;
+    scan_threads(s, counted, none, t0, t1);
+    if (static_cast<u64>(set.k) < t0) {
         const Group g = find_group(s, row, vocab, top, set.c, false, set.k - 1);
         total = g.above_mass + (set.k - g.above_count) * g.mass;
     }
@@ -459,32 +482,36 @@ __device__ inline float slice_max(Shared<TH> &s, const T *row, int lo, int hi) {
 }
 
 // Adds [lo, hi) to the histogram; returns this thread's mass of what min-p
-// keeps (min_p > 0).
-template <int TH, typename T>
-__device__ inline u64 slice_histogram(Shared<TH> &s, const T *row, int lo, int hi, float top, const Settings &set,
-                                      bool counts) {
+// keeps (FLOORS).
+template <int TH, bool COUNTS, bool FLOORS, typename T>
+__device__ inline u64 add_slice(Shared<TH> &s, const T *row, int lo, int hi, float top, float c, float min_p) {
     u64 kept = 0;
-    const bool floors = set.min_p > 0.0f;
     scan_row<TH>(row, lo, hi, [&](int, float z) {
-        const float t = scaled(z, top, set.c), w = weight(t);
+        const float t = scaled(z, top, c), w = weight(t);
         const uint32_t m = mass_of(w);
         if (!m) return;
         const uint32_t bin = bin_of(t);
         atomicAdd(&s.mass[bin], static_cast<u64>(m));
-        if (counts) atomicAdd(&s.count[bin], 1u);
-        if (floors && w >= set.min_p) kept += m;
+        if (COUNTS) atomicAdd(&s.count[bin], 1u);
+        if (FLOORS && w >= min_p) kept += m;
     });
     return kept;
+}
+template <int TH, typename T>
+__device__ inline u64 slice_histogram(Shared<TH> &s, const T *row, int lo, int hi, float top, const Settings &set,
+                                      bool counts) {
+    if (counts)
+        return set.min_p > 0.0f ? add_slice<TH, true, true>(s, row, lo, hi, top, set.c, set.min_p)
+                                : add_slice<TH, true, false>(s, row, lo, hi, top, set.c, set.min_p);
+    return set.min_p > 0.0f ? add_slice<TH, false, true>(s, row, lo, hi, top, set.c, set.min_p)
+                            : add_slice<TH, false, false>(s, row, lo, hi, top, set.c, set.min_p);
 }
 
 // Calls add(key and ~index) for the tokens of [lo, hi) in wanted bins.
 template <int TH, typename T, typename F>
-__device__ inline void slice_collect(const T *row, int lo, int hi, float top, const Settings &set, const Wanted &w,
-                                     F add) {
+__device__ inline void slice_collect(const T *row, int lo, int hi, float top, float c, const Wanted &w, F add) {
     scan_row<TH>(row, lo, hi, [&](int i, float z) {
-        const float t = scaled(z, top, set.c);
-        if (t >= -32.0f && w.has(bin_of(t)) && mass_of(weight(t)))
-            add(static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i));
+        if (w.has(scaled(z, top, c))) add(static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i));
     });
 }
 
@@ -508,32 +535,35 @@ __global__ __launch_bounds__(1024, 8) void sample_rows_kernel(const T *__restric
             continue;
         }
         const Settings set = settings_of(settings, r, vocab);
-        const float u = uniform[r];
+        const float u = uniform_value(uniform[r]);
+        float *prob = probs ? probs + r : nullptr;
+        if (top == __builtin_inff()) {
+            search_row(s, row, vocab, set, u, top, tokens + r, prob);
+            continue;
+        }
         clear_bins(s);
         u64 kept = slice_histogram(s, row, 0, vocab, top, set, set.k < vocab), none = 0, t0, t1;
         __syncthreads();
         scan_bins(s);
-        const u64 all = s.mass[kBins], counted = set.k < vocab ? s.count[kBins] : 0;
         if (set.min_p > 0.0f) {
             scan_threads(s, kept, none, t0, t1);
             kept = t0;
         } else {
-            kept = all;
+            kept = s.mass[kBins];
         }
         const Wanted w = wanted_bins(s, set, u, kept);
         if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
-        slice_collect<TH>(row, 0, vocab, top, set, w, [&](u64 v) {
+        slice_collect<TH>(row, 0, vocab, top, set.c, w, [&](u64 v) {
             const uint32_t at = atomicAdd(&s.listed, 1u);
             if (at < kRoom) s.list[at] = v;
         });
         __syncthreads();
         const uint32_t listed = s.listed;
-        float *prob = probs ? probs + r : nullptr;
         if (listed <= kRoom)
             finish(s, set, u, kept, top, listed, tokens + r, prob);
         else
-            search_row(s, row, vocab, set, u, all, counted, kept, top, tokens + r, prob);
+            search_row(s, row, vocab, set, u, top, tokens + r, prob);
         __syncthreads();
     }
 }
@@ -555,7 +585,7 @@ __device__ inline float row_top(const RowSpace &space, int slices) {
     float best = lane < slices ? space.top[lane] : -__builtin_inff();
     const bool bad = __any(best != best);
     for (int o = 32; o; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
-    return bad ? __builtin_nanf("") : best;
+    return uniform_value(bad ? __builtin_nanf("") : best);
 }
 
 template <typename T>
@@ -583,7 +613,7 @@ __global__ __launch_bounds__(kSliceThreads) void slice_histogram_kernel(const T 
     RowSpace &space = spaces[r];
     const Settings set = settings_of(settings, r, vocab);
     const float top = row_top(space, gridDim.x);
-    if (!(top > -__builtin_inff())) return;
+    if (!(top > -__builtin_inff() && top < __builtin_inff())) return;
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
     clear_bins(s);
     u64 kept = slice_histogram(s, logits + r * ldk, lo, hi, top, set, set.k < vocab), none = 0, t0, t1;
@@ -612,7 +642,8 @@ __global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *
     const T *row = logits + r * ldk;
     RowSpace &space = spaces[r];
     const Settings set = settings_of(settings, r, vocab);
-    const float u = uniform[r];
+    const float u = uniform_value(uniform[r]);
+    float *prob = probs ? probs + r : nullptr;
     const u64 floored = space.kept;
     for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = space.mass[i], s.count[i] = space.count[i];
     const float top = row_top(space, gridDim.x);
@@ -623,13 +654,16 @@ __global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *
         }
         return;
     }
+    if (top == __builtin_inff()) {
+        if (blockIdx.x == 0) search_row(s, row, vocab, set, u, top, tokens + r, prob);
+        return;
+    }
     __syncthreads();
     scan_bins(s);
-    const u64 all = s.mass[kBins], counted = set.k < vocab ? s.count[kBins] : 0;
-    const u64 kept = set.min_p > 0.0f ? floored : all;
+    const u64 kept = set.min_p > 0.0f ? floored : s.mass[kBins];
     const Wanted w = wanted_bins(s, set, u, kept);
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
-    slice_collect<TH>(row, lo, hi, top, set, w, [&](u64 v) {
+    slice_collect<TH>(row, lo, hi, top, set.c, w, [&](u64 v) {
         const uint32_t at = atomicAdd(&space.listed, 1u);
         if (at < kRoom) __hip_atomic_store(&space.list[at], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     });
@@ -644,14 +678,13 @@ __global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *
     __syncthreads();
     if (!s.last) return;
     const uint32_t listed = __hip_atomic_load(&space.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    float *prob = probs ? probs + r : nullptr;
     if (listed <= kRoom) {
         for (int i = threadIdx.x; i < static_cast<int>(listed); i += TH)
             s.list[i] = __hip_atomic_load(&space.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         finish(s, set, u, kept, top, listed, tokens + r, prob);
     } else {
-        search_row(s, row, vocab, set, u, all, counted, kept, top, tokens + r, prob);
+        search_row(s, row, vocab, set, u, top, tokens + r, prob);
     }
 }
 
