@@ -41,6 +41,7 @@ typedef unsigned long long u64;
 constexpr int kBins = 2048, kBinBits = 11;
 constexpr int kRoom = 4096;          // tokens that a row's search can collect
 constexpr int kMostSlices = 64;      // of a row
+constexpr int kThreads = 512;
 constexpr float kPerOctave = 64.0f;  // bins per factor of two of weight
 
 __device__ inline float value(float v) { return v; }
@@ -63,12 +64,15 @@ __device__ inline float scaled(float z, float top, float c) {
 }
 // The same where the largest logit may be infinite.
 __device__ inline float scaled_any(float z, float top, float c) { return z == top ? 0.0f : scaled(z, top, c); }
-__device__ inline float weight(float t) { return __builtin_amdgcn_exp2f(fmaxf(t, -126.0f)); }
+// 2^t; where the instruction flushes its result (t < -126) there is no mass.
+__device__ inline float weight(float t) { return __builtin_amdgcn_exp2f(t); }
 __device__ inline uint32_t mass_of(float w) { return static_cast<uint32_t>(fmaf(w, 0x1p31f, 0.5f)); }
 // The bin of a token that has mass (t >= -32).
 __device__ inline uint32_t bin_of(float t) {
     return min(static_cast<uint32_t>(-kPerOctave * t), static_cast<uint32_t>(kBins - 1));
 }
+// The same of any; kBins where there is no mass.
+__device__ inline int bin_of_any(float t) { return t >= -32.0f ? static_cast<int>(bin_of(t)) : kBins; }
 
 // f(index, logit) for the elements [lo, hi) of a row, by a block of TH threads.
 template <int TH, typename T, typename F>
@@ -146,6 +150,14 @@ __device__ inline u64 place(float u, u64 total) {
     return min(at > 0.0 ? static_cast<u64>(at) : u64{0}, total - 1);
 }
 
+// The tokens a row's search needs: three ranges of logits.
+struct Wanted {
+    float lo[3], hi[3];
+    __device__ bool has(float z) const {
+        return (z >= lo[0] && z <= hi[0]) || (z >= lo[1] && z <= hi[1]) || (z >= lo[2] && z <= hi[2]);
+    }
+};
+
 template <int TH>
 struct Shared {
     u64 mass[kBins + 1];        // a histogram, then the sums before each bin; the total
@@ -153,8 +165,9 @@ struct Shared {
     u64 list[kRoom];            // key, then ~index: the larger is the earlier in the order
     u64 wave_a[TH / 64], wave_b[TH / 64];
     u64 found_mass, found_count, total;
-    uint32_t found[2], listed, last;
+    uint32_t found, listed, last;
     float wave_max[TH / 64];
+    Wanted wanted;
 };
 
 // The largest value of the block's, NaN if one is.
@@ -173,23 +186,37 @@ __device__ inline float block_max(Shared<TH> &s, float best, bool bad) {
     return uniform_value(best);
 }
 
+// Sums over the lanes up to this one.
+template <int CTRL, int ROWS>
+__device__ inline u64 moved(u64 v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0u, static_cast<uint32_t>(v), CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0u, static_cast<uint32_t>(v >> 32), CTRL, ROWS, 0xf, false);
+    return static_cast<u64>(hi) << 32 | lo;
+}
+__device__ inline u64 wave_scan(u64 v) {
+    v += moved<0x111, 0xf>(v);  // from 1, 2, 4 and 8 lanes before, in rows of 16
+    v += moved<0x112, 0xf>(v);
+    v += moved<0x114, 0xf>(v);
+    v += moved<0x118, 0xf>(v);
+    v += moved<0x142, 0xa>(v);  // a row's last lane to the next row
+    v += moved<0x143, 0xc>(v);  // lane 31 to the upper half
+    return v;
+}
+
 // Sums of a and b over the threads before this one; the totals in ta, tb.
 template <int TH>
 __device__ inline void scan_threads(Shared<TH> &s, u64 &a, u64 &b, u64 &ta, u64 &tb) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 ia = a, ib = b;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 ua = __shfl_up(ia, o), ub = __shfl_up(ib, o);
-        if (lane >= o) ia += ua, ib += ub;
-    }
-    if (lane == 63) s.wave_a[wave] = ia, s.wave_b[wave] = ib;
+    const int wave = threadIdx.x >> 6;
+    const u64 ia = wave_scan(a), ib = wave_scan(b);
+    if ((threadIdx.x & 63) == 63) s.wave_a[wave] = ia, s.wave_b[wave] = ib;
     __syncthreads();
     a = ia - a, b = ib - b;
     ta = tb = 0;
+#pragma unroll
     for (int w = 0; w < TH / 64; ++w) {
-        if (w == wave) a += ta, b += tb;
-        ta += s.wave_a[w], tb += s.wave_b[w];
+        const u64 x = s.wave_a[w], y = s.wave_b[w];
+        a += w < wave ? x : 0, b += w < wave ? y : 0;
+        ta += x, tb += y;
     }
     __syncthreads();
 }
@@ -200,17 +227,14 @@ __device__ inline void clear_bins(Shared<TH> &s) {
     __syncthreads();
 }
 
-// Turns the histogram into the sums before each bin.
+// The sums before each bin, of a histogram whose bins thread i holds kOwn
+// of, from kOwn i.
 template <int TH>
-__device__ inline void scan_bins(Shared<TH> &s) {
+__device__ inline void scan_bins(Shared<TH> &s, const u64 (&m)[kBins / TH], const uint32_t (&c)[kBins / TH]) {
     constexpr int kOwn = kBins / TH;
-    u64 m[kOwn], a = 0, b = 0, ta, tb;
-    uint32_t c[kOwn];
+    u64 a = 0, b = 0, ta, tb;
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        m[i] = s.mass[threadIdx.x * kOwn + i], c[i] = s.count[threadIdx.x * kOwn + i];
-        a += m[i], b += c[i];
-    }
+    for (int i = 0; i < kOwn; ++i) a += m[i], b += c[i];
     scan_threads(s, a, b, ta, tb);
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
@@ -221,64 +245,67 @@ __device__ inline void scan_bins(Shared<TH> &s) {
     __syncthreads();
 }
 
-// The bins that hold the places x0 and x1 of mass (below the total).
-template <int TH>
-__device__ inline void bins_at(Shared<TH> &s, u64 x0, u64 x1, uint32_t &b0, uint32_t &b1) {
-    for (int bin = threadIdx.x; bin < kBins; bin += TH) {
-        const u64 lo = s.mass[bin], hi = s.mass[bin + 1];
-        if (lo <= x0 && x0 < hi) s.found[0] = bin;
-        if (lo <= x1 && x1 < hi) s.found[1] = bin;
-    }
-    __syncthreads();
-    b0 = s.found[0], b1 = s.found[1];
-    __syncthreads();
+// The bin that holds the place x (below the total); by a wave.
+template <typename U>
+__device__ inline int bin_at(const U *before, U x) {
+    static_assert(kBins == 64 * 32, "two steps");
+    const int lane = threadIdx.x & 63;
+    const int part = __ffsll(static_cast<u64>(__ballot(before[32 * lane] <= x && x < before[32 * lane + 32]))) - 1;
+    const int bin = 32 * part + (lane & 31);
+    return 32 * part + ((__ffsll(static_cast<u64>(__ballot(before[bin] <= x && x < before[bin + 1]))) - 1) & 31);
 }
 
-// The bins that a row's search needs, as three ranges lo < t <= hi.
-struct Wanted {
-    float lo[3], hi[3];
-    __device__ void set(int i, uint32_t first, uint32_t last) {
-        hi[i] = uniform_value(static_cast<float>(first) * (-1.0f / kPerOctave));
-        // The last bin ends with the smallest mass, at t = -32.
-        lo[i] = last == kBins - 1 ? -32.000004f
-                                  : uniform_value(static_cast<float>(last + 1) * (-1.0f / kPerOctave));
+// The smallest key whose bin is `bin` or an earlier one; each lane its own.
+// pred(key) is monotone, false at -infinity and true at the largest logit.
+__device__ inline uint32_t first_key(int bin, float top, float c) {
+    uint32_t lo = key_of(-__builtin_inff()), hi = key_of(top);
+    auto pred = [&](uint32_t key) { return bin_of_any(scaled(logit_of(key), top, c)) <= bin; };
+    if (bin < 0) return hi + 1;
+    // Where the inverse puts it, give or take its rounding.
+    const float guess = top - static_cast<float>(bin + 1) / (kPerOctave * c);
+    if (guess == guess && guess > -__builtin_inff()) {
+        const uint32_t g = key_of(guess), a = g - 64, b = g + 64;
+        if (a > lo && a < hi) (pred(a) ? hi : lo) = a;
+        if (b > lo && b < hi) (pred(b) ? hi : lo) = b;
     }
-    __device__ bool has(float t) const {
-        return (t > lo[0] && t <= hi[0]) || (t > lo[1] && t <= hi[1]) || (t > lo[2] && t <= hi[2]);
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        (pred(mid) ? hi : lo) = mid;
     }
-};
+    return hi;
+}
 
-// From the summed histogram.  A step's total, with which the next one works,
-// is known to a range lo..hi: of top-k's cut its bin is wanted, of top-p's
-// and the draw's the bins from one end's to the other's.  kept: the mass
-// that min-p keeps.
+// What to collect, from the summed histogram; by the block's first wave.  A
+// step's total, with which the next one works, is known to a range lo..hi:
+// of top-k's cut its bin is wanted, of top-p's and the draw's the bins from
+// one end's to the other's.  kept: the mass that min-p keeps.
 template <int TH>
-__device__ inline Wanted wanted_bins(Shared<TH> &s, const Settings &set, float u, u64 kept) {
-    Wanted w;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) w.lo[i] = w.hi[i] = 1.0f;  // none
+__device__ inline void find_wanted(Shared<TH> &s, const Settings &set, float u, u64 kept, float top) {
+    if (threadIdx.x >= 64) return;
+    int first[3] = {0, 0, 0}, last[3] = {-1, -1, -1};  // none
     u64 lo = s.mass[kBins], hi = lo;
     const uint32_t k = static_cast<uint32_t>(set.k);
-    uint32_t b0, b1;
     if (k < s.count[kBins]) {
-        for (int bin = threadIdx.x; bin < kBins; bin += TH)
-            if (s.count[bin] < k && k <= s.count[bin + 1]) s.found[0] = bin;
-        __syncthreads();
-        b0 = s.found[0];
-        __syncthreads();
-        w.set(0, b0, b0);
-        lo = s.mass[b0], hi = s.mass[b0 + 1];
+        first[0] = last[0] = bin_at<uint32_t>(s.count, k - 1);
+        lo = s.mass[first[0]], hi = s.mass[first[0] + 1];
     }
     if (set.top_p < 1.0f) {
         const u64 p0 = max(nucleus(set.top_p, lo), u64{1}), p1 = nucleus(set.top_p, hi);
-        bins_at(s, p0 - 1, p1 - 1, b0, b1);
-        w.set(1, b0, b1);
-        lo = p0, hi = min(hi, s.mass[b1 + 1]);
+        first[1] = bin_at<u64>(s.mass, p0 - 1), last[1] = bin_at<u64>(s.mass, p1 - 1);
+        lo = p0, hi = min(hi, s.mass[last[1] + 1]);
     }
     lo = max(min(lo, kept), u64{1}), hi = min(hi, kept);
-    bins_at(s, place(u, lo), place(u, hi), b0, b1);
-    w.set(2, b0, b1);
-    return w;
+    first[2] = bin_at<u64>(s.mass, place(u, lo)), last[2] = bin_at<u64>(s.mass, place(u, hi));
+    const int lane = threadIdx.x, i = lane >> 1;
+    if (lane < 6) {
+        const int from = i == 0 ? first[0] : i == 1 ? first[1] : first[2],
+                  to = i == 0 ? last[0] : i == 1 ? last[1] : last[2];
+        const uint32_t key = first_key(lane & 1 ? from - 1 : to, top, set.c);
+        if (lane & 1)
+            s.wanted.hi[i] = to < from ? -1.0f : logit_of(key - 1);
+        else
+            s.wanted.lo[i] = to < from ? 1.0f : logit_of(key);
+    }
 }
 
 // Sorts list[0, n), n a power of two, from the largest.
@@ -295,10 +322,52 @@ __device__ inline void sort_list(u64 *list, int n) {
         }
 }
 
-// Finds the token among those collected, which are all of the wanted bins'.
+// Finds the token among those collected, which are all of the wanted bins':
+// at most 64 of them, by a wave, each token against each.
+template <int TH>
+__device__ inline void finish_few(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
+                                  int32_t *token, float *prob) {
+    const int lane = threadIdx.x;
+    const u64 own = lane < listed ? s.list[lane] : 0;
+    const float t = scaled(logit_of(static_cast<uint32_t>(own >> 32)), top, set.c);
+    const uint32_t m = lane < listed ? mass_of(weight(t)) : 0, bin = lane < listed ? bin_of(t) : kBins;
+    u64 before = s.mass[bin];
+    uint32_t rank = s.count[bin];
+    for (int j = 0; j < listed; ++j) {
+        const u64 other = static_cast<u64>(__builtin_amdgcn_readlane(static_cast<uint32_t>(own >> 32), j)) << 32 |
+                          static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(own), j));
+        const bool ahead = static_cast<uint32_t>(__builtin_amdgcn_readlane(bin, j)) == bin && other > own;
+        before += ahead ? static_cast<uint32_t>(__builtin_amdgcn_readlane(m, j)) : 0u;
+        rank += ahead;
+    }
+    auto through_of = [&](bool here) {  // the sum up to and with the one token where `here` holds
+        const int at = __ffsll(static_cast<u64>(__ballot(here))) - 1;
+        const u64 v = before + m;
+        return static_cast<u64>(__builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), at)) << 32 |
+               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(v), at));
+    };
+    const bool some = lane < listed;
+    u64 total = s.mass[kBins];
+    if (static_cast<uint32_t>(set.k) < s.count[kBins])
+        total = through_of(some && rank == static_cast<uint32_t>(set.k) - 1);
+    const u64 limit = nucleus(set.top_p, total);
+    if (limit < total) total = through_of(some && before < limit && limit <= before + m);
+    total = min(total, kept);
+    const u64 target = place(u, total);
+    if (some && before <= target && target < before + m) {
+        *token = static_cast<int32_t>(~static_cast<uint32_t>(own));
+        if (prob) *prob = static_cast<float>(m) / static_cast<float>(total);
+    }
+}
+
+// The same, of any number, sorted by the block.
 template <int TH>
 __device__ inline void finish(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
                               int32_t *token, float *prob) {
+    if (listed <= 64) {
+        if (threadIdx.x < 64) finish_few(s, set, u, kept, top, listed, token, prob);
+        return;
+    }
     int n = 1;
     while (n < listed) n <<= 1;
     for (int i = listed + threadIdx.x; i < n; i += TH) s.list[i] = 0;
@@ -380,7 +449,7 @@ __device__ inline void find_bin(Shared<TH> &s, bool by_mass, u64 target) {
     for (int i = 0; i < kOwn; ++i) {
         const int bin = kBins - 1 - (threadIdx.x * kOwn + i);
         const u64 before = by_mass ? b : a, own = by_mass ? s.mass[bin] : s.count[bin];
-        if (before <= target && target < before + own) s.found[0] = bin, s.found_count = a, s.found_mass = b;
+        if (before <= target && target < before + own) s.found = bin, s.found_count = a, s.found_mass = b;
         a += s.count[bin], b += s.mass[bin];
     }
     __syncthreads();
@@ -404,7 +473,7 @@ __device__ Group find_group(Shared<TH> &s, const T *row, int vocab, float top, f
         });
         __syncthreads();
         find_bin(s, by_mass, target);
-        const uint32_t bin = s.found[0];
+        const uint32_t bin = s.found;
         target -= by_mass ? s.found_mass : s.found_count;
         g.above_count += s.found_count;
         g.above_mass += s.found_mass;
@@ -429,7 +498,7 @@ __device__ int find_index(Shared<TH> &s, const T *row, int vocab, uint32_t key, 
         __syncthreads();
         find_bin(s, false, n);
         n -= s.found_count;
-        prefix = prefix << kBinBits | s.found[0];
+        prefix = prefix << kBinBits | s.found;
         __syncthreads();
     }
     return static_cast<int>(~prefix);
@@ -507,22 +576,25 @@ __device__ inline u64 slice_histogram(Shared<TH> &s, const T *row, int lo, int h
                             : add_slice<TH, false, false>(s, row, lo, hi, top, set.c, set.min_p);
 }
 
-// Calls add(key and ~index) for the tokens of [lo, hi) in wanted bins.
+// Calls add(key and ~index) for the wanted tokens of [lo, hi).
 template <int TH, typename T, typename F>
-__device__ inline void slice_collect(const T *row, int lo, int hi, float top, float c, const Wanted &w, F add) {
+__device__ inline void slice_collect(const T *row, int lo, int hi, const Wanted &wanted, F add) {
+    Wanted w;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w.lo[i] = uniform_value(wanted.lo[i]), w.hi[i] = uniform_value(wanted.hi[i]);
     scan_row<TH>(row, lo, hi, [&](int i, float z) {
-        if (w.has(scaled(z, top, c))) add(static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i));
+        if (w.has(z)) add(static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i));
     });
 }
 
 // -------------------------------------------------------------- block a row
 
 template <typename T>
-__global__ __launch_bounds__(1024, 8) void sample_rows_kernel(const T *__restrict__ logits, int64_t rows, int vocab,
+__global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(const T *__restrict__ logits, int64_t rows, int vocab,
                                                               int64_t ldk, const float *__restrict__ uniform,
                                                               SampleSettings settings, int32_t *__restrict__ tokens,
                                                               float *__restrict__ probs) {
-    constexpr int TH = 1024;
+    constexpr int TH = kThreads;
     __shared__ Shared<TH> s;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ldk;
@@ -544,17 +616,22 @@ __global__ __launch_bounds__(1024, 8) void sample_rows_kernel(const T *__restric
         clear_bins(s);
         u64 kept = slice_histogram(s, row, 0, vocab, top, set, set.k < vocab), none = 0, t0, t1;
         __syncthreads();
-        scan_bins(s);
+        u64 m[kBins / TH];
+        uint32_t c[kBins / TH];
+#pragma unroll
+        for (int i = 0; i < kBins / TH; ++i)
+            m[i] = s.mass[threadIdx.x * (kBins / TH) + i], c[i] = s.count[threadIdx.x * (kBins / TH) + i];
+        scan_bins(s, m, c);
         if (set.min_p > 0.0f) {
             scan_threads(s, kept, none, t0, t1);
             kept = t0;
         } else {
             kept = s.mass[kBins];
         }
-        const Wanted w = wanted_bins(s, set, u, kept);
+        find_wanted(s, set, u, kept, top);
         if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
-        slice_collect<TH>(row, 0, vocab, top, set.c, w, [&](u64 v) {
+        slice_collect<TH>(row, 0, vocab, s.wanted, [&](u64 v) {
             const uint32_t at = atomicAdd(&s.listed, 1u);
             if (at < kRoom) s.list[at] = v;
         });
@@ -576,8 +653,6 @@ struct RowSpace {
     float top[kMostSlices];
 };
 
-constexpr int kSliceThreads = 512;
-
 // The row's largest logit, NaN if one is; every wave by itself.
 __device__ inline float row_top(const RowSpace &space, int slices) {
     static_assert(kMostSlices <= 64, "a lane each");
@@ -589,13 +664,13 @@ __device__ inline float row_top(const RowSpace &space, int slices) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSliceThreads) void slice_max_kernel(const T *__restrict__ logits, int vocab, int64_t ldk,
+__global__ __launch_bounds__(kThreads) void slice_max_kernel(const T *__restrict__ logits, int vocab, int64_t ldk,
                                                                   int slice, RowSpace *__restrict__ spaces) {
-    __shared__ Shared<kSliceThreads> s;
+    __shared__ Shared<kThreads> s;
     const int64_t r = blockIdx.y;
     RowSpace &space = spaces[r];
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
-    for (int i = blockIdx.x * kSliceThreads + threadIdx.x; i < kBins; i += gridDim.x * kSliceThreads)
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < kBins; i += gridDim.x * kThreads)
         space.mass[i] = 0, space.count[i] = 0;
     if (blockIdx.x == 0 && threadIdx.x == 0) space.kept = 0, space.listed = 0, space.done = 0;
     const float top = slice_max(s, logits + r * ldk, lo, hi);
@@ -603,11 +678,11 @@ __global__ __launch_bounds__(kSliceThreads) void slice_max_kernel(const T *__res
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSliceThreads) void slice_histogram_kernel(const T *__restrict__ logits, int vocab,
+__global__ __launch_bounds__(kThreads) void slice_histogram_kernel(const T *__restrict__ logits, int vocab,
                                                                         int64_t ldk, int slice,
                                                                         SampleSettings settings,
                                                                         RowSpace *__restrict__ spaces) {
-    constexpr int TH = kSliceThreads;
+    constexpr int TH = kThreads;
     __shared__ Shared<TH> s;
     const int64_t r = blockIdx.y;
     RowSpace &space = spaces[r];
@@ -629,14 +704,14 @@ __global__ __launch_bounds__(kSliceThreads) void slice_histogram_kernel(const T 
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *__restrict__ logits, int vocab,
+__global__ __launch_bounds__(kThreads, 4) void slice_token_kernel(const T *__restrict__ logits, int vocab,
                                                                     int64_t ldk, int slice,
                                                                     const float *__restrict__ uniform,
                                                                     SampleSettings settings,
                                                                     RowSpace *__restrict__ spaces,
                                                                     int32_t *__restrict__ tokens,
                                                                     float *__restrict__ probs) {
-    constexpr int TH = kSliceThreads;
+    constexpr int TH = kThreads;
     __shared__ Shared<TH> s;
     const int64_t r = blockIdx.y;
     const T *row = logits + r * ldk;
@@ -645,7 +720,11 @@ __global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *
     const float u = uniform_value(uniform[r]);
     float *prob = probs ? probs + r : nullptr;
     const u64 floored = space.kept;
-    for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = space.mass[i], s.count[i] = space.count[i];
+    u64 m[kBins / TH];
+    uint32_t c[kBins / TH];
+#pragma unroll
+    for (int i = 0; i < kBins / TH; ++i)
+        m[i] = space.mass[threadIdx.x * (kBins / TH) + i], c[i] = space.count[threadIdx.x * (kBins / TH) + i];
     const float top = row_top(space, gridDim.x);
     if (!(top > -__builtin_inff())) {
         if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -658,12 +737,12 @@ __global__ __launch_bounds__(kSliceThreads, 4) void slice_token_kernel(const T *
         if (blockIdx.x == 0) search_row(s, row, vocab, set, u, top, tokens + r, prob);
         return;
     }
-    __syncthreads();
-    scan_bins(s);
+    scan_bins(s, m, c);
     const u64 kept = set.min_p > 0.0f ? floored : s.mass[kBins];
-    const Wanted w = wanted_bins(s, set, u, kept);
+    find_wanted(s, set, u, kept, top);
+    __syncthreads();
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
-    slice_collect<TH>(row, lo, hi, top, set.c, w, [&](u64 v) {
+    slice_collect<TH>(row, lo, hi, s.wanted, [&](u64 v) {
         const uint32_t at = atomicAdd(&space.listed, 1u);
         if (at < kRoom) __hip_atomic_store(&space.list[at], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     });
@@ -699,16 +778,16 @@ bool launch(const T *logits, int64_t rows, int32_t vocab, int64_t ldk, const flo
             const SampleSettings &settings, int32_t *tokens, float *probs, void *workspace, hipStream_t stream) {
     const int slices = slices_of(rows, vocab);
     if (slices == 1) {
-        sample_rows_kernel<<<static_cast<unsigned>(std::min<int64_t>(rows, 512)), 1024, 0, stream>>>(
+        sample_rows_kernel<<<static_cast<unsigned>(std::min<int64_t>(rows, 512)), kThreads, 0, stream>>>(
             logits, rows, vocab, ldk, uniform, settings, tokens, probs);
         return hipGetLastError() == hipSuccess;
     }
     const int slice = ((vocab + slices - 1) / slices + 7) / 8 * 8;  // whole vectors
     const dim3 grid((vocab + slice - 1) / slice, static_cast<unsigned>(rows));
     auto *spaces = static_cast<RowSpace *>(workspace);
-    slice_max_kernel<<<grid, kSliceThreads, 0, stream>>>(logits, vocab, ldk, slice, spaces);
-    slice_histogram_kernel<<<grid, kSliceThreads, 0, stream>>>(logits, vocab, ldk, slice, settings, spaces);
-    slice_token_kernel<<<grid, kSliceThreads, 0, stream>>>(logits, vocab, ldk, slice, uniform, settings, spaces, tokens,
+    slice_max_kernel<<<grid, kThreads, 0, stream>>>(logits, vocab, ldk, slice, spaces);
+    slice_histogram_kernel<<<grid, kThreads, 0, stream>>>(logits, vocab, ldk, slice, settings, spaces);
+    slice_token_kernel<<<grid, kThreads, 0, stream>>>(logits, vocab, ldk, slice, uniform, settings, spaces, tokens,
                                                            probs);
     return hipGetLastError() == hipSuccess;
 }
