@@ -26,7 +26,15 @@
 //
 // Many rows: a block per row.  Fewer: a row's slices on several blocks, a
 // kernel for each step, histogram and tokens in the workspace; the block of a
-// row that ends last finds its token.
+// row that ends last finds its token.  Many long bf16 rows: a pass counts the
+// tokens of each 16-bit value, exact places follow from the counts, and a
+// second pass finds the token.
+//
+// Bound by the reads of the logits: three passes over a row (two for counted
+// ones), of which the first comes from memory and the others partly from the
+// caches.  2048 x 128256 f32: 455 us (6.9 TB/s over the three); bf16: 200 us
+// (5.2 TB/s over the two), 321 in three; one pass of copying's rate would be
+// 219 and 109.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -74,25 +82,28 @@ __device__ inline uint32_t bin_of(float t) {
 // The same of any; kBins where there is no mass.
 __device__ inline int bin_of_any(float t) { return t >= -32.0f ? static_cast<int>(bin_of(t)) : kBins; }
 
-// f(index, logit) for the elements [lo, hi) of a row, by a block of TH threads.
+// f(index of the first, logits[n]) for the elements [lo, hi) of a row, some
+// at a time so that their steps interleave, by a block of TH threads.
 template <int TH, typename T, typename F>
 __device__ inline void scan_row(const T *row, int lo, int hi, F f) {
-    constexpr int kPer = 16 / sizeof(T), kAhead = 4;
+    constexpr int kPer = 16 / sizeof(T), kAhead = 2;
     const uintptr_t at = reinterpret_cast<uintptr_t>(row + lo);
     const int head = min(hi - lo, static_cast<int>((16 - (at & 15)) & 15) / static_cast<int>(sizeof(T)));
     const int vectors = (hi - lo - head) / kPer, first = lo + head, tail = first + vectors * kPer;
     const uint4 *v = reinterpret_cast<const uint4 *>(row + first);
     auto each = [&](int i, uint4 u) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        float z[kPer];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if constexpr (sizeof(T) == 4) {
-                f(first + i * 4 + j, __uint_as_float(w[j]));
+                z[j] = __uint_as_float(w[j]);
             } else {
-                f(first + i * 8 + 2 * j, __uint_as_float(w[j] << 16));
-                f(first + i * 8 + 2 * j + 1, __uint_as_float(w[j] & 0xffff0000u));
+                z[2 * j] = __uint_as_float(w[j] << 16);
+                z[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
             }
         }
+        f(first + i * kPer, z);
     };
     int i = threadIdx.x;
     for (; i + (kAhead - 1) * TH < vectors; i += kAhead * TH) {
@@ -104,10 +115,20 @@ __device__ inline void scan_row(const T *row, int lo, int hi, F f) {
     }
     for (; i < vectors; i += TH) each(i, v[i]);
     const int rest = static_cast<int>(threadIdx.x);
-    if (rest < head)
-        f(lo + rest, value(row[lo + rest]));
-    else if (tail + rest - head < hi)
-        f(tail + rest - head, value(row[tail + rest - head]));
+    const int at_end = rest < head ? lo + rest : tail + rest - head;
+    if (at_end < hi) {
+        const float z[1] = {value(row[at_end])};
+        f(at_end, z);
+    }
+}
+
+// f(index, logit), one by one.
+template <int TH, typename T, typename F>
+__device__ inline void scan_row_singly(const T *row, int lo, int hi, F f) {
+    scan_row<TH>(row, lo, hi, [&](int i, const auto &z) {
+#pragma unroll
+        for (int j = 0; j < static_cast<int>(sizeof(z) / sizeof(float)); ++j) f(i + j, z[j]);
+    });
 }
 
 // A value that is the same in a wave, in a scalar register.
@@ -154,25 +175,29 @@ __device__ inline u64 place(float u, u64 total) {
 struct Wanted {
     float lo[3], hi[3];
     __device__ bool has(float z) const {
-        return (z >= lo[0] && z <= hi[0]) || (z >= lo[1] && z <= hi[1]) || (z >= lo[2] && z <= hi[2]);
+        return (z >= lo[0] & z <= hi[0]) | (z >= lo[1] & z <= hi[1]) | (z >= lo[2] & z <= hi[2]);  // no branches
     }
 };
 
 template <int TH>
-struct Shared {
-    u64 mass[kBins + 1];        // a histogram, then the sums before each bin; the total
+struct Bins {
+    u64 mass[kBins + 1];  // a histogram, then the sums before each bin; the total
     uint32_t count[kBins + 1];
-    u64 list[kRoom];            // key, then ~index: the larger is the earlier in the order
-    u64 wave_a[TH / 64], wave_b[TH / 64];
-    u64 found_mass, found_count, total;
-    uint32_t found, listed, last;
+    u64 wave_a[TH / 64], wave_b[TH / 64], found_mass, found_count;
+    uint32_t found;
     float wave_max[TH / 64];
+};
+template <int TH>
+struct Shared : Bins<TH> {
+    u64 list[kRoom];  // key, then ~index: the larger is the earlier in the order
+    u64 total;
+    uint32_t listed, last;
     Wanted wanted;
 };
 
 // The largest value of the block's, NaN if one is.
 template <int TH>
-__device__ inline float block_max(Shared<TH> &s, float best, bool bad) {
+__device__ inline float block_max(Bins<TH> &s, float best, bool bad) {
     for (int o = 32; o; o >>= 1) best = fmaxf(best, __shfl_xor(best, o));
     if (__any(bad)) best = __builtin_nanf("");
     if ((threadIdx.x & 63) == 0) s.wave_max[threadIdx.x >> 6] = best;
@@ -205,16 +230,16 @@ __device__ inline u64 wave_scan(u64 v) {
 
 // Sums of a and b over the threads before this one; the totals in ta, tb.
 template <int TH>
-__device__ inline void scan_threads(Shared<TH> &s, u64 &a, u64 &b, u64 &ta, u64 &tb) {
+__device__ inline void scan_threads(u64 *wave_a, u64 *wave_b, u64 &a, u64 &b, u64 &ta, u64 &tb) {
     const int wave = threadIdx.x >> 6;
     const u64 ia = wave_scan(a), ib = wave_scan(b);
-    if ((threadIdx.x & 63) == 63) s.wave_a[wave] = ia, s.wave_b[wave] = ib;
+    if ((threadIdx.x & 63) == 63) wave_a[wave] = ia, wave_b[wave] = ib;
     __syncthreads();
     a = ia - a, b = ib - b;
     ta = tb = 0;
 #pragma unroll
     for (int w = 0; w < TH / 64; ++w) {
-        const u64 x = s.wave_a[w], y = s.wave_b[w];
+        const u64 x = wave_a[w], y = wave_b[w];
         a += w < wave ? x : 0, b += w < wave ? y : 0;
         ta += x, tb += y;
     }
@@ -222,7 +247,12 @@ __device__ inline void scan_threads(Shared<TH> &s, u64 &a, u64 &b, u64 &ta, u64 
 }
 
 template <int TH>
-__device__ inline void clear_bins(Shared<TH> &s) {
+__device__ inline void scan_threads(Bins<TH> &s, u64 &a, u64 &b, u64 &ta, u64 &tb) {
+    scan_threads<TH>(s.wave_a, s.wave_b, a, b, ta, tb);
+}
+
+template <int TH>
+__device__ inline void clear_bins(Bins<TH> &s) {
     for (int i = threadIdx.x; i < kBins; i += TH) s.mass[i] = 0, s.count[i] = 0;
     __syncthreads();
 }
@@ -230,12 +260,12 @@ __device__ inline void clear_bins(Shared<TH> &s) {
 // The sums before each bin, of a histogram whose bins thread i holds kOwn
 // of, from kOwn i.
 template <int TH>
-__device__ inline void scan_bins(Shared<TH> &s, const u64 (&m)[kBins / TH], const uint32_t (&c)[kBins / TH]) {
+__device__ inline void scan_bins(Bins<TH> &s, const u64 (&m)[kBins / TH], const uint32_t (&c)[kBins / TH]) {
     constexpr int kOwn = kBins / TH;
     u64 a = 0, b = 0, ta, tb;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) a += m[i], b += c[i];
-    scan_threads(s, a, b, ta, tb);
+    scan_threads<TH>(s, a, b, ta, tb);
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
         s.mass[threadIdx.x * kOwn + i] = a, s.count[threadIdx.x * kOwn + i] = static_cast<uint32_t>(b);
@@ -377,7 +407,7 @@ __device__ inline void finish(Shared<TH> &s, const Settings &set, float u, u64 k
     auto t_at = [&](int i) { return scaled(logit_of(static_cast<uint32_t>(s.list[i] >> 32)), top, set.c); };
     u64 sum = 0, none = 0, t0, t1;
     for (int i = base; i < end; ++i) sum += mass_of(weight(t_at(i)));
-    scan_threads(s, sum, none, t0, t1);
+    scan_threads<TH>(s, sum, none, t0, t1);
     // A bin's sums become those to add to a place in the list.
     u64 at = sum;
     for (int i = base; i < end; ++i) {
@@ -438,14 +468,14 @@ struct Group {  // the tokens of one logit in the order
 // The first bin, from the highest, through which the measure exceeds
 // `target`.
 template <int TH>
-__device__ inline void find_bin(Shared<TH> &s, bool by_mass, u64 target) {
+__device__ inline void find_bin(Bins<TH> &s, bool by_mass, u64 target) {
     constexpr int kOwn = kBins / TH;
     u64 a = 0, b = 0, ta, tb;
     for (int i = 0; i < kOwn; ++i) {
         const int bin = kBins - 1 - (threadIdx.x * kOwn + i);
         a += s.count[bin], b += s.mass[bin];
     }
-    scan_threads(s, a, b, ta, tb);
+    scan_threads<TH>(s, a, b, ta, tb);
     for (int i = 0; i < kOwn; ++i) {
         const int bin = kBins - 1 - (threadIdx.x * kOwn + i);
         const u64 before = by_mass ? b : a, own = by_mass ? s.mass[bin] : s.count[bin];
@@ -456,14 +486,14 @@ __device__ inline void find_bin(Shared<TH> &s, bool by_mass, u64 target) {
 }
 
 template <int TH, typename T>
-__device__ Group find_group(Shared<TH> &s, const T *row, int vocab, float top, float c, bool by_mass, u64 target) {
+__device__ Group find_group(Bins<TH> &s, const T *row, int vocab, float top, float c, bool by_mass, u64 target) {
     Group g = {0, 0, 0, 0};
     const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
     for (int level = 0; level < 3; ++level) {
         const int shift = shifts[level];
         const uint32_t mask = (1u << bits[level]) - 1;
-        clear_bins(s);
-        scan_row<TH>(row, 0, vocab, [&](int, float z) {
+        clear_bins<TH>(s);
+        scan_row_singly<TH>(row, 0, vocab, [&](int, float z) {
             const uint32_t key = key_of(z);
             if (level && (key >> (shift + bits[level])) != g.key) return;
             const uint32_t bin = (key >> shift) & mask, m = mass_of(weight(scaled_any(z, top, c)));
@@ -472,7 +502,7 @@ __device__ Group find_group(Shared<TH> &s, const T *row, int vocab, float top, f
             atomicAdd(&s.mass[bin], static_cast<u64>(m));
         });
         __syncthreads();
-        find_bin(s, by_mass, target);
+        find_bin<TH>(s, by_mass, target);
         const uint32_t bin = s.found;
         target -= by_mass ? s.found_mass : s.found_count;
         g.above_count += s.found_count;
@@ -486,17 +516,17 @@ __device__ Group find_group(Shared<TH> &s, const T *row, int vocab, float top, f
 
 // The index of the n-th token of key `key`.
 template <int TH, typename T>
-__device__ int find_index(Shared<TH> &s, const T *row, int vocab, uint32_t key, u64 n) {
+__device__ int find_index(Bins<TH> &s, const T *row, int vocab, uint32_t key, u64 n) {
     uint32_t prefix = 0;
     for (int shift = 22; shift >= 0; shift -= kBinBits) {
-        clear_bins(s);
-        scan_row<TH>(row, 0, vocab, [&](int i, float z) {
+        clear_bins<TH>(s);
+        scan_row_singly<TH>(row, 0, vocab, [&](int i, float z) {
             const uint32_t r = ~static_cast<uint32_t>(i);  // find_bin counts from the highest bin
             if (key_of(z) != key || (shift < 22 && (r >> (shift + kBinBits)) != prefix)) return;
             atomicAdd(&s.count[(r >> shift) & (kBins - 1)], 1u);
         });
         __syncthreads();
-        find_bin(s, false, n);
+        find_bin<TH>(s, false, n);
         n -= s.found_count;
         prefix = prefix << kBinBits | s.found;
         __syncthreads();
@@ -505,31 +535,31 @@ __device__ int find_index(Shared<TH> &s, const T *row, int vocab, uint32_t key, 
 }
 
 template <int TH, typename T>
-__device__ __noinline__ void search_row(Shared<TH> &s, const T *row, int vocab, Settings set, float u, float top,
+__device__ __noinline__ void search_row(Bins<TH> &s, const T *row, int vocab, Settings set, float u, float top,
                                         int32_t *token, float *prob) {
     u64 total = 0, kept = 0, counted = 0, none = 0, t0, t1;
-    scan_row<TH>(row, 0, vocab, [&](int, float z) {
+    scan_row_singly<TH>(row, 0, vocab, [&](int, float z) {
         const float w = weight(scaled_any(z, top, set.c));
         const uint32_t m = mass_of(w);
         total += m, counted += m != 0;
         if (!(w < set.min_p)) kept += m;
     });
-    scan_threads(s, total, kept, t0, t1);
+    scan_threads<TH>(s, total, kept, t0, t1);
     total = t0, kept = t1;
-    scan_threads(s, counted, none, t0, t1);
+    scan_threads<TH>(s, counted, none, t0, t1);
     if (static_cast<u64>(set.k) < t0) {
-        const Group g = find_group(s, row, vocab, top, set.c, false, set.k - 1);
+        const Group g = find_group<TH>(s, row, vocab, top, set.c, false, set.k - 1);
         total = g.above_mass + (set.k - g.above_count) * g.mass;
     }
     const u64 limit = nucleus(set.top_p, total);
     if (limit < total) {
-        const Group g = find_group(s, row, vocab, top, set.c, true, limit - 1);
+        const Group g = find_group<TH>(s, row, vocab, top, set.c, true, limit - 1);
         total = g.above_mass + ((limit - 1 - g.above_mass) / g.mass + 1) * g.mass;
     }
     total = min(total, kept);
     const u64 target = place(u, total);
-    const Group g = find_group(s, row, vocab, top, set.c, true, target);
-    const int index = find_index(s, row, vocab, g.key, (target - g.above_mass) / g.mass);
+    const Group g = find_group<TH>(s, row, vocab, top, set.c, true, target);
+    const int index = find_index<TH>(s, row, vocab, g.key, (target - g.above_mass) / g.mass);
     if (threadIdx.x == 0) {
         *token = index;
         if (prob) *prob = static_cast<float>(g.mass) / static_cast<float>(total);
@@ -540,34 +570,44 @@ __device__ __noinline__ void search_row(Shared<TH> &s, const T *row, int vocab, 
 // ------------------------------------------------------------------ steps
 
 template <int TH, typename T>
-__device__ inline float slice_max(Shared<TH> &s, const T *row, int lo, int hi) {
+__device__ inline float slice_max(Bins<TH> &s, const T *row, int lo, int hi) {
     float best = -__builtin_inff();
     bool bad = false;
-    scan_row<TH>(row, lo, hi, [&](int, float z) {
-        bad |= z != z;
-        best = fmaxf(best, z);
+    scan_row<TH>(row, lo, hi, [&](int, const auto &z) {
+#pragma unroll
+        for (float v : z) {
+            bad |= v != v;
+            best = fmaxf(best, v);
+        }
     });
-    return block_max(s, best, bad);
+    return block_max<TH>(s, best, bad);
 }
 
 // Adds [lo, hi) to the histogram; returns this thread's mass of what min-p
 // keeps (FLOORS).
 template <int TH, bool COUNTS, bool FLOORS, typename T>
-__device__ inline u64 add_slice(Shared<TH> &s, const T *row, int lo, int hi, float top, float c, float min_p) {
+__device__ inline u64 add_slice(Bins<TH> &s, const T *row, int lo, int hi, float top, float c, float min_p) {
     u64 kept = 0;
-    scan_row<TH>(row, lo, hi, [&](int, float z) {
-        const float t = scaled(z, top, c), w = weight(t);
-        const uint32_t m = mass_of(w);
-        if (!m) return;
-        const uint32_t bin = bin_of(t);
-        atomicAdd(&s.mass[bin], static_cast<u64>(m));
-        if (COUNTS) atomicAdd(&s.count[bin], 1u);
-        if (FLOORS && w >= min_p) kept += m;
+    scan_row<TH>(row, lo, hi, [&](int, const auto &z) {
+        constexpr int n = sizeof(z) / sizeof(float);
+        uint32_t m[n], bin[n];
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+            const float t = scaled(z[j], top, c), w = weight(t);
+            m[j] = mass_of(w), bin[j] = bin_of(t);
+            if (FLOORS) kept += w >= min_p ? m[j] : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < n; ++j)
+            if (m[j]) {
+                atomicAdd(&s.mass[bin[j]], static_cast<u64>(m[j]));
+                if (COUNTS) atomicAdd(&s.count[bin[j]], 1u);
+            }
     });
     return kept;
 }
 template <int TH, typename T>
-__device__ inline u64 slice_histogram(Shared<TH> &s, const T *row, int lo, int hi, float top, const Settings &set,
+__device__ inline u64 slice_histogram(Bins<TH> &s, const T *row, int lo, int hi, float top, const Settings &set,
                                       bool counts) {
     if (counts)
         return set.min_p > 0.0f ? add_slice<TH, true, true>(s, row, lo, hi, top, set.c, set.min_p)
@@ -582,8 +622,15 @@ __device__ inline void slice_collect(const T *row, int lo, int hi, const Wanted 
     Wanted w;
 #pragma unroll
     for (int i = 0; i < 3; ++i) w.lo[i] = uniform_value(wanted.lo[i]), w.hi[i] = uniform_value(wanted.hi[i]);
-    scan_row<TH>(row, lo, hi, [&](int i, float z) {
-        if (w.has(z)) add(static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i));
+    scan_row<TH>(row, lo, hi, [&](int i, const auto &z) {
+        constexpr int n = sizeof(z) / sizeof(float);
+        bool some = false;
+#pragma unroll
+        for (int j = 0; j < n; ++j) some |= w.has(z[j]);
+        if (!some) return;
+#pragma unroll
+        for (int j = 0; j < n; ++j)
+            if (w.has(z[j])) add(static_cast<u64>(key_of(z[j])) << 32 | ~static_cast<uint32_t>(i + j));
     });
 }
 
@@ -591,14 +638,15 @@ __device__ inline void slice_collect(const T *row, int lo, int hi, const Wanted 
 
 template <typename T>
 __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(const T *__restrict__ logits, int64_t rows, int vocab,
-                                                              int64_t ldk, const float *__restrict__ uniform,
-                                                              SampleSettings settings, int32_t *__restrict__ tokens,
-                                                              float *__restrict__ probs) {
+                                                                  int64_t ldk, const float *__restrict__ uniform,
+                                                                  SampleSettings settings,
+                                                                  int32_t *__restrict__ tokens,
+                                                                  float *__restrict__ probs) {
     constexpr int TH = kThreads;
     __shared__ Shared<TH> s;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ldk;
-        const float top = slice_max(s, row, 0, vocab);
+        const float top = slice_max<TH>(s, row, 0, vocab);
         if (!(top > -__builtin_inff())) {
             if (threadIdx.x == 0) {
                 tokens[r] = -1;
@@ -610,20 +658,20 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(const T *__res
         const float u = uniform_value(uniform[r]);
         float *prob = probs ? probs + r : nullptr;
         if (top == __builtin_inff()) {
-            search_row(s, row, vocab, set, u, top, tokens + r, prob);
+            search_row<TH>(s, row, vocab, set, u, top, tokens + r, prob);
             continue;
         }
-        clear_bins(s);
-        u64 kept = slice_histogram(s, row, 0, vocab, top, set, set.k < vocab), none = 0, t0, t1;
+        clear_bins<TH>(s);
+        u64 kept = slice_histogram<TH>(s, row, 0, vocab, top, set, set.k < vocab), none = 0, t0, t1;
         __syncthreads();
         u64 m[kBins / TH];
         uint32_t c[kBins / TH];
 #pragma unroll
         for (int i = 0; i < kBins / TH; ++i)
             m[i] = s.mass[threadIdx.x * (kBins / TH) + i], c[i] = s.count[threadIdx.x * (kBins / TH) + i];
-        scan_bins(s, m, c);
+        scan_bins<TH>(s, m, c);
         if (set.min_p > 0.0f) {
-            scan_threads(s, kept, none, t0, t1);
+            scan_threads<TH>(s, kept, none, t0, t1);
             kept = t0;
         } else {
             kept = s.mass[kBins];
@@ -640,7 +688,305 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(const T *__res
         if (listed <= kRoom)
             finish(s, set, u, kept, top, listed, tokens + r, prob);
         else
-            search_row(s, row, vocab, set, u, top, tokens + r, prob);
+            search_row<TH>(s, row, vocab, set, u, top, tokens + r, prob);
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------- bf16: a block a row
+//
+// 16-bit logits need no bins: a pass counts the tokens of every value, in
+// LDS.  The rest follows from the counts, place by place in descending order
+// of the values, and a second pass finds the token among those of the drawn
+// value.  Three blocks a compute unit, so that one row's loads run beside
+// another's sums (the row held in registers, read once, at a block a compute
+// unit: 330 us for the 200 of 2048 x 128256; four blocks of 64 registers, 214).
+
+// A dword counts a magnitude, from 2^-32 to 2^32: the positive value in its
+// lower half, the negative in its upper.  A count that overflows its half
+// shows in the sum of all.  Zeros are counted apart; values of -2^32 and
+// below are taken for masks.
+constexpr int kValues = 64 * 128, kGroups = kValues / 64;
+constexpr uint32_t kSmallest = 95 << 7, kBeyond = kSmallest + kValues, kInfinity = 0x7f80;
+// Places in the order of the values: the positive groups downwards, zero, the
+// negative groups; padded.
+constexpr int kZeroPlace = kGroups, kPlaces = 512;
+
+struct ValueShared {
+    union {
+        uint32_t counts[kValues + 64];  // the last: of each lane's tokens elsewhere, unused
+        uint32_t matches[kValues];      // a bit per token beside the row's ends: it has the drawn value
+        Bins<kThreads> search;
+    };
+    u64 mass[kPlaces + 1];  // sums before each place
+    uint32_t count[kPlaces + 1];
+    u64 wave_a[kThreads / 64], wave_b[kThreads / 64], in_head, in_tail;
+    uint32_t highest, lowest, sum, zeros, outside, odd, bits, nth;
+    float prob;
+};
+
+// The counted values of a group, in their order: positive ones downwards,
+// negative ones upwards.
+struct Value {
+    uint32_t bits, count;
+};
+__device__ inline Value value_at(const ValueShared &s, int place) {
+    const int lane = threadIdx.x & 63;
+    if (place == kZeroPlace) return {0, lane == 0 ? s.zeros : 0};
+    const bool negative = place > kZeroPlace;
+    const uint32_t i = negative ? (place - kZeroPlace - 1) * 64 + lane : (kGroups - 1 - place) * 64 + 63 - lane;
+    const uint32_t c = s.counts[i];
+    return negative ? Value{0x8000u | (i + kSmallest), c >> 16} : Value{i + kSmallest, c & 0xffff};
+}
+__device__ inline float logit_of_bits(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+__device__ inline u64 last_lane(u64 v) {
+    return static_cast<u64>(__builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), 63)) << 32 |
+           static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(v), 63));
+}
+
+// The place of the n-th set bit.
+__device__ inline int nth_bit(u64 v, int n) {
+    for (; n; --n) v &= v - 1;
+    return __ffsll(v) - 1;
+}
+
+// A value at a given count or mass of the order: one token's mass, and what
+// is before the value.
+struct Found {
+    uint32_t bits, m;
+    u64 count_before, mass_before;
+};
+
+// The value at x below the total, by a wave; before: s.count or s.mass.
+template <typename U>
+__device__ inline Found find_value(const ValueShared &s, const U *before, float top, float c, U x) {
+    static_assert(kPlaces == 64 * 8, "two steps");
+    const int lane = threadIdx.x & 63;
+    const int part = __ffsll(static_cast<u64>(__ballot(before[8 * lane] <= x && x < before[8 * lane + 8]))) - 1;
+    const int at = 8 * part + (lane & 7);
+    const int place =
+        8 * part + ((__ffsll(static_cast<u64>(__ballot(before[at] <= x && x < before[at + 1]))) - 1) & 7);
+    const Value v = value_at(s, place);
+    const uint32_t m = v.count ? mass_of(weight(scaled(logit_of_bits(v.bits), top, c))) : 0;
+    const u64 gc = m ? v.count : 0, gm = static_cast<u64>(m) * v.count;
+    const u64 ic = s.count[place] + wave_scan(gc), im = s.mass[place] + wave_scan(gm);
+    const int l = __ffsll(static_cast<u64>(__ballot(x < (sizeof(U) == 8 ? im : ic)))) - 1;
+    return {static_cast<uint32_t>(__shfl(v.bits, l)), static_cast<uint32_t>(__shfl(m, l)), __shfl(ic - gc, l),
+            __shfl(im - gm, l)};
+}
+
+__global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(const uint16_t *__restrict__ logits, int64_t rows,
+                                                                    int vocab, int64_t ldk,
+                                                                    const float *__restrict__ uniform,
+                                                                    SampleSettings settings,
+                                                                    int32_t *__restrict__ tokens,
+                                                                    float *__restrict__ probs) {
+    constexpr int TH = kThreads, kAhead = 4;
+    typedef uint16_t Half2 __attribute__((ext_vector_type(2)));
+    __shared__ ValueShared s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const uint16_t *row = logits + r * ldk;
+        const int head = min(vocab, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / 2);
+        const int vectors = (vocab - head) / 8, tail = head + vectors * 8;
+        const uint4 *src = reinterpret_cast<const uint4 *>(row + head);
+        const int edge = tid < head ? tid : tail + tid - head;  // one of the few tokens beside the vectors
+        const uint32_t edge_bits = edge < vocab ? row[edge] : 0;
+        const Settings set = settings_of(settings, r, vocab);
+        const float u = uniform_value(uniform[r]);
+        for (int i = tid; i < kValues / 4; i += TH)
+            reinterpret_cast<uint4 *>(s.counts)[i] = make_uint4(0, 0, 0, 0);
+        if (tid == 0) s.highest = s.sum = s.zeros = s.outside = s.odd = 0, s.lowest = kValues;
+        __syncthreads();
+
+        uint32_t outside = 0, zeros = 0, odd = 0;
+        auto classify = [&](uint32_t bits) {  // of a value that has no counter
+            const uint32_t magnitude = bits & 0x7fff;
+            if (magnitude - kSmallest < static_cast<uint32_t>(kValues)) return;
+            ++outside;
+            if (magnitude == 0)
+                ++zeros;
+            else if (!(bits > 0x8000u && magnitude >= kBeyond && magnitude <= kInfinity))
+                odd = 1;
+        };
+        auto each = [&](uint4 v) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t most = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t h = e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffff;
+                const uint32_t i = (h & 0x7fff) - kSmallest;
+                most = max(most, i);
+                atomicAdd(&s.counts[min(i, static_cast<uint32_t>(kValues + lane))], 1u + (h >> 15) * 0xffffu);
+            }
+            if (most >= static_cast<uint32_t>(kValues)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) classify(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffff);
+            }
+        };
+        int at = tid;
+        for (; at + (kAhead - 1) * TH < vectors; at += kAhead * TH) {
+            uint4 v[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) v[a] = src[at + a * TH];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) each(v[a]);
+        }
+        for (; at < vectors; at += TH) each(src[at]);
+        if (edge < vocab) {
+            const uint32_t i = (edge_bits & 0x7fff) - kSmallest;
+            if (i < static_cast<uint32_t>(kValues)) atomicAdd(&s.counts[i], 1u + (edge_bits >> 15) * 0xffffu);
+            classify(edge_bits);
+        }
+        if (outside) atomicAdd(&s.outside, outside);
+        if (zeros) atomicAdd(&s.zeros, zeros);
+        if (odd) s.odd = 1;
+        __syncthreads();
+
+        // The largest value, and whether every token is accounted for.  The
+        // waves take groups in turn; which of them hold a token: a bit each.
+        uint32_t sum = 0, some = 0, highest = 0, lowest = kValues;  // highest: plus 1
+#pragma unroll 4
+        for (int i = 0; i < kGroups / (TH / 64); ++i) {
+            const uint32_t magnitude = (i * (TH / 64) + wave) * 64 + lane, c = s.counts[magnitude];
+            if (!__any(c != 0)) continue;
+            some |= 1u << i;
+            sum += (c & 0xffff) + (c >> 16);
+            if (c & 0xffff) highest = magnitude + 1;
+            if (c >> 16) lowest = min(lowest, magnitude);
+        }
+        if (sum) atomicAdd(&s.sum, sum);
+        if (highest) atomicMax(&s.highest, highest);
+        if (lowest < kValues) atomicMin(&s.lowest, lowest);
+        for (int i = tid; i <= kPlaces; i += TH) s.mass[i] = 0, s.count[i] = 0;
+        __syncthreads();
+        const uint32_t top_bits = s.highest ? s.highest - 1 + kSmallest : s.zeros ? 0 : 0x8000u | (s.lowest + kSmallest);
+        const float top = uniform_value(logit_of_bits(top_bits));
+        float *prob = probs ? probs + r : nullptr;
+        // Rows that the counts cannot tell: over 65535 tokens of a value,
+        // values without a counter, none with one, or masks that have mass.
+        if (__builtin_amdgcn_readfirstlane(s.sum + s.outside != static_cast<uint32_t>(vocab) || s.odd ||
+                                           s.sum + s.zeros == 0 || scaled(-0x1p32f, top, set.c) > -33.0f)) {
+            __syncthreads();
+            const float best = slice_max<TH>(s.search, row, 0, vocab);
+            if (best > -__builtin_inff()) {
+                search_row<TH>(s.search, row, vocab, set, u, best, tokens + r, prob);
+            } else if (tid == 0) {
+                tokens[r] = -1;
+                if (prob) *prob = best != best ? best : 0.0f;
+            }
+            __syncthreads();
+            continue;
+        }
+
+        // The places' masses and counts, then the sums before them.
+        u64 kept = 0;
+        auto add_place = [&](int place) {
+            const Value x = value_at(s, place);
+            if (!__any(x.count != 0)) return;
+            const float w = weight(scaled(logit_of_bits(x.bits), top, set.c));
+            const uint32_t one = x.count ? mass_of(w) : 0;
+            const u64 m = static_cast<u64>(one) * x.count;
+            if (!(w < set.min_p)) kept += m;
+            const u64 mass = last_lane(wave_scan(m)), counted = last_lane(wave_scan(one ? x.count : 0));
+            if (lane == 0) s.mass[place] = mass, s.count[place] = static_cast<uint32_t>(counted);
+        };
+        for (uint32_t left = __builtin_amdgcn_readfirstlane(some); left; left &= left - 1) {
+            const int group = (__ffs(left) - 1) * (TH / 64) + wave;
+            add_place(kGroups - 1 - group);
+            add_place(kZeroPlace + 1 + group);
+        }
+        if (wave == 0) add_place(kZeroPlace);
+        __syncthreads();
+        static_assert(kPlaces == TH, "a place each");
+        u64 mass = s.mass[tid], counted = s.count[tid], none = 0, all, all_counted, t0;
+        scan_threads<TH>(s.wave_a, s.wave_b, mass, counted, all, all_counted);
+        s.mass[tid] = mass, s.count[tid] = static_cast<uint32_t>(counted);
+        if (tid == 0) s.mass[kPlaces] = all, s.count[kPlaces] = static_cast<uint32_t>(all_counted);
+        scan_threads<TH>(s.wave_a, s.wave_b, kept, none, t0, none);
+        kept = t0;
+        if (wave == 0) {
+            u64 total = all;
+            if (static_cast<u64>(set.k) < all_counted) {
+                const Found f = find_value<uint32_t>(s, s.count, top, set.c, set.k - 1);
+                total = f.mass_before + (set.k - f.count_before) * f.m;
+            }
+            const u64 limit = nucleus(set.top_p, total);
+            if (limit < total) {
+                const Found f = find_value<u64>(s, s.mass, top, set.c, limit - 1);
+                total = f.mass_before + ((limit - 1 - f.mass_before) / f.m + 1) * f.m;
+            }
+            total = min(total, kept);
+            const u64 target = place(u, total);
+            const Found f = find_value<u64>(s, s.mass, top, set.c, target);
+            if (lane == 0) {
+                s.bits = f.bits;
+                s.nth = static_cast<uint32_t>((target - f.mass_before) / f.m);
+                if (prob) *prob = static_cast<float>(f.m) / static_cast<float>(total);
+            }
+        }
+        __syncthreads();
+
+        // The n-th token of the drawn value: a bit for each token.
+        const int words = (vectors + 3) / 4;
+        for (int i = tid; i < words; i += TH) s.matches[i] = 0;
+        __syncthreads();
+        const uint32_t bits = s.bits, both = bits == 0 ? 0x7fffu : 0xffffu;  // the zeros are one value
+        const uint32_t mask = both | both << 16, want = (bits & both) * 0x10001u;
+        auto match = [&](int i, uint4 v) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            uint32_t differ[4], all_differ = 0xffffffffu;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t x = (w[e] & mask) ^ want;
+                differ[e] = __builtin_bit_cast(
+                    uint32_t, __builtin_elementwise_min(__builtin_bit_cast(Half2, x), Half2{1, 1}));
+                all_differ &= differ[e];
+            }
+            if (all_differ == 0x10001u) return;
+            uint32_t found = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) found |= ((~differ[e] & 1) | (~differ[e] >> 15 & 2)) << (2 * e);
+            reinterpret_cast<uint8_t *>(s.matches)[i] = static_cast<uint8_t>(found);
+        };
+        at = tid;
+        for (; at + (kAhead - 1) * TH < vectors; at += kAhead * TH) {
+            uint4 v[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) v[a] = src[at + a * TH];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) match(at + a * TH, v[a]);
+        }
+        for (; at < vectors; at += TH) match(at, src[at]);
+        if (wave == 0) {
+            const bool hit = edge < vocab && ((edge_bits ^ bits) & both) == 0;
+            const u64 in_head = __ballot(hit && tid < head), in_tail = __ballot(hit && tid >= head);
+            if (lane == 0) s.in_head = in_head, s.in_tail = in_tail;
+        }
+        __syncthreads();
+        const int own = (words + TH - 1) / TH, from = min(tid * own, words), to = min(from + own, words);
+        u64 before = 0, t1;
+        none = 0;
+        for (int i = from; i < to; ++i) before += __popc(s.matches[i]);
+        const u64 mine = before;
+        scan_threads<TH>(s.wave_a, s.wave_b, before, none, t0, t1);
+        const u64 nth = s.nth, heads = __popcll(s.in_head);
+        if (tid == 0) {
+            if (nth < heads) tokens[r] = nth_bit(s.in_head, static_cast<int>(nth));
+            if (nth >= heads + t0) tokens[r] = tail - head + nth_bit(s.in_tail, static_cast<int>(nth - heads - t0));
+        }
+        if (nth >= heads && nth - heads - before < mine) {
+            u64 left = nth - heads - before;
+            for (int i = from; i < to; ++i) {
+                const uint32_t have = __popc(s.matches[i]);
+                if (left < have) {
+                    tokens[r] = head + i * 32 + nth_bit(s.matches[i], static_cast<int>(left));
+                    break;
+                }
+                left -= have;
+            }
+        }
         __syncthreads();
     }
 }
@@ -673,7 +1019,7 @@ __global__ __launch_bounds__(kThreads) void slice_max_kernel(const T *__restrict
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < kBins; i += gridDim.x * kThreads)
         space.mass[i] = 0, space.count[i] = 0;
     if (blockIdx.x == 0 && threadIdx.x == 0) space.kept = 0, space.listed = 0, space.done = 0;
-    const float top = slice_max(s, logits + r * ldk, lo, hi);
+    const float top = slice_max<kThreads>(s, logits + r * ldk, lo, hi);
     if (threadIdx.x == 0) space.top[blockIdx.x] = top;
 }
 
@@ -690,15 +1036,15 @@ __global__ __launch_bounds__(kThreads) void slice_histogram_kernel(const T *__re
     const float top = row_top(space, gridDim.x);
     if (!(top > -__builtin_inff() && top < __builtin_inff())) return;
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
-    clear_bins(s);
-    u64 kept = slice_histogram(s, logits + r * ldk, lo, hi, top, set, set.k < vocab), none = 0, t0, t1;
+    clear_bins<TH>(s);
+    u64 kept = slice_histogram<TH>(s, logits + r * ldk, lo, hi, top, set, set.k < vocab), none = 0, t0, t1;
     __syncthreads();
     for (int i = threadIdx.x; i < kBins; i += TH) {
         if (s.mass[i]) atomicAdd(&space.mass[i], s.mass[i]);
         if (s.count[i]) atomicAdd(&space.count[i], s.count[i]);
     }
     if (set.min_p > 0.0f) {
-        scan_threads(s, kept, none, t0, t1);
+        scan_threads<TH>(s, kept, none, t0, t1);
         if (threadIdx.x == 0 && t0) atomicAdd(&space.kept, t0);
     }
 }
@@ -734,10 +1080,10 @@ __global__ __launch_bounds__(kThreads, 4) void slice_token_kernel(const T *__res
         return;
     }
     if (top == __builtin_inff()) {
-        if (blockIdx.x == 0) search_row(s, row, vocab, set, u, top, tokens + r, prob);
+        if (blockIdx.x == 0) search_row<TH>(s, row, vocab, set, u, top, tokens + r, prob);
         return;
     }
-    scan_bins(s, m, c);
+    scan_bins<TH>(s, m, c);
     const u64 kept = set.min_p > 0.0f ? floored : s.mass[kBins];
     find_wanted(s, set, u, kept, top);
     __syncthreads();
@@ -763,19 +1109,41 @@ __global__ __launch_bounds__(kThreads, 4) void slice_token_kernel(const T *__res
         __syncthreads();
         finish(s, set, u, kept, top, listed, tokens + r, prob);
     } else {
-        search_row(s, row, vocab, set, u, top, tokens + r, prob);
+        search_row<TH>(s, row, vocab, set, u, top, tokens + r, prob);
     }
 }
 
-// Blocks per row: about two a compute unit in all, of 2048 tokens at least;
-// 1: a block per row.
+// Blocks per row; 1: a block per row and one kernel.  Three kernels and the
+// blocks' meeting cost 6 us over one, a block reads 3000 tokens a us: rows are
+// split where that saves more than 16384 tokens, over one block a compute
+// unit (1 x 128256 f32: 16 us for 50; 64 x 50257: 25 for 26; 128 x 32000: 29
+// for 24, so not).
 int slices_of(int64_t rows, int32_t vocab) {
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / rows, vocab / 2048, kMostSlices})));
+    const int64_t slices = std::min<int64_t>({256 / rows, vocab / 4096, kMostSlices});
+    return slices > 1 && vocab - vocab / slices >= 16384 ? static_cast<int>(slices) : 1;
+}
+
+// Whether a row's values are counted, with a block a row.  That costs some
+// 17 us whatever the length, the histogram of weights 10 and more per token,
+// most where much lies near the cuts (us, histogram / counts, of top-k 50 and
+// top-p 0.9; top-p 0.95): 128 x 16384: 16 / 20, 21 / 20; 128 x 32000: 21 / 24,
+// 28 / 23; 64 x 50257: 27 / 24, 37 / 24; 2048 x 16384: 70 / 83, 83 / 82;
+// 2048 x 32000: 107 / 96, 126 / 94; 2048 x 128256: 321 / 200.  Few rows are
+// split instead: 32 x 128256: 27 / 33, 44 / 33; 16 x 32000: 20 / 23, 25 / 22;
+// 1 x 128256: 17 / 32.  The upper limit is that of the matches' bits.
+bool by_values(bool bf16, int64_t rows, int32_t vocab) {
+    return bf16 && rows >= 32 && vocab >= 28 * 1024 && vocab <= 32 * kValues;
 }
 
 template <typename T>
 bool launch(const T *logits, int64_t rows, int32_t vocab, int64_t ldk, const float *uniform,
             const SampleSettings &settings, int32_t *tokens, float *probs, void *workspace, hipStream_t stream) {
+    if constexpr (sizeof(T) == 2)
+        if (by_values(true, rows, vocab)) {
+            sample_values_kernel<<<static_cast<unsigned>(std::min<int64_t>(rows, 768)), kThreads, 0, stream>>>(
+                logits, rows, vocab, ldk, uniform, settings, tokens, probs);
+            return hipGetLastError() == hipSuccess;
+        }
     const int slices = slices_of(rows, vocab);
     if (slices == 1) {
         sample_rows_kernel<<<static_cast<unsigned>(std::min<int64_t>(rows, 512)), kThreads, 0, stream>>>(
@@ -794,8 +1162,9 @@ bool launch(const T *logits, int64_t rows, int32_t vocab, int64_t ldk, const flo
 
 }  // namespace
 
-int64_t sample_workspace_bytes(int64_t rows, int32_t vocab) {
-    return rows > 0 && slices_of(rows, vocab) > 1 ? rows * static_cast<int64_t>(sizeof(RowSpace)) : 0;
+int64_t sample_workspace_bytes(bool bf16, int64_t rows, int32_t vocab) {
+    if (rows <= 0 || by_values(bf16, rows, vocab) || slices_of(rows, vocab) == 1) return 0;
+    return rows * static_cast<int64_t>(sizeof(RowSpace));
 }
 
 bool sample_launch(const void *logits, bool bf16, int64_t rows, int32_t vocab, int64_t ldk, const float *uniform,

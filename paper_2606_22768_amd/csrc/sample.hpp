@@ -16,7 +16,7 @@ struct SampleSettings {
 };
 
 // Device workspace of a call.
-int64_t sample_workspace_bytes(int64_t rows, int32_t vocab);
+int64_t sample_workspace_bytes(bool bf16, int64_t rows, int32_t vocab);
 
 // Samples one token per row of `logits` ([rows][ldk], element-aligned rows
 // of `vocab` logits); probs may be NULL.  False if a launch failed.

@@ -39,7 +39,7 @@ fgd_status fgd_sample_workspace_size(int32_t dtype, int64_t num_rows, int64_t vo
     fgd::api_clear();
     if (!bytes) return api_fail(FGD_ERR_INVALID_ARG, "NULL bytes");
     if (fgd_status st = check_sizes(dtype, num_rows, vocab)) return st;
-    *bytes = fgd::sample_workspace_bytes(num_rows, static_cast<int32_t>(vocab));
+    *bytes = fgd::sample_workspace_bytes(dtype == FGD_BF16, num_rows, static_cast<int32_t>(vocab));
     return FGD_OK;
 }
 

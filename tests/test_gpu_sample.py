@@ -288,3 +288,64 @@ def test_other_stream_and_graph(env):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(tok, want[0]) and torch.equal(prob, want[1])
+
+
+def test_many_long_bf16_rows(env):
+    """Rows whose 16-bit values are counted, beside each of the reasons that
+    send a row another way: values without a counter (tiny, huge), more of a
+    value than half a counter holds, infinities, NaN, rows of masks alone."""
+    fgd, torch = env
+    n, V = 40, 70001
+    rng = np.random.default_rng(11)
+    z = rng.integers(-24, 9, (n, V)).astype(np.float32)
+    z[rng.random((n, V)) < 0.1] = -np.inf
+    lowest = -float(torch.finfo(torch.bfloat16).max)
+    z[1] = -np.inf
+    z[2, 5::2] = lowest
+    z[3] = lowest
+    z[4] = 0.0
+    z[4, ::3] = -0.0
+    z[5] = np.where(rng.random(V) < 0.5, 0.0, -0.0)
+    z[6] = 4.0  # 70001 tokens of one value
+    z[7] = -3.0
+    z[8, 100] = np.nan
+    z[9, 60000] = z[9, 61000] = np.inf
+    z[10, :] = -5.0
+    z[10, 69999] = 2.0 ** -40
+    z[11, 17] = 2.0 ** 40
+    z[12] = -np.inf
+    z[12, 70000] = -1.0
+    z[13] = -np.inf
+    z[13, 0] = 2.0
+    z[14] = -(2.0 ** 33)
+    z[15, 1:] = -np.inf
+    u = rng.random(n).astype(np.float32)
+    settings = [SETTINGS[i % len(SETTINGS)] if i < 20 else SETTINGS[-(i % len(SETTINGS)) - 1] for i in range(n)]
+    get = lambda k, d: _rows(torch, [s.get(k, d) for s in settings],  # noqa: E731
+                             np.int32 if k == "top_k" else np.float32)
+    kw = dict(top_k=get("top_k", 0), top_p=get("top_p", 1.0), min_p=get("min_p", 0.0))
+    dense = _cuda(torch, z, "bf16")
+    wide = torch.full((n, V + 6), 9.0, dtype=torch.bfloat16, device="cuda")
+    for shift in (0, 1, 3):  # rows that start on no boundary of 16 bytes
+        wide.fill_(9.0)
+        wide[:, shift:shift + V] = dense
+        for T in (UNIT_T, 0.0):
+            print(f"[sample] counted rows, shift {shift}, T {T}", flush=True)
+            tok, prob = fgd.sample(wide[:, shift:shift + V], _rows(torch, u), T, **kw)
+            tok, prob = tok.cpu().numpy(), prob.cpu().numpy()
+            for i, s in enumerate(settings):
+                t, mass, total, _, _, _ = ref.sample(z[i], u[i], T, **s)
+                assert tok[i] == t, (i, s, u[i])
+                if i == 8:
+                    assert np.isnan(prob[i])
+                elif t < 0:
+                    assert prob[i] == 0
+                elif T:
+                    assert prob[i] == np.float32(np.float32(mass) / np.float32(total)), (i, s)
+    # Few rows take another form: the same tokens and probabilities.
+    got = fgd.sample(dense, _rows(torch, u), 0.7, **kw)
+    for lo in range(0, n, 8):
+        few = fgd.sample(dense[lo:lo + 8], _rows(torch, u[lo:lo + 8]), 0.7,
+                         **{k: v[lo:lo + 8] for k, v in kw.items()})
+        for a, b in zip(got, few):
+            assert torch.equal(torch.nan_to_num(a[lo:lo + 8], nan=-9.0), torch.nan_to_num(b, nan=-9.0))
