@@ -9,10 +9,15 @@ gradients need it:
     w4 = mx4_quantize(w)                  # w [N][K], or [M][N][K]: every worker's
     y = mx4_linear(x, w4)                 # x [T][K] -> y [T][N]
     dx, dw = mx4_linear_grads(dy, x, mx4_quantize(w.mT))
+
+A call that is given a stream runs on it, and the tensors that it allocates
+belong to that stream, as under torch.cuda.stream; before another stream uses
+them, it has to wait.
 """
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 from . import DTYPES, FGD_BF16, FGD_F32, _check, _dev, _stream, lib
@@ -116,20 +121,22 @@ def _on_gpu(name, t, device):
         raise ValueError(f"{name}: expected a tensor on {'a GPU' if device is None else device}, got {t.device}")
 
 
-def _current(device, stream):
-    """The given stream, or torch's current one on `device`."""
-    if stream is not None:
-        return stream
+_HERE = contextlib.nullcontext()
+
+
+def _on(device, stream=None):
+    """A context in which `device` and the stream (torch's current one when
+    none is given) are current, so that what a call allocates in it belongs to
+    the stream that uses it."""
     import torch
 
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-def _on(device):
-    """A context in which `device` is current."""
-    import torch
-
-    return torch.cuda.device(device)
+    if stream is None:
+        return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device)
+    if stream.device != device:
+        raise ValueError(f"stream: expected a stream of {device}, got one of {stream.device}")
+    return torch.cuda.stream(stream)
 
 
 def _is_mx4(q, name):
@@ -138,24 +145,31 @@ def _is_mx4(q, name):
     return q
 
 
-def _output(out, dtype, shape, device):
-    """The output tensor, checked or new, and its dtype code and strides."""
+def _output_dtype(out, dtype, shape, device):
+    """torch's dtype of the output tensor, which is checked if there is one."""
     import torch
 
     if out is None:
         t = {"f32": torch.float32, "bf16": torch.bfloat16}.get(dtype, dtype)
         if t not in (torch.float32, torch.bfloat16):
             raise TypeError(f"dtype: expected 'f32' or 'bf16', got {dtype!r}")
+        return t
+    _dtype_code(out, "out")
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError(f"out: expected shape {tuple(shape)}, got {tuple(out.shape)}")
+    _on_gpu("out", out, device)
+    if out.shape[-1] > 1 and out.stride(-1) != 1:
+        raise ValueError("out: rows must be contiguous")
+    return out.dtype
+
+
+def _output(out, t, shape, device):
+    """The output tensor, new if there is none, and its dtype code and strides."""
+    import torch
+
+    if out is None:
         out = torch.empty(shape, dtype=t, device=device)
-    else:
-        _dtype_code(out, "out")
-        if tuple(out.shape) != tuple(shape):
-            raise ValueError(f"out: expected shape {tuple(shape)}, got {tuple(out.shape)}")
-        _on_gpu("out", out, device)
-        if out.shape[-1] > 1 and out.stride(-1) != 1:
-            raise ValueError("out: rows must be contiguous")
-    code = FGD_F32 if out.dtype == torch.float32 else FGD_BF16
-    return out, code, (out.stride(0) if out.dim() == 3 else 0), out.stride(-2)
+    return out, FGD_F32 if t == torch.float32 else FGD_BF16, (out.stride(0) if out.dim() == 3 else 0), out.stride(-2)
 
 
 def mx4_quantize(x, stream=None) -> Mx4:
@@ -175,10 +189,10 @@ def mx4_quantize(x, stream=None) -> Mx4:
     _on_gpu("x", x, None)
     n = 1 if batch is None else batch
     cb, sb = fgd_mx4_size(n, rows, cols)
-    pool = torch.empty(cb + sb, dtype=torch.uint8, device=x.device)
-    q = Mx4(pool[:cb], pool[cb:], batch, rows, cols)
-    with _on(x.device):
-        fgd_mx4_quantize(x, code, n, rows, cols, bs, rs, cs, q.codes, q.scales, _current(x.device, stream))
+    with _on(x.device, stream):
+        pool = torch.empty(cb + sb, dtype=torch.uint8, device=x.device)
+        q = Mx4(pool[:cb], pool[cb:], batch, rows, cols)
+        fgd_mx4_quantize(x, code, n, rows, cols, bs, rs, cs, q.codes, q.scales)
     return q
 
 
@@ -186,10 +200,11 @@ def mx4_dequantize(q, dtype="f32", out=None, stream=None):
     """The values of q, as a tensor of `dtype` ("f32", "bf16" or torch's) or
     into `out`."""
     _is_mx4(q, "q")
-    out, code, bs, rs = _output(out, dtype, q.shape, q.device)
-    with _on(q.device):
-        fgd_mx4_dequantize(q.codes, q.scales, 1 if q.batch is None else q.batch, q.rows, q.cols, out, code, bs, rs,
-                           _current(q.device, stream))
+    t = _output_dtype(out, dtype, q.shape, q.device)
+    _on_gpu("q", q, None)
+    with _on(q.device, stream):
+        out, code, bs, rs = _output(out, t, q.shape, q.device)
+        fgd_mx4_dequantize(q.codes, q.scales, 1 if q.batch is None else q.batch, q.rows, q.cols, out, code, bs, rs)
     return out
 
 
@@ -203,10 +218,12 @@ def mx4_matmul(a, w, dtype="bf16", out=None, stream=None):
     if a.device != w.device:
         raise ValueError(f"a and w must be on one GPU, got {a.device} and {w.device}")
     shape = (a.rows, w.rows) if a.batch is None else (a.batch, a.rows, w.rows)
-    out, code, bs, rs = _output(out, dtype, shape, a.device)
-    with _on(a.device):
+    t = _output_dtype(out, dtype, shape, a.device)
+    _on_gpu("a", a, None)
+    with _on(a.device, stream):
+        out, code, bs, rs = _output(out, t, shape, a.device)
         fgd_mx4_matmul(a.codes, a.scales, w.codes, w.scales, 1 if a.batch is None else a.batch, a.rows, w.rows,
-                       a.cols, out, code, bs, rs, _current(a.device, stream))
+                       a.cols, out, code, bs, rs)
     return out
 
 
@@ -227,15 +244,16 @@ def mx4_linear(x, w, dtype=None, out=None, workspace=None, stream=None):
     _on_gpu("x", x, w.device)
     n = 1 if batch is None else batch
     shape = (rows, w.rows) if batch is None else (batch, rows, w.rows)
-    out, ocode, obs, ors = _output(out, x.dtype if dtype is None else dtype, shape, x.device)
+    t = _output_dtype(out, x.dtype if dtype is None else dtype, shape, x.device)
     need = fgd_mx4_linear_workspace_size(n, rows, cols)
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
-    else:
+    if workspace is not None:
         _check_workspace(workspace, need, x.device)
-    with _on(x.device):
+    with _on(x.device, stream):
+        out, ocode, obs, ors = _output(out, t, shape, x.device)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
         fgd_mx4_linear(x, code, bs, rs, w.codes, w.scales, n, rows, w.rows, cols, out, ocode, obs, ors, workspace,
-                       workspace.numel() * workspace.element_size(), _current(x.device, stream))
+                       workspace.numel() * workspace.element_size())
     return out
 
 

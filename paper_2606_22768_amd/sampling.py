@@ -6,6 +6,7 @@ from __future__ import annotations
 import ctypes
 
 from . import DTYPES, FGD_BF16, FGD_F32, _check, _dev, _stream, lib
+from .mx4 import _check_workspace, _on
 
 
 class fgd_sampling(ctypes.Structure):
@@ -89,20 +90,16 @@ def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, voca
         _rows(probs_out, "probs_out", torch.float32, U, dev)
     need = fgd_sample_workspace_size(dtype, U, V)
     if workspace is not None:
-        from .mx4 import _check_workspace
-
         _check_workspace(workspace, need, dev)
     if dev.type != "cuda":
         raise ValueError(f"logits: expected a tensor on a GPU, got {dev}")
-    tokens_out = torch.empty(U, dtype=torch.int32, device=dev) if tokens_out is None else tokens_out
-    probs_out = torch.empty(U, dtype=torch.float32, device=dev) if probs_out is None else probs_out
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    if stream is None:
-        stream = torch.cuda.current_stream(dev).cuda_stream
-    with torch.cuda.device(dev):
+    with _on(dev, stream):
+        tokens_out = torch.empty(U, dtype=torch.int32, device=dev) if tokens_out is None else tokens_out
+        probs_out = torch.empty(U, dtype=torch.float32, device=dev) if probs_out is None else probs_out
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         fgd_sample(logits, dtype, U, V, ldk, uniform, s, tokens_out, probs_out, workspace,
-                   0 if workspace is None else workspace.numel() * workspace.element_size(), stream)
+                   0 if workspace is None else workspace.numel() * workspace.element_size())
     return tokens_out, probs_out
 
 

@@ -332,3 +332,32 @@ def test_other_stream_and_graph(env):
         torch.cuda.synchronize()
         assert torch.equal(y, want), rep
         assert np.array_equal(_host(back), ref.mx4_values(_host(w)))
+
+
+def test_what_a_call_allocates_belongs_to_its_stream(env):
+    """The calls' own workspaces, temporaries and outputs are not handed to
+    the current stream while the stream that they were given is still to run."""
+    fgd, torch = env
+    x = _tensor(torch, _values((1000, 512), 3), "bf16")
+    w = _tensor(torch, _values((600, 512), 4), "bf16")
+    dy = _tensor(torch, _values((1000, 600), 5), "bf16")
+    z = _tensor(torch, _values((2, 200000), 6), "f32")
+    u = torch.full((2,), 0.5, device="cuda")
+    w4, w_t4 = fgd.mx4_quantize(w), fgd.mx4_quantize(w.mT)
+
+    def calls(stream):
+        return [fgd.mx4_linear(x, w4, stream=stream), *fgd.mx4_linear_grads(dy, x, w_t4, stream=stream),
+                fgd.mx4_dequantize(fgd.mx4_quantize(x, stream), stream=stream), *fgd.sample(z, u, stream=stream)]
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)  # about 10 ms
+        got = calls(stream)
+        mine = [torch.full((n,), 0xA5, dtype=torch.uint8, device="cuda")
+                for n in [2 ** k for k in range(9, 22)] for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all(bool((t == 0xA5).all()) for t in mine)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
