@@ -65,36 +65,72 @@ __device__ inline void store4(uint16_t *row, int64_t c, int64_t n, float4v v) {
     }
 }
 
-// Stores one lane's part of a 32 x 32 result: columns c0 + 8 q + 4 (lane /
-// 32) + e of its row.  Two lanes of a bf16 row first exchange halves, so that
-// each stores eight consecutive columns.  (Stores of whole lines, by way of
-// LDS, measured no faster: 2048 x 128256 x 4096 to bf16 in 653 us for 629.)
-__device__ inline void store_rows(float *row, int64_t c0, int64_t n, bool in, int lane, float16v v) {
-    if (!in) return;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-        store4(row, c0 + 8 * q + (lane >> 5) * 4, n, float4v{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]});
-}
-__device__ inline void store_rows(uint16_t *row, int64_t c0, int64_t n, bool in, int lane, float16v v) {
+// Stores a 32 x 32 result, whose rows are the first m of those at `rows` and
+// whose columns are the first n of those there; ALL: all are, and there are
+// kStores<T> stores that nothing skips.  Lanes first exchange registers, so
+// that four of them, l % 16 alike, store 64 consecutive bytes of a row.
+// (Whole lines by way of LDS, pieces of 32 bytes and stores past the caches
+// measured no faster at 2048 x 128256 x 4096 to bf16: 4, 0 and 20% slower.)
+template <typename T>
+constexpr int kStores = sizeof(T);
+
+template <bool ALL>
+__device__ inline void store_rows(float *rows, int64_t stride, int64_t m, int64_t n, int lane, float16v v) {
+    const int r = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int q = 0; q < 4; q += 2) {
-        uint32_t w[4];
+        float4v even, odd;  // of rows r and r + 16: the 4 columns from c
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = round_bf16(v[4 * q + 2 * e]) | static_cast<uint32_t>(round_bf16(v[4 * q + 2 * e + 1])) << 16;
-        // w[0..1]: columns 4 (lane / 32) .. + 3, w[2..3]: those + 8.
-        const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-        const auto hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-        const int64_t c = c0 + 8 * q + (lane >> 5) * 8;
-        const uint32_t x[4] = {lo[0], hi[0], lo[1], hi[1]};
-        if (!in) continue;
-        if (c + 7 < n) {
-            *reinterpret_cast<Eight16 *>(row + c) = Eight16{{x[0], x[1], x[2], x[3]}};
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e < n) row[c + e] = static_cast<uint16_t>(x[e >> 1] >> (16 * (e & 1)));
+        for (int e = 0; e < 4; ++e) {
+            const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[4 * q + e]),
+                                                            __float_as_uint(v[4 * q + 4 + e]), false, false);
+            even[e] = __uint_as_float(x[0]), odd[e] = __uint_as_float(x[1]);
         }
+        const int c = 8 * q + (g & 1) * 8 + (g >> 1) * 4;
+        if (ALL) {
+            *reinterpret_cast<Four32 *>(rows + r * stride + c) = Four32{{even[0], even[1], even[2], even[3]}};
+            *reinterpret_cast<Four32 *>(rows + (r + 16) * stride + c) = Four32{{odd[0], odd[1], odd[2], odd[3]}};
+        } else {
+            if (r < m) store4(rows + r * stride, c, n, even);
+            if (r + 16 < m) store4(rows + (r + 16) * stride, c, n, odd);
+        }
+    }
+}
+
+__device__ inline void store8(uint16_t *row, int64_t c, int64_t n, Eight16 x) {
+    if (c + 7 < n) {
+        *reinterpret_cast<Eight16 *>(row + c) = x;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < n) row[c + e] = static_cast<uint16_t>(x.v[e >> 1] >> (16 * (e & 1)));
+    }
+}
+template <bool ALL>
+__device__ inline void store_rows(uint16_t *rows, int64_t stride, int64_t m, int64_t n, int lane, float16v v) {
+    const int r = lane & 15, g = lane >> 4;
+    uint32_t w[8];  // columns 8 i + 4 (lane / 32) .. + 3 in w[2 i ..]
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        w[i] = round_bf16(v[2 * i]) | static_cast<uint32_t>(round_bf16(v[2 * i + 1])) << 16;
+    Eight16 even, odd;  // of rows r and r + 16: the 8 columns from c
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        // Eight columns a lane, 8 (lane / 32) .. + 7 of each 16 ...
+        const auto lo = __builtin_amdgcn_permlane32_swap(w[i], w[2 + i], false, false);
+        const auto hi = __builtin_amdgcn_permlane32_swap(w[4 + i], w[6 + i], false, false);
+        // ... then those of 16 rows.
+        const auto x = __builtin_amdgcn_permlane16_swap(lo[0], hi[0], false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(lo[1], hi[1], false, false);
+        even.v[i] = x[0], odd.v[i] = x[1], even.v[2 + i] = y[0], odd.v[2 + i] = y[1];
+    }
+    const int c = (g & 1) * 16 + (g >> 1) * 8;
+    if (ALL) {
+        *reinterpret_cast<Eight16 *>(rows + r * stride + c) = even;
+        *reinterpret_cast<Eight16 *>(rows + (r + 16) * stride + c) = odd;
+    } else {
+        if (r < m) store8(rows + r * stride, c, n, even);
+        if (r + 16 < m) store8(rows + (r + 16) * stride, c, n, odd);
     }
 }
 
@@ -263,8 +299,16 @@ __device__ inline void outer(float16v (&acc)[NW][NA], int i, int j, const int4v 
     acc[i + 1][j + 1] = mfma<3, 3>(x[3], y[3], acc[i + 1][j + 1], sx, sy);
 }
 
-// Waits until at most LOADS of this wave's loads are on their way and all
-// that it read from LDS has come, then for the block's other waves.
+// Waits until at most N of this wave's loads and stores are on their way.
+template <int N>
+__device__ inline void outstanding() {
+    static_assert(N < 64, "the counter's range");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
+// The same, and until all that it read from LDS has come, then for the
+// block's other waves.
 template <int LOADS>
 __device__ inline void arrive() {
     static_assert(LOADS < 64, "the counter's range");
@@ -297,7 +341,13 @@ __device__ inline void interleave() {
 // ------------------------------------------------------------ large products
 //
 // GN x GA waves, each holding WN x WA tiles of 64 x 64 outputs (rows of w by
-// rows of a) in registers.
+// rows of a) in registers.  A block takes block after block of the outputs,
+// as one run of steps: the first tiles of the next are on their way while the
+// last products of one are stored (2048 x 128256 x 4096 to bf16: 652 us for
+// 695 with a block each; 8192^3: 255 for 263).  Bound by the matrix unit's
+// power over the steps (8192^3 without loads and reads: 240 us of 255, 4.3
+// PFLOP/s) and by the memory's writes between them, which the steps do not
+// hide: 2048 x 128256 x 4096 without stores takes 531 us.
 template <int GN, int GA, int WN, int WA, typename T>
 __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_kernel(
     const uint8_t *__restrict__ a_codes, const uint8_t *__restrict__ a_scales, const uint8_t *__restrict__ w_codes,
@@ -307,52 +357,79 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
     constexpr int kCodes = (N + A) * 256 / kThreads, kScales = ((N + A) * 64 + kThreads - 1) / kThreads;
     constexpr int kLoads = kCodes + kScales, kSlots = 3;
     // Every wave issues the same loads, so that it can count them: scales
-    // past the last tile's repeat its last ones, behind them.
+    // past the last tile's repeat its, behind them.
     constexpr int kStage = (N + A) * kMx4CodeBytes + kScales * kThreads * 4;
     static_assert(kCodes * kThreads == (N + A) * 256, "whole chunks per thread");
     __shared__ __attribute__((aligned(16))) uint8_t lds[kSlots * kStage];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = wave % GN, wa = wave / GN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wn = wave % GN,
+              wa = wave / GN;
     // Blocks go to the eight dies in turn; each die takes a contiguous range
     // of the order below, in which 32 neighbours (a die's compute units) are
     // 8 blocks of a by 4 of w: what its L2 serves to all of them is least.
-    const int64_t id = static_cast<int64_t>(blockIdx.x & 7) * blocks_per_xcd + (blockIdx.x >> 3);
-    const int64_t per_batch = static_cast<int64_t>(n_blocks) * a_blocks, b = id / per_batch;
-    if (b >= batch) return;
-    const int in_batch = static_cast<int>(id % per_batch), strip = in_batch / (8 * n_blocks) * 8,
-              in_strip = in_batch % (8 * n_blocks), width = min(8, a_blocks - strip);
-    const int nb = in_strip / width, ab = strip + in_strip % width;
+    const uint32_t per_batch = static_cast<uint32_t>(n_blocks) * a_blocks, first = (blockIdx.x & 7) * blocks_per_xcd;
+    const int count = static_cast<int>(min(static_cast<int64_t>(blocks_per_xcd), batch * per_batch - first));
+    const int stride = gridDim.x >> 3;
     const int64_t a_tiles = (m + 63) / 64, w_tiles = (n + 63) / 64;
-
-    // Tiles past the end repeat the last one, unstored.
-    auto tile_of = [&](int j) {
-        return j < N ? b * w_tiles + min(static_cast<int64_t>(nb) * N + j, w_tiles - 1)
-                     : b * a_tiles + min(static_cast<int64_t>(ab) * A + (j - N), a_tiles - 1);
+    struct Place {
+        int64_t b, nb, ab;
     };
+    auto place_of = [&](int item) {
+        const uint32_t id = first + item, b = id / per_batch, in_batch = id - b * per_batch, across = 8u * n_blocks;
+        const uint32_t strip = in_batch / across * 8, in_strip = in_batch % across,
+                       width = min(8u, static_cast<uint32_t>(a_blocks) - strip);
+        auto uniform = [](uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(v)); };
+        return Place{uniform(b), uniform(in_strip / width), uniform(strip + in_strip % width)};
+    };
+
+    // What is loaded next: step `ahead` of a block of the outputs.  A wave's
+    // chunks of 64 lanes lie within a tile.
     const uint8_t *code_src[kCodes], *scale_src[kScales];
+    int item = blockIdx.x >> 3, loading = item, ahead = 0;
+    if (item >= count) return;
+    auto aim = [&] {
+        const Place at = place_of(loading);
+        // Tiles past the end repeat the last one, unstored.
+        auto tile_of = [&](int j) {
+            return j < N ? at.b * w_tiles + min(at.nb * N + j, w_tiles - 1)
+                         : at.b * a_tiles + min(at.ab * A + (j - N), a_tiles - 1);
+        };
 #pragma unroll
-    for (int i = 0; i < kCodes; ++i) {
-        const int c = i * kThreads + tid, j = c >> 8;
-        code_src[i] = (j < N ? w_codes : a_codes) + tile_of(j) * kt * kMx4CodeBytes + (c & 255) * 16;
-    }
+        for (int i = 0; i < kCodes; ++i) {
+            const int c = i * kThreads + wave * 64, j = c >> 8;
+            code_src[i] = (j < N ? w_codes : a_codes) + tile_of(j) * kt * kMx4CodeBytes + (c & 255) * 16;
+        }
 #pragma unroll
-    for (int i = 0; i < kScales; ++i) {
-        const int c = min(i * kThreads + tid, (N + A) * 64 - 1), j = c >> 6;
-        scale_src[i] = (j < N ? w_scales : a_scales) + tile_of(j) * kt * kMx4ScaleBytes + (c & 63) * 4;
-    }
-    // Copies step k's tiles to a slot: 16 (or 4) bytes a lane, straight to LDS.
-    auto fetch = [&](int k, int slot) {
+        for (int i = 0; i < kScales; ++i) {
+            const int j = min(i * (kThreads / 64) + wave, N + A - 1);
+            scale_src[i] = (j < N ? w_scales : a_scales) + tile_of(j) * kt * kMx4ScaleBytes;
+        }
+    };
+    // Copies its tiles to a slot: 16 (or 4) bytes a lane, straight to LDS.
+    const uint32_t lane16 = lane * 16, lane4 = lane * 4;
+    auto fetch = [&](int slot) {
         uint8_t *p = lds + slot * kStage, *q = p + (N + A) * kMx4CodeBytes;
 #pragma unroll
         for (int i = 0; i < kCodes; ++i)
             __builtin_amdgcn_global_load_lds(
-                (const __attribute__((address_space(1))) void *)(code_src[i] + static_cast<int64_t>(k) * kMx4CodeBytes),
+                (const __attribute__((address_space(1))) void *)(code_src[i] +
+                                                                 static_cast<int64_t>(ahead) * kMx4CodeBytes + lane16),
                 (__attribute__((address_space(3))) void *)(p + (i * kThreads + wave * 64) * 16), 16, 0, 0);
 #pragma unroll
         for (int i = 0; i < kScales; ++i)
             __builtin_amdgcn_global_load_lds(
                 (const __attribute__((address_space(1))) void *)(scale_src[i] +
-                                                                 static_cast<int64_t>(k) * kMx4ScaleBytes),
+                                                                 static_cast<int64_t>(ahead) * kMx4ScaleBytes + lane4),
                 (__attribute__((address_space(3))) void *)(q + (i * kThreads + wave * 64) * 4), 4, 0, 0);
+    };
+    // Past the last step that one is loaded again, and unused: a branch
+    // around the loads would cost the registers that hold the result.
+    auto advance = [&] {
+        if (++ahead < kt) return;
+        ahead = kt - 1;
+        if (loading + stride >= count) return;
+        ahead = 0;
+        loading += stride;
+        aim();
     };
     auto frag = [&](int slot, int tile, int f) {
         return *reinterpret_cast<const int4v *>(lds + slot * kStage + tile * kMx4CodeBytes + f * 1024 + lane * 16);
@@ -362,7 +439,7 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
                                               lane * 4);
     };
 
-    float16v acc[2 * WN][2 * WA] = {};
+    float16v acc[2 * WN][2 * WA];
     // A step's operands in registers.
     struct Operands {
         int4v w[4 * WN], a[4 * WA];
@@ -390,53 +467,88 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
             for (int u = 0; u < 2 * WA; ++u) asm volatile("" : "+v"(acc[t][u]));
     };
 
-    // The ring of slots.  While step k multiplies, its own slot, already
-    // read, takes step k + kSlots, and the operands of step k + 1 are read
-    // from theirs; the barrier before says that step k is read and that step
-    // k + 1 has arrived everywhere.
+    // The ring of slots.  While a step multiplies, its own slot, already read,
+    // takes the step kSlots after it, and the next one's operands are read
+    // from theirs; the barrier before says that this step is read and the
+    // next one has arrived everywhere.  Loads and stores complete in their
+    // order: what has to have arrived was issued two steps before, so behind
+    // it are one step's loads and, for two steps, the stores of a block.
+    constexpr int kBehind = 4 * WN * WA * kStores<T>;
+    aim();
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) fetch(min(i, kt - 1), i);
+    for (int i = 0; i < kSlots; ++i) {
+        fetch(i);
+        advance();
+    }
     arrive<(kSlots - 1) * kLoads>();
     read(held[0], 0);
-    int slot = 0, k = 0;
+    int slot = 0, stored = 0;
     auto step = [&](int p) {
         const int after = slot == kSlots - 1 ? 0 : slot + 1;
-        arrive<(kSlots - 2) * kLoads>();
+        if (stored) {
+            --stored;
+            outstanding<(kSlots - 2) * kLoads + kBehind>();
+        } else {
+            outstanding<(kSlots - 2) * kLoads>();
+        }
+        arrive<(kSlots - 2) * kLoads + kBehind>();
         __builtin_amdgcn_sched_barrier(0);
-        // Past the last step these read and load tiles that nothing uses:
-        // a branch would cost the registers that hold the result.
         read(held[p ^ 1], after);
-        fetch(min(k + kSlots, kt - 1), slot);
+        fetch(slot);
         multiply(held[p]);
         interleave<8 * WN * WA, 5 * (WN + WA), kLoads>();
         __builtin_amdgcn_sched_barrier(0);
         slot = after;
-        ++k;
+        advance();
     };
-    while (k + 1 < kt) {
-        step(0);
-        step(1);
-    }
-    if (k < kt) step(0);
-    __builtin_amdgcn_s_waitcnt(7 << 4 | 15 << 8);  // vmcnt(0): nothing may still be on its way to this block's LDS
-    const int64_t n0 = (static_cast<int64_t>(nb) * N + wn * WN) * 64;
-    const int64_t m0 = (static_cast<int64_t>(ab) * A + wa * WA) * 64 + (lane & 31);
+    for (; item < count; item += stride) {
 #pragma unroll
-    for (int j = 0; j < 2 * WA; ++j) {
-        const int64_t i = m0 + j * 32;
-        T *row = out + b * batch_stride + i * row_stride;
+        for (int f = 0; f < 2 * WN; ++f)
 #pragma unroll
-        for (int f = 0; f < 2 * WN; ++f) store_rows(row, n0 + f * 32, n, i < m, lane, acc[f][j]);
+            for (int j = 0; j < 2 * WA; ++j) acc[f][j] = float16v{};
+        int k = 0;
+        for (; k + 1 < kt; k += 2) {
+            step(0);
+            step(1);
+        }
+        if (k < kt) {
+            step(0);
+            held[0] = held[1];
+        }
+        const Place at = place_of(item);
+        const int64_t n0 = (at.nb * N + wn * WN) * 64,
+                      m0 = (at.ab * A + wa * WA) * 64;
+        T *to = out + at.b * batch_stride + m0 * row_stride + n0;
+        auto store = [&](auto all) {
+#pragma unroll
+            for (int j = 0; j < 2 * WA; ++j)
+#pragma unroll
+                for (int f = 0; f < 2 * WN; ++f)
+                    store_rows<decltype(all)::value>(to + j * 32 * row_stride + f * 32, row_stride, m - m0 - j * 32,
+                                                     n - n0 - f * 32, lane, acc[f][j]);
+        };
+        if (n0 + 64 * WN <= n && m0 + 64 * WA <= m) {
+            store(std::true_type());
+            stored = 2;
+        } else {
+            store(std::false_type());
+            outstanding<0>();  // an unknown number of them
+        }
     }
+    outstanding<0>();  // nothing may still be on its way to this block's LDS
 }
 
 template <int GN, int GA, int WN, int WA, typename T>
 bool launch_tiled(const uint8_t *ac, const uint8_t *as, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m,
                   int64_t n, int64_t kt, T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
+    // A die's range: whole groups of eight blocks.
     const int64_t nb = (mx4_row_tiles(n) + GN * WN - 1) / (GN * WN), ab = (mx4_row_tiles(m) + GA * WA - 1) / (GA * WA);
-    const int64_t per = (batch * nb * ab + 7) / 8;
-    if (nb * ab > INT32_MAX / 8 || per * 8 > INT32_MAX || kt > INT32_MAX) return false;
-    tiled_kernel<GN, GA, WN, WA, T><<<static_cast<unsigned>(per * 8), 64 * GN * GA, 0, stream>>>(
+    const int64_t per = (batch * nb * ab + 63) / 64 * 8;
+    if (nb * ab > INT32_MAX / 8 || per > INT32_MAX / 8 || kt > INT32_MAX) return false;
+    // As many blocks as the card holds: one of 512 threads a compute unit, two
+    // of 256.
+    const int64_t held = 32 * 512 / (64 * GN * GA);
+    tiled_kernel<GN, GA, WN, WA, T><<<static_cast<unsigned>(std::min(per, held) * 8), 64 * GN * GA, 0, stream>>>(
         ac, as, wc, ws, m, n, static_cast<int>(kt), batch, static_cast<int>(nb), static_cast<int>(ab),
         static_cast<int>(per), out, batch_stride, row_stride);
     return hipGetLastError() == hipSuccess;
