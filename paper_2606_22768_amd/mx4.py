@@ -139,6 +139,14 @@ def _on(device, stream=None):
     return torch.cuda.stream(stream)
 
 
+def _current(device):
+    """torch's current stream on `device` (its number spares torch a search for
+    the current one, which takes longer than the rest of a call)."""
+    import torch
+
+    return torch.cuda.current_stream(device.index).cuda_stream
+
+
 def _is_mx4(q, name):
     if not isinstance(q, Mx4):
         raise TypeError(f"{name}: expected an Mx4 matrix (mx4_quantize), got {type(q).__name__}")
@@ -192,7 +200,7 @@ def mx4_quantize(x, stream=None) -> Mx4:
     with _on(x.device, stream):
         pool = torch.empty(cb + sb, dtype=torch.uint8, device=x.device)
         q = Mx4(pool[:cb], pool[cb:], batch, rows, cols)
-        fgd_mx4_quantize(x, code, n, rows, cols, bs, rs, cs, q.codes, q.scales)
+        fgd_mx4_quantize(x, code, n, rows, cols, bs, rs, cs, q.codes, q.scales, _current(x.device))
     return q
 
 
@@ -204,7 +212,8 @@ def mx4_dequantize(q, dtype="f32", out=None, stream=None):
     _on_gpu("q", q, None)
     with _on(q.device, stream):
         out, code, bs, rs = _output(out, t, q.shape, q.device)
-        fgd_mx4_dequantize(q.codes, q.scales, 1 if q.batch is None else q.batch, q.rows, q.cols, out, code, bs, rs)
+        fgd_mx4_dequantize(q.codes, q.scales, 1 if q.batch is None else q.batch, q.rows, q.cols, out, code, bs, rs,
+                           _current(q.device))
     return out
 
 
@@ -223,7 +232,7 @@ def mx4_matmul(a, w, dtype="bf16", out=None, stream=None):
     with _on(a.device, stream):
         out, code, bs, rs = _output(out, t, shape, a.device)
         fgd_mx4_matmul(a.codes, a.scales, w.codes, w.scales, 1 if a.batch is None else a.batch, a.rows, w.rows,
-                       a.cols, out, code, bs, rs)
+                       a.cols, out, code, bs, rs, _current(a.device))
     return out
 
 
@@ -253,7 +262,7 @@ def mx4_linear(x, w, dtype=None, out=None, workspace=None, stream=None):
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
         fgd_mx4_linear(x, code, bs, rs, w.codes, w.scales, n, rows, w.rows, cols, out, ocode, obs, ors, workspace,
-                       workspace.numel() * workspace.element_size())
+                       workspace.numel() * workspace.element_size(), _current(x.device))
     return out
 
 
@@ -283,6 +292,8 @@ def mx4_linear_grads(dy, x, w_t, dx_dtype=None, dw_dtype="f32", stream=None):
         if x.shape[:-1] != dy.shape[:-1] or x.shape[-1] != w_t.rows:
             raise ValueError(f"x: expected shape {(*dy.shape[:-1], w_t.rows)}, got {tuple(x.shape)}")
         x_t = mx4_quantize(x.mT, stream)
+    elif x_t.rows != w_t.rows:
+        raise ValueError(f"x: expected {w_t.rows} rows of its transpose, got shape {x_t.shape}")
     dx = mx4_matmul(mx4_quantize(dy, stream), w_t, dy.dtype if dx_dtype is None else dx_dtype, stream=stream)
     dw = mx4_matmul(mx4_quantize(dy.mT, stream), x_t, dw_dtype, stream=stream)
     return dx, dw

@@ -6,7 +6,7 @@ from __future__ import annotations
 import ctypes
 
 from . import DTYPES, FGD_BF16, FGD_F32, _check, _dev, _stream, lib
-from .mx4 import _check_workspace, _on
+from .mx4 import _check_workspace, _current, _on
 
 
 class fgd_sampling(ctypes.Structure):
@@ -99,7 +99,7 @@ def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, voca
         if workspace is None and need:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         fgd_sample(logits, dtype, U, V, ldk, uniform, s, tokens_out, probs_out, workspace,
-                   0 if workspace is None else workspace.numel() * workspace.element_size())
+                   0 if workspace is None else workspace.numel() * workspace.element_size(), _current(dev))
     return tokens_out, probs_out
 
 

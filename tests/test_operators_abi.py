@@ -221,3 +221,16 @@ def test_sample_tensors_are_checked_before_any_launch():
         args = {"logits": z, "uniform": u, **bad}
         with pytest.raises(error, match=text):
             fgd.sample(**args)
+
+
+def test_gradients_check_a_kept_transpose():
+    import torch
+
+    import paper_2606_22768_amd as fgd
+
+    def packed(rows, cols):
+        c, n = fgd.fgd_mx4_size(1, rows, cols)
+        return fgd.Mx4(torch.zeros(c, dtype=torch.uint8), torch.zeros(n, dtype=torch.uint8), None, rows, cols)
+
+    with pytest.raises(ValueError, match="rows of its transpose"):
+        fgd.mx4_linear_grads(torch.zeros(8, 16), packed(40, 8), packed(32, 16))
