@@ -570,7 +570,7 @@ bool launch_few(Left left, const uint8_t *wc, const uint8_t *ws, int64_t batch, 
 }
 
 // Which kernel a product takes.
-enum Shape { kFew1x1, kFew1x1Deep, kFew1x2, kFew2x2, kTiled128, kTiled256 };
+enum Shape { kFew1x1, kFew1x1Deep, kFew1x2Deep, kFew2x2, kFew2x2Deep, kTiled128, kTiled256 };
 
 Shape shape_of(int64_t batch, int64_t m, int64_t n, int64_t kt) {
     constexpr int64_t kCus = 256;
@@ -581,13 +581,18 @@ Shape shape_of(int64_t batch, int64_t m, int64_t n, int64_t kt) {
         // 3.3 times one of a 128 x 128 block (1.1 and 0.33 us, the card full).
         return 10 * ((small + kCus - 1) / kCus) >= 33 * ((large + kCus - 1) / kCus) ? kTiled256 : kTiled128;
     // Below that a compute unit's block is the smaller, the fewer there are,
-    // and its waves share out the columns.  Eight waves for four: 5.2 us for
-    // 5.9 at 1 x 2048 x 8192, but 31 for 23 at 1 x 128256 x 2048.  At 256 x
-    // 8192 x 8192 these take 22 us and 128 x 128 tiles 30; at 512 x 8192 x
-    // 8192, 39 and 34.
+    // and its waves share out the columns: eight where there are no more
+    // blocks than compute units (5.2 us for four waves' 5.9 at 1 x 2048 x 8192;
+    // 11.8 for 12.8 at 128 x 8192 x 8192), else four (23 for 31 at 1 x 128256 x
+    // 2048, 19.3 for 21.5 at 256 x 8192 x 8192).  Over few columns there is
+    // little to share, and 128 x 128 tiles are faster: 10.4 us for 16.3 at 777
+    // x 4100 x 1000, 10.3 for 15.6 at 64 x 50257 x 768; at 2048 x 1024 x 4096
+    // they take 13.6 for 12.0.
     if (blocks(32, 32) <= kCus) return kFew1x1Deep;
     if (m <= 32) return kFew1x1;
-    return blocks(64, 32) <= kCus ? kFew1x2 : kFew2x2;
+    if (blocks(64, 32) <= kCus) return kFew1x2Deep;
+    if (blocks(64, 64) <= kCus) return kFew2x2Deep;
+    return kt > 0 && kt <= 16 ? kTiled128 : kFew2x2;
 }
 
 template <typename T>
@@ -598,9 +603,11 @@ bool launch(Packed a, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64
             return launch_few<1, 1, 4, 4>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
         case kFew1x1Deep:
             return launch_few<1, 1, 8, 4>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
-        case kFew1x2:
+        case kFew1x2Deep:
             return launch_few<1, 2, 8, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
         case kFew2x2:
+            return launch_few<2, 2, 4, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew2x2Deep:
             return launch_few<2, 2, 8, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
         case kTiled128:
             return launch_tiled<2, 2, 1, 1>(a.codes, a.scales, wc, ws, batch, m, n, kt, out, batch_stride, row_stride,
