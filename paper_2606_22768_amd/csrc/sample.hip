@@ -189,9 +189,9 @@ struct Bins {
 };
 template <int TH>
 struct Shared : Bins<TH> {
-    u64 list[kRoom];  // key, then ~index: the larger is the earlier in the order
+    __attribute__((aligned(16))) u64 list[kRoom];  // key, then ~index: the larger is the earlier in the order
     u64 total;
-    uint32_t listed, last;
+    uint32_t listed, first, last;
     Wanted wanted;
 };
 
@@ -338,7 +338,9 @@ __device__ inline void find_wanted(Shared<TH> &s, const Settings &set, float u, 
     }
 }
 
-// Sorts list[0, n), n a power of two, from the largest.
+// Sorts list[0, n), n a power of two above 64, from the largest.  A wave's 64
+// pairs at a distance of up to 64 are 128 neighbours, which no other wave
+// touches: between such steps, a wave's own order is enough.
 template <int TH>
 __device__ inline void sort_list(u64 *list, int n) {
     for (int size = 2; size <= n; size <<= 1)
@@ -348,40 +350,53 @@ __device__ inline void sort_list(u64 *list, int n) {
                 const u64 x = list[a], y = list[b];
                 if ((x < y) == ((a & size) == 0)) list[a] = y, list[b] = x;
             }
-            __syncthreads();
+            const int next = step > 1 ? step >> 1 : size;
+            if (max(step, next) > 64)
+                __syncthreads();
+            else
+                asm volatile("" ::: "memory");
         }
 }
 
 // Finds the token among those collected, which are all of the wanted bins':
-// at most 64 of them, by a wave, each token against each.
+// at most one a thread, each against each.
 template <int TH>
 __device__ inline void finish_few(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
                                   int32_t *token, float *prob) {
-    const int lane = threadIdx.x;
-    const u64 own = lane < listed ? s.list[lane] : 0;
+    static_assert(4 * TH <= kRoom, "the pairs' room");
+    const int i = threadIdx.x;
+    const bool some = i < listed;
+    const u64 own = some ? s.list[i] : 0;
     const float t = scaled(logit_of(static_cast<uint32_t>(own >> 32)), top, set.c);
-    const uint32_t m = lane < listed ? mass_of(weight(t)) : 0, bin = lane < listed ? bin_of(t) : kBins;
+    const uint32_t m = some ? mass_of(weight(t)) : 0, bin = some ? bin_of(t) : kBins;
+    // Beside each other: a token, its bin and mass.
+    u64 *pairs = s.list + kRoom / 2;
+    if (some) pairs[2 * i] = own, pairs[2 * i + 1] = static_cast<u64>(bin) << 32 | m;
+    __syncthreads();
     u64 before = s.mass[bin];
     uint32_t rank = s.count[bin];
-    for (int j = 0; j < listed; ++j) {
-        const u64 other = static_cast<u64>(__builtin_amdgcn_readlane(static_cast<uint32_t>(own >> 32), j)) << 32 |
-                          static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(own), j));
-        const bool ahead = static_cast<uint32_t>(__builtin_amdgcn_readlane(bin, j)) == bin && other > own;
-        before += ahead ? static_cast<uint32_t>(__builtin_amdgcn_readlane(m, j)) : 0u;
-        rank += ahead;
+    if (i < (listed + 63) / 64 * 64) {  // the others' waves go on
+#pragma unroll 4
+        for (int j = 0; j < listed; ++j) {
+            const u64 other = pairs[2 * j], what = pairs[2 * j + 1];
+            const bool ahead = static_cast<uint32_t>(what >> 32) == bin && other > own;
+            before += ahead ? static_cast<uint32_t>(what) : 0u;
+            rank += ahead;
+        }
     }
-    auto through_of = [&](bool here) {  // the sum up to and with the one token where `here` holds
-        const int at = __ffsll(static_cast<u64>(__ballot(here))) - 1;
-        const u64 v = before + m;
-        return static_cast<u64>(__builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), at)) << 32 |
-               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<uint32_t>(v), at));
-    };
-    const bool some = lane < listed;
     u64 total = s.mass[kBins];
-    if (static_cast<uint32_t>(set.k) < s.count[kBins])
-        total = through_of(some && rank == static_cast<uint32_t>(set.k) - 1);
+    if (static_cast<uint32_t>(set.k) < s.count[kBins]) {
+        if (some && rank == static_cast<uint32_t>(set.k) - 1) s.total = before + m;
+        __syncthreads();
+        total = s.total;
+        __syncthreads();
+    }
     const u64 limit = nucleus(set.top_p, total);
-    if (limit < total) total = through_of(some && before < limit && limit <= before + m);
+    if (limit < total) {
+        if (some && before < limit && limit <= before + m) s.total = before + m;
+        __syncthreads();
+        total = s.total;
+    }
     total = min(total, kept);
     const u64 target = place(u, total);
     if (some && before <= target && target < before + m) {
@@ -394,8 +409,8 @@ __device__ inline void finish_few(Shared<TH> &s, const Settings &set, float u, u
 template <int TH>
 __device__ inline void finish(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
                               int32_t *token, float *prob) {
-    if (listed <= 64) {
-        if (threadIdx.x < 64) finish_few(s, set, u, kept, top, listed, token, prob);
+    if (listed <= TH) {
+        finish_few(s, set, u, kept, top, listed, token, prob);
         return;
     }
     int n = 1;
@@ -1088,10 +1103,21 @@ __global__ __launch_bounds__(kThreads, 4) void slice_token_kernel(const T *__res
     find_wanted(s, set, u, kept, top);
     __syncthreads();
     const int lo = blockIdx.x * slice, hi = min(vocab, lo + slice);
+    if (threadIdx.x == 0) s.listed = 0;
+    __syncthreads();
     slice_collect<TH>(row, lo, hi, s.wanted, [&](u64 v) {
-        const uint32_t at = atomicAdd(&space.listed, 1u);
-        if (at < kRoom) __hip_atomic_store(&space.list[at], v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        if (at < kRoom) s.list[at] = v;
     });
+    __syncthreads();
+    // One place for the block's, found at once: a place each costs a round
+    // trip to memory each time (22 us of 64 x 50257 for 18).
+    const uint32_t own = s.listed;
+    if (threadIdx.x == 0) s.first = own ? atomicAdd(&space.listed, own) : 0;
+    __syncthreads();
+    const uint32_t base = s.first;
+    for (uint32_t i = threadIdx.x; i < min(own, static_cast<uint32_t>(kRoom)) && base + i < kRoom; i += TH)
+        __hip_atomic_store(&space.list[base + i], s.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     // The last of the row's blocks finds the token.  The tokens are stored
     // and read at the device's scope, past the dies' own L2s, and a wave
     // counts its block only when its stores are acknowledged; a fence would
