@@ -570,7 +570,7 @@ bool launch_few(Left left, const uint8_t *wc, const uint8_t *ws, int64_t batch, 
 }
 
 // Which kernel a product takes.
-enum Shape { kFew1x1, kFew1x1Deep, kFew1x2Deep, kFew2x2, kFew2x2Deep, kTiled128, kTiled256 };
+enum Shape { kFew2x1, kFew2x1Deep, kFew1x1Deep, kFew1x2Deep, kFew2x2, kFew2x2Deep, kTiled128, kTiled256 };
 
 Shape shape_of(int64_t batch, int64_t m, int64_t n, int64_t kt) {
     constexpr int64_t kCus = 256;
@@ -583,13 +583,14 @@ Shape shape_of(int64_t batch, int64_t m, int64_t n, int64_t kt) {
     // Below that a compute unit's block is the smaller, the fewer there are,
     // and its waves share out the columns: eight where there are no more
     // blocks than compute units (5.2 us for four waves' 5.9 at 1 x 2048 x 8192;
-    // 11.8 for 12.8 at 128 x 8192 x 8192), else four (23 for 31 at 1 x 128256 x
-    // 2048, 19.3 for 21.5 at 256 x 8192 x 8192).  Over few columns there is
+    // 11.7 for 14.2 at 1 x 9000 x 8192; 11.8 for 12.8 at 128 x 8192 x 8192),
+    // else four (17.0 for 20.2 at 16 x 128256 x 1024, 19.3 for 21.5 at 256 x
+    // 8192 x 8192; blocks of 32 rows of w for 64: 19.6).  Over few columns there is
     // little to share, and 128 x 128 tiles are faster: 10.4 us for 16.3 at 777
     // x 4100 x 1000, 10.3 for 15.6 at 64 x 50257 x 768; at 2048 x 1024 x 4096
     // they take 13.6 for 12.0.
     if (blocks(32, 32) <= kCus) return kFew1x1Deep;
-    if (m <= 32) return kFew1x1;
+    if (m <= 32) return blocks(32, 64) <= kCus ? kFew2x1Deep : kFew2x1;
     if (blocks(64, 32) <= kCus) return kFew1x2Deep;
     if (blocks(64, 64) <= kCus) return kFew2x2Deep;
     return kt > 0 && kt <= 16 ? kTiled128 : kFew2x2;
@@ -599,8 +600,10 @@ template <typename T>
 bool launch(Packed a, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m, int64_t n, int64_t kt, T *out,
             int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
     switch (shape_of(batch, m, n, kt)) {
-        case kFew1x1:
-            return launch_few<1, 1, 4, 4>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew2x1:
+            return launch_few<2, 1, 4, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew2x1Deep:
+            return launch_few<2, 1, 8, 2>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
         case kFew1x1Deep:
             return launch_few<1, 1, 8, 4>(a, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
         case kFew1x2Deep:
@@ -621,9 +624,14 @@ bool launch(Packed a, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64
 template <typename T, typename X>
 bool launch_dense(Dense<X> x, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m, int64_t n, int64_t kt,
                   T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
-    if (shape_of(batch, m, n, kt) == kFew1x1)
-        return launch_few<1, 1, 4, 4>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
-    return launch_few<1, 1, 8, 4>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+    switch (shape_of(batch, m, n, kt)) {
+        case kFew2x1:
+            return launch_few<2, 1, 4, 2>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        case kFew2x1Deep:
+            return launch_few<2, 1, 8, 2>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+        default:
+            return launch_few<1, 1, 8, 4>(x, wc, ws, batch, m, n, kt, out, batch_stride, row_stride, stream);
+    }
 }
 
 }  // namespace
@@ -645,7 +653,9 @@ bool mx4_linear_fuses(int64_t batch, int64_t m, int64_t n, int64_t k) {
     if (batch == 0 || m == 0 || n == 0 || k == 0 || m > 32) return false;
     const int64_t kt = mx4_col_tiles(k);
     const Shape shape = shape_of(batch, m, n, kt);
-    return (shape == kFew1x1 && m * 4 * kt <= 256) || (shape == kFew1x1Deep && m * 4 * kt <= 512);
+    // A thread quantises a block of x at most.
+    return (shape == kFew2x1 && m * 4 * kt <= 256) ||
+           ((shape == kFew2x1Deep || shape == kFew1x1Deep) && m * 4 * kt <= 512);
 }
 
 bool mx4_linear_launch(const void *x, bool x_bf16, int64_t x_batch_stride, int64_t x_row_stride, const void *w_codes,

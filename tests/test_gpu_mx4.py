@@ -361,3 +361,30 @@ def test_what_a_call_allocates_belongs_to_its_stream(env):
         torch.cuda.synchronize()
         assert all(bool((t == 0xA5).all()) for t in mine)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("bmnk", [(1, 7, 17001, 300), (1, 30, 17001, 1300), (1, 2, 40000, 2048), (1, 1, 40001, 96),
+                                  (1, 1100, 17000, 300), (1, 1100, 17000, 640), (1, 2100, 33000, 100),
+                                  (1, 2100, 33000, 300), (1, 2100, 33000, 385), (3, 300, 9000, 200),
+                                  (2, 130, 40000, 129)], ids=str)
+def test_products_of_many_blocks(env, bmnk):
+    """More blocks of the result than the card holds at once, whole ones and
+    the matrix's edges, over even and odd numbers of column tiles."""
+    fgd, torch = env
+    b, m, n, k = bmnk
+    print(f"[mx4] many blocks {bmnk}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(sum(bmnk))
+    x = torch.randn(b, m, k, device="cuda", generator=g).bfloat16()
+    w = torch.randn(b, n, k, device="cuda", generator=g).bfloat16()
+    a4, w4 = fgd.mx4_quantize(x), fgd.mx4_quantize(w)
+    y, y16 = fgd.mx4_matmul(a4, w4, "f32"), fgd.mx4_matmul(a4, w4)
+    assert torch.equal(y16, y.bfloat16())
+    lines = torch.full((b, m, n + 3), 7.0, dtype=torch.float32, device="cuda")
+    assert torch.equal(fgd.mx4_linear(x, w4, out=lines[:, :, 1:n + 1]), y)
+    lines[:, :, 1:n + 1] = 7.0
+    assert bool((lines == 7.0).all())
+    for i in range(b):
+        p = torch.from_numpy(ref.mx4_values(_host(x[i]))).cuda()
+        q = torch.from_numpy(ref.mx4_values(_host(w[i]))).cuda().T.contiguous()
+        off = (y[i].double() - p @ q).abs_()
+        assert bool((off <= (k / 128 + 128) * 2.0 ** -24 * (p.abs() @ q.abs())).all())
