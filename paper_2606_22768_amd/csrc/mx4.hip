@@ -17,7 +17,8 @@ template <typename F>
 __device__ inline void for_tiles(int64_t row_tiles, int64_t col_tiles, int64_t batch, F f) {
     for (int64_t b = blockIdx.z; b < batch; b += gridDim.z)
         for (int64_t r = blockIdx.y; r < row_tiles; r += gridDim.y)
-            f((b * row_tiles + r) * col_tiles + blockIdx.x, b, r, static_cast<int64_t>(blockIdx.x));
+            for (int64_t k = blockIdx.x; k < col_tiles; k += gridDim.x)
+                f((b * row_tiles + r) * col_tiles + k, b, r, k);
 }
 
 // Rows contiguous: a 64 x 128 tile per block of 256 threads, a thread per
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restri
 }
 
 dim3 grid_for(int64_t batch, int64_t row_tiles, int64_t col_tiles) {
-    return dim3(static_cast<unsigned>(col_tiles), static_cast<unsigned>(std::min<int64_t>(row_tiles, 65535)),
+    return dim3(static_cast<unsigned>(std::min<int64_t>(col_tiles, 1 << 22)), static_cast<unsigned>(std::min<int64_t>(row_tiles, 65535)),
                 static_cast<unsigned>(std::min<int64_t>(batch, 65535)));
 }
 
@@ -163,7 +164,6 @@ bool mx4_quantize_launch(const void *x, bool bf16, int64_t batch, int64_t rows, 
                          int64_t row_stride, int64_t col_stride, void *codes, void *scales, hipStream_t stream) {
     const int64_t rt = mx4_row_tiles(rows), kt = mx4_col_tiles(cols);
     if (batch == 0 || rt == 0 || kt == 0) return true;
-    if (kt > INT32_MAX) return false;
     auto *c = static_cast<uint8_t *>(codes), *s = static_cast<uint8_t *>(scales);
     if (bf16)
         quantize(static_cast<const uint16_t *>(x), batch, rows, cols, rt, kt, batch_stride, row_stride, col_stride, c, s,
@@ -178,7 +178,6 @@ bool mx4_dequantize_launch(const void *codes, const void *scales, int64_t batch,
                            void *out, bool bf16, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
     const int64_t rt = mx4_row_tiles(rows), kt = mx4_col_tiles(cols);
     if (batch == 0 || rt == 0 || kt == 0) return true;
-    if (kt > INT32_MAX) return false;
     auto *c = static_cast<const uint8_t *>(codes), *s = static_cast<const uint8_t *>(scales);
     if (bf16)
         dequantize_kernel<<<grid_for(batch, rt, kt), 256, 0, stream>>>(c, s, batch, rows, cols, rt, kt,

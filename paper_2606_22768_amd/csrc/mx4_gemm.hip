@@ -178,7 +178,7 @@ template <int NW, int NA, int WAVES, int AHEAD, typename T, typename Left>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(Left left, const uint8_t *__restrict__ w_codes,
                                                          const uint8_t *__restrict__ w_scales, int64_t m, int64_t n,
                                                          int kt, int64_t n_blocks, int64_t m_blocks,
-                                                         T *__restrict__ out, int64_t batch_stride,
+                                                         int64_t first_batch, T *__restrict__ out, int64_t batch_stride,
                                                          int64_t row_stride) {
     constexpr bool kDense = !std::is_same<Left, Packed>::value;
     static_assert(!kDense || NA == 1, "dense rows: of one fragment");
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Left left, const uint8_
     __shared__ uint8_t x_scales[kDense ? 64 * WAVES : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t w_tiles = (n + 63) / 64, items = n_blocks * m_blocks;
-    const int64_t b = blockIdx.y;
+    const int64_t b = first_batch + blockIdx.y;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t nb = item % n_blocks, mb = item / n_blocks;
         const int wh = NW == 2 ? 0 : nb & 1, ah = NA == 2 ? 0 : mb & 1;  // the half of a tile, where it is one
@@ -558,14 +558,17 @@ template <int NW, int NA, int WAVES, int AHEAD, typename T, typename Left>
 bool launch_few(Left left, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m, int64_t n, int64_t kt,
                 T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
     const int64_t nb = (n + 32 * NW - 1) / (32 * NW), mb = (m + 32 * NA - 1) / (32 * NA);
-    if (nb * mb > INT32_MAX || batch > 65535 || kt > INT32_MAX / 64) return false;
+    if (kt > INT32_MAX / 64) return false;
     // Dense rows are quantised once a block, so there are two blocks a compute
     // unit, which go round (768 blocks: 34 us at 1 x 128256 x 2048, 512: 28,
     // 256: 36).
-    const int64_t most = std::is_same<Left, Packed>::value ? nb * mb : std::max<int64_t>(1, 512 / batch);
-    const dim3 grid(static_cast<unsigned>(std::min(nb * mb, most)), static_cast<unsigned>(batch));
-    few_kernel<NW, NA, WAVES, AHEAD, T, Left><<<grid, 64 * WAVES, 0, stream>>>(
-        left, wc, ws, m, n, static_cast<int>(kt), nb, mb, out, batch_stride, row_stride);
+    const int64_t most = std::is_same<Left, Packed>::value ? 1 << 20 : std::max<int64_t>(1, 512 / batch);
+    for (int64_t b = 0; b < batch; b += 65535) {  // a grid's most
+        const dim3 grid(static_cast<unsigned>(std::min(nb * mb, most)),
+                        static_cast<unsigned>(std::min<int64_t>(batch - b, 65535)));
+        few_kernel<NW, NA, WAVES, AHEAD, T, Left><<<grid, 64 * WAVES, 0, stream>>>(
+            left, wc, ws, m, n, static_cast<int>(kt), nb, mb, b, out, batch_stride, row_stride);
+    }
     return hipGetLastError() == hipSuccess;
 }
 

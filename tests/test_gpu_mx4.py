@@ -388,3 +388,22 @@ def test_products_of_many_blocks(env, bmnk):
         q = torch.from_numpy(ref.mx4_values(_host(w[i]))).cuda().T.contiguous()
         off = (y[i].double() - p @ q).abs_()
         assert bool((off <= (k / 128 + 128) * 2.0 ** -24 * (p.abs() @ q.abs())).all())
+
+
+def test_more_matrices_than_a_grid_holds(env):
+    """A batch of 70000 tiny matrices: quantised, read back, multiplied."""
+    fgd, torch = env
+    b, m, n, k = 70000, 2, 3, 40
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(b, m, k, device="cuda", generator=g)
+    w = torch.randn(b, n, k, device="cuda", generator=g)
+    x4, w4 = fgd.mx4_quantize(x), fgd.mx4_quantize(w)
+    p, q = fgd.mx4_dequantize(x4), fgd.mx4_dequantize(w4)
+    for i in (0, 1, 65534, 65535, 65536, b - 1):
+        assert np.array_equal(_host(p[i]), ref.mx4_values(_host(x[i])))
+        assert np.array_equal(_host(q[i]), ref.mx4_values(_host(w[i])))
+    y, p, q = fgd.mx4_matmul(x4, w4, "f32"), p.double(), q.double()
+    assert torch.equal(fgd.mx4_linear(x, w4), y)
+    terms = p[:, :, None, :] * q[:, None, :, :]
+    off = (y.double() - terms.sum(-1)).abs()
+    assert bool((off <= (k / 128 + 128) * 2.0 ** -24 * terms.abs().sum(-1)).all())
