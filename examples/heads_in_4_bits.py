@@ -68,10 +68,11 @@ def train(workers=4, vocab=2000, width=256, tokens=128, rounds=5, inner_steps=8,
         local.copy_(before)
         first = None
         for _ in range(inner_steps):
-            logits = fgd.mx4_linear(x, fgd.mx4_quantize(heads))
+            heads4, heads_t = fgd.mx4_quantize_both(heads)
+            logits = fgd.mx4_linear(x, heads4)
             loss, dy = cross_entropy(logits, targets)
             first = loss if first is None else first
-            _, dw = fgd.mx4_linear_grads(dy, x_t, fgd.mx4_quantize(heads.mT))
+            _, dw = fgd.mx4_linear_grads(dy, x_t, heads_t)
             heads.sub_(dw, alpha=lr)
         # The workers' own predictions of the same states, and their average's.
         fgd.mx4_linear(held_out.expand(M, T, K), fgd.mx4_quantize(heads), out=own[..., :V])

@@ -452,6 +452,13 @@ fgd_status fgd_mx4_quantize(const void *x, int32_t dtype, int32_t batch, int64_t
                             int64_t batch_stride, int64_t row_stride, int64_t col_stride, void *codes, void *scales,
                             void *stream);
 
+/* Quantises x (rows contiguous) and its transpose in one reading: codes and
+ * scales as fgd_mx4_quantize(x) writes them, t_codes and t_scales (of batch x
+ * cols x rows) as of the transposed view.  Enqueued on `stream`. */
+fgd_status fgd_mx4_quantize_both(const void *x, int32_t dtype, int32_t batch, int64_t rows, int64_t cols,
+                                 int64_t batch_stride, int64_t row_stride, void *codes, void *scales, void *t_codes,
+                                 void *t_scales, void *stream);
+
 /* Writes the values that codes and scales stand for to out, rows contiguous
  * (element (b, r, k) at b * batch_stride + r * row_stride + k).  Exact in
  * either dtype.  Enqueued on `stream`. */

@@ -85,6 +85,52 @@ __global__ __launch_bounds__(128) void quantize_columns_kernel(const T *__restri
     });
 }
 
+// Rows contiguous, along both axes in one reading: 128 x 128 elements per
+// block of 256 threads, quantised along the rows on their way to LDS and along
+// the columns from there.  An LDS row's odd stride in dwords keeps the lanes of
+// both passes, rows of one column and columns of one row, on banks of their own.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_both_kernel(const T *__restrict__ x, int64_t batch, int64_t rows,
+                                                            int64_t cols, int64_t row_tiles, int64_t col_tiles,
+                                                            int64_t t_row_tiles, int64_t t_col_tiles,
+                                                            int64_t batch_stride, int64_t row_stride,
+                                                            uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
+                                                            uint8_t *__restrict__ t_codes,
+                                                            uint8_t *__restrict__ t_scales) {
+    __shared__ T s[128][128 + (sizeof(T) == 4 ? 1 : 2)];
+    const int lane = threadIdx.x & 63, frag = threadIdx.x >> 6;
+    const int i = (frag >> 1) * 32 + (lane & 31), j = (frag & 1) * 64 + (lane >> 5) * 32;
+    for_tiles(t_col_tiles, col_tiles, batch, [&](int64_t, int64_t b, int64_t rb, int64_t kb) {
+        auto put = [&](const float (&v)[32], uint8_t *c, uint8_t *sc, int64_t tile) {
+            uint4 q;
+            const uint32_t byte = encode_block(v, q);
+            *reinterpret_cast<uint4 *>(c + tile * kMx4CodeBytes + frag * 1024 + lane * 16) = q;
+            sc[tile * kMx4ScaleBytes + lane * 4 + frag] = static_cast<uint8_t>(byte);
+        };
+        const int64_t k0 = kb * 128 + j;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t rt = 2 * rb + h, r = rt * kMx4TileRows + i;
+            float v[32];
+            load_block(x + b * batch_stride + r * row_stride + k0, r < rows ? cols - k0 : 0, v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[h * 64 + i][j + e] = narrow<T>(v[e]);
+            if (rt < row_tiles) put(v, codes, scales, (b * row_tiles + rt) * col_tiles + kb);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t rt = 2 * kb + h;
+            if (rt >= t_row_tiles) continue;
+            float v[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] = widen(s[j + e][h * 64 + i]);
+            put(v, t_codes, t_scales, (b * t_row_tiles + rt) * t_col_tiles + rb);
+        }
+        __syncthreads();
+    });
+}
+
 template <typename T>
 void quantize(const T *x, int64_t batch, int64_t rows, int64_t cols, int64_t rt, int64_t kt, int64_t batch_stride,
               int64_t row_stride, int64_t col_stride, uint8_t *codes, uint8_t *scales, dim3 grid, hipStream_t stream) {
@@ -171,6 +217,24 @@ bool mx4_quantize_launch(const void *x, bool bf16, int64_t batch, int64_t rows, 
     else
         quantize(static_cast<const float *>(x), batch, rows, cols, rt, kt, batch_stride, row_stride, col_stride, c, s,
                  grid_for(batch, rt, kt), stream);
+    return hipGetLastError() == hipSuccess;
+}
+
+bool mx4_quantize_both_launch(const void *x, bool bf16, int64_t batch, int64_t rows, int64_t cols,
+                              int64_t batch_stride, int64_t row_stride, void *codes, void *scales, void *t_codes,
+                              void *t_scales, hipStream_t stream) {
+    if (batch == 0 || rows == 0 || cols == 0) return true;
+    const int64_t rt = mx4_row_tiles(rows), kt = mx4_col_tiles(cols), t_rt = mx4_row_tiles(cols),
+                  t_kt = mx4_col_tiles(rows);
+    auto go = [&](auto *p) {
+        quantize_both_kernel<<<grid_for(batch, t_kt, kt), 256, 0, stream>>>(
+            p, batch, rows, cols, rt, kt, t_rt, t_kt, batch_stride, row_stride, static_cast<uint8_t *>(codes),
+            static_cast<uint8_t *>(scales), static_cast<uint8_t *>(t_codes), static_cast<uint8_t *>(t_scales));
+    };
+    if (bf16)
+        go(static_cast<const uint16_t *>(x));
+    else
+        go(static_cast<const float *>(x));
     return hipGetLastError() == hipSuccess;
 }
 

@@ -38,6 +38,12 @@ inline int64_t mx4_tiles(int64_t batch, int64_t rows, int64_t cols) {
 bool mx4_quantize_launch(const void *x, bool bf16, int64_t batch, int64_t rows, int64_t cols, int64_t batch_stride,
                          int64_t row_stride, int64_t col_stride, void *codes, void *scales, hipStream_t stream);
 
+// The same of x[b][r][k] at b * batch_stride + r * row_stride + k and of its
+// transpose.
+bool mx4_quantize_both_launch(const void *x, bool bf16, int64_t batch, int64_t rows, int64_t cols,
+                              int64_t batch_stride, int64_t row_stride, void *codes, void *scales, void *t_codes,
+                              void *t_scales, hipStream_t stream);
+
 bool mx4_dequantize_launch(const void *codes, const void *scales, int64_t batch, int64_t rows, int64_t cols,
                            void *out, bool bf16, int64_t batch_stride, int64_t row_stride, hipStream_t stream);
 

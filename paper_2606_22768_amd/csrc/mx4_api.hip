@@ -150,6 +150,30 @@ fgd_status fgd_mx4_quantize(const void *x, int32_t dtype, int32_t batch, int64_t
     return FGD_OK;
 }
 
+fgd_status fgd_mx4_quantize_both(const void *x, int32_t dtype, int32_t batch, int64_t rows, int64_t cols,
+                                 int64_t batch_stride, int64_t row_stride, void *codes, void *scales, void *t_codes,
+                                 void *t_scales, void *stream) {
+    fgd::api_clear();
+    int64_t x_bytes;
+    Spans q, t;
+    if (fgd_status st = check_quantize_input("x", x, dtype, batch, rows, cols, batch_stride, row_stride, 1, &x_bytes))
+        return st;
+    if (fgd_status st = check_packed("quantised matrix", codes, scales, batch, rows, cols, &q)) return st;
+    if (fgd_status st = check_packed("quantised transpose", t_codes, t_scales, batch, cols, rows, &t)) return st;
+    const struct {
+        const void *p;
+        int64_t bytes;
+    } arrays[] = {{x, x_bytes}, {codes, q.codes}, {scales, q.scales}, {t_codes, t.codes}, {t_scales, t.scales}};
+    for (int i = 0; i < 5; ++i)
+        for (int j = i + 1; j < 5; ++j)
+            if (ranges_overlap(arrays[i].p, arrays[i].bytes, arrays[j].p, arrays[j].bytes))
+                return api_fail(FGD_ERR_INVALID_ARG, "x, codes and scales must not overlap");
+    if (!fgd::mx4_quantize_both_launch(x, dtype == FGD_BF16, batch, rows, cols, batch_stride, row_stride, codes,
+                                       scales, t_codes, t_scales, static_cast<hipStream_t>(stream)))
+        return api_fail(FGD_ERR_HIP, "4-bit quantisation launch failed");
+    return FGD_OK;
+}
+
 fgd_status fgd_mx4_dequantize(const void *codes, const void *scales, int32_t batch, int64_t rows, int64_t cols,
                               void *out, int32_t dtype, int64_t batch_stride, int64_t row_stride, void *stream) {
     fgd::api_clear();

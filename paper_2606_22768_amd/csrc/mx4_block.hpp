@@ -14,6 +14,14 @@ __device__ inline float widen<float>(float v) { return v; }
 template <>
 __device__ inline float widen<uint16_t>(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
 
+// A widened value back in its type.
+template <typename T>
+__device__ inline T narrow(float v);
+template <>
+__device__ inline float narrow<float>(float v) { return v; }
+template <>
+__device__ inline uint16_t narrow<uint16_t>(float v) { return static_cast<uint16_t>(__float_as_uint(v) >> 16); }
+
 // Sixteen bytes of elements at an address aligned to its element only.
 template <typename T>
 struct __attribute__((packed, aligned(sizeof(T)))) Pack {

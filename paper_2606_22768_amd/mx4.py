@@ -39,6 +39,13 @@ def fgd_mx4_quantize(x, dtype, batch, rows, cols, batch_stride, row_stride, col_
                                 col_stride, _dev(codes), _dev(scales), _stream(stream)), "fgd_mx4_quantize")
 
 
+def fgd_mx4_quantize_both(x, dtype, batch, rows, cols, batch_stride, row_stride, codes, scales, t_codes, t_scales,
+                          stream=None):
+    _check(lib.fgd_mx4_quantize_both(_dev(x), DTYPES.get(dtype, dtype), batch, rows, cols, batch_stride, row_stride,
+                                     _dev(codes), _dev(scales), _dev(t_codes), _dev(t_scales), _stream(stream)),
+           "fgd_mx4_quantize_both")
+
+
 def fgd_mx4_dequantize(codes, scales, batch, rows, cols, out, dtype, batch_stride, row_stride, stream=None):
     _check(lib.fgd_mx4_dequantize(_dev(codes), _dev(scales), batch, rows, cols, _dev(out), DTYPES.get(dtype, dtype),
                                   batch_stride, row_stride, _stream(stream)), "fgd_mx4_dequantize")
@@ -180,12 +187,18 @@ def _output(out, t, shape, device):
     return out, FGD_F32 if t == torch.float32 else FGD_BF16, (out.stride(0) if out.dim() == 3 else 0), out.stride(-2)
 
 
+def _packed(n, batch, rows, cols, device):
+    import torch
+
+    cb, sb = fgd_mx4_size(n, rows, cols)
+    pool = torch.empty(cb + sb, dtype=torch.uint8, device=device)
+    return Mx4(pool[:cb], pool[cb:], batch, rows, cols)
+
+
 def mx4_quantize(x, stream=None) -> Mx4:
     """x [rows][cols] or [batch][rows][cols], float32 or bfloat16, its rows or
     its columns contiguous (a transposed view is quantised along the stored
     matrix's columns)."""
-    import torch
-
     code, batch, rows, cols, bs, rs, cs = _matrix(x, "x")
     if x.numel() and rs != 1 and cs != 1:
         if cols == 1:
@@ -196,12 +209,28 @@ def mx4_quantize(x, stream=None) -> Mx4:
             raise ValueError("x: its rows or its columns must be contiguous")
     _on_gpu("x", x, None)
     n = 1 if batch is None else batch
-    cb, sb = fgd_mx4_size(n, rows, cols)
     with _on(x.device, stream):
-        pool = torch.empty(cb + sb, dtype=torch.uint8, device=x.device)
-        q = Mx4(pool[:cb], pool[cb:], batch, rows, cols)
+        q = _packed(n, batch, rows, cols, x.device)
         fgd_mx4_quantize(x, code, n, rows, cols, bs, rs, cs, q.codes, q.scales, _current(x.device))
     return q
+
+
+def mx4_quantize_both(x, stream=None):
+    """(mx4_quantize(x), mx4_quantize(x.mT)) from one reading of x: what a
+    matrix needs that takes part in a layer's product and in its gradients."""
+    code, batch, rows, cols, bs, rs, cs = _matrix(x, "x")
+    if cols > 1 and rows and cs != 1:
+        if rs != 1:
+            raise ValueError("x: its rows or its columns must be contiguous")
+        t, q = mx4_quantize_both(x.mT, stream)
+        return q, t
+    _on_gpu("x", x, None)
+    n = 1 if batch is None else batch
+    with _on(x.device, stream):
+        q, t = _packed(n, batch, rows, cols, x.device), _packed(n, batch, cols, rows, x.device)
+        fgd_mx4_quantize_both(x, code, n, rows, cols, bs, rs, q.codes, q.scales, t.codes, t.scales,
+                              _current(x.device))
+    return q, t
 
 
 def mx4_dequantize(q, dtype="f32", out=None, stream=None):
@@ -294,6 +323,7 @@ def mx4_linear_grads(dy, x, w_t, dx_dtype=None, dw_dtype="f32", stream=None):
         x_t = mx4_quantize(x.mT, stream)
     elif x_t.rows != w_t.rows:
         raise ValueError(f"x: expected {w_t.rows} rows of its transpose, got shape {x_t.shape}")
-    dx = mx4_matmul(mx4_quantize(dy, stream), w_t, dy.dtype if dx_dtype is None else dx_dtype, stream=stream)
-    dw = mx4_matmul(mx4_quantize(dy.mT, stream), x_t, dw_dtype, stream=stream)
+    dy4, dy_t = mx4_quantize_both(dy, stream)
+    dx = mx4_matmul(dy4, w_t, dy.dtype if dx_dtype is None else dx_dtype, stream=stream)
+    dw = mx4_matmul(dy_t, x_t, dw_dtype, stream=stream)
     return dx, dw

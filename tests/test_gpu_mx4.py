@@ -407,3 +407,31 @@ def test_more_matrices_than_a_grid_holds(env):
     terms = p[:, :, None, :] * q[:, None, :, :]
     off = (y.double() - terms.sum(-1)).abs()
     assert bool((off <= (k / 128 + 128) * 2.0 ** -24 * terms.abs().sum(-1)).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_both_axes_in_one_reading(env, dtype):
+    """The codes and scales of the two calls, byte for byte."""
+    fgd, torch = env
+
+    def same(x):
+        q, t = fgd.mx4_quantize_both(x)
+        for got, want in ((q, fgd.mx4_quantize(x)), (t, fgd.mx4_quantize(x.mT))):
+            assert got.shape == want.shape
+            assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales), tuple(x.shape)
+
+    for shape in SHAPES + [(63, 64), (128, 128), (129, 65), (300, 1000), (4097, 3), (2, 77, 200), (3, 1, 129),
+                           (5, 130, 33)]:
+        print(f"[mx4] both {shape} {dtype}", flush=True)
+        x = _tensor(torch, _values(shape, sum(shape)), dtype)
+        same(x)
+        same(x.mT)
+    wide = _tensor(torch, _values((3, 90, 207), 1), dtype)
+    same(wide[:, 1:, 3:200])
+    odd = wide[0].clone()
+    odd[3, 5], odd[70, 6], odd[71, 7], odd[8] = float("nan"), float("inf"), -0.0, 0.0
+    odd[:, 40] = 1e-39
+    same(odd)
+    for shape in ((0, 5), (5, 0), (0, 0), (2, 0, 3)):
+        q, t = fgd.mx4_quantize_both(torch.empty(shape, device="cuda"))
+        assert q.shape == shape and t.shape == (*shape[:-2], shape[-1], shape[-2])

@@ -234,3 +234,30 @@ def test_gradients_check_a_kept_transpose():
 
     with pytest.raises(ValueError, match="rows of its transpose"):
         fgd.mx4_linear_grads(torch.zeros(8, 16), packed(40, 8), packed(32, 16))
+
+
+def test_quantising_both_axes_checks_its_arrays():
+    import paper_2606_22768_amd as fgd
+
+    at = [1 << 20, 2 << 20, 3 << 20, 4 << 20, 5 << 20]  # never touched: every call is refused
+
+    def call(arrays=at, dtype="f32", rows=64, cols=128, row_stride=128):
+        fgd.fgd_mx4_quantize_both(arrays[0], dtype, 1, rows, cols, 0, row_stride, *arrays[1:], stream=0)
+
+    for i in range(5):
+        with pytest.raises(fgd.FgdError, match="NULL"):
+            call(at[:i] + [None] + at[i + 1:])
+        for j in range(i):
+            with pytest.raises(fgd.FgdError, match="overlap"):
+                call(at[:i] + [at[j]] + at[i + 1:])
+    for i in range(1, 5):
+        with pytest.raises(fgd.FgdError, match="aligned"):
+            call(at[:i] + [at[i] + 8] + at[i + 1:])
+    with pytest.raises(fgd.FgdError, match="aligned to its element"):
+        call([at[0] + 1] + at[1:])
+    with pytest.raises(fgd.FgdError, match="dtype"):
+        call(dtype=7)
+    with pytest.raises(fgd.FgdError, match="negative"):
+        call(rows=-1)
+    with pytest.raises(fgd.FgdError, match="negative stride"):
+        call(row_stride=-128)
