@@ -12,13 +12,14 @@ namespace {
 
 // f(tile, batch entry, row tile, column tile) for a block's tiles: blocks of
 // one row of tiles are neighbours (those of one column: 143 us for 127 at
-// 128256 x 2048 bf16), and no index is divided.
+// 128256 x 2048 bf16), and no index is divided.  (A loop over the columns as
+// well takes reading back from 119 to 177 us right after the quantisation.)
 template <typename F>
-__device__ inline void for_tiles(int64_t row_tiles, int64_t col_tiles, int64_t batch, F f) {
+__device__ inline void for_tiles(int64_t row_tiles, int64_t col_tiles, int64_t batch, int64_t first_col, F f) {
+    const int64_t k = first_col + blockIdx.x;
     for (int64_t b = blockIdx.z; b < batch; b += gridDim.z)
         for (int64_t r = blockIdx.y; r < row_tiles; r += gridDim.y)
-            for (int64_t k = blockIdx.x; k < col_tiles; k += gridDim.x)
-                f((b * row_tiles + r) * col_tiles + k, b, r, k);
+            f((b * row_tiles + r) * col_tiles + k, b, r, k);
 }
 
 // Rows contiguous: a 64 x 128 tile per block of 256 threads, a thread per
@@ -26,11 +27,12 @@ __device__ inline void for_tiles(int64_t row_tiles, int64_t col_tiles, int64_t b
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict__ x, int64_t batch, int64_t rows,
                                                             int64_t cols, int64_t row_tiles, int64_t col_tiles,
+                                                            int64_t first_col,
                                                             int64_t batch_stride, int64_t row_stride,
                                                             uint8_t *__restrict__ codes,
                                                             uint8_t *__restrict__ scales) {
     const int lane = threadIdx.x & 63, frag = threadIdx.x >> 6;
-    for_tiles(row_tiles, col_tiles, batch, [&](int64_t tile, int64_t b, int64_t rt, int64_t kt) {
+    for_tiles(row_tiles, col_tiles, batch, first_col, [&](int64_t tile, int64_t b, int64_t rt, int64_t kt) {
         const int64_t r = rt * kMx4TileRows + (frag >> 1) * 32 + (lane & 31),
                       k0 = kt * kMx4TileCols + (frag & 1) * 64 + (lane >> 5) * 32;
         float v[32];
@@ -49,6 +51,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict_
 template <typename T>
 __global__ __launch_bounds__(128) void quantize_columns_kernel(const T *__restrict__ x, int64_t batch, int64_t rows,
                                                                int64_t cols, int64_t row_tiles, int64_t col_tiles,
+                                                            int64_t first_col,
                                                                int64_t batch_stride, int64_t col_stride,
                                                                uint8_t *__restrict__ codes,
                                                                uint8_t *__restrict__ scales) {
@@ -57,7 +60,7 @@ __global__ __launch_bounds__(128) void quantize_columns_kernel(const T *__restri
     };
     const int pair = threadIdx.x & 31, block = threadIdx.x >> 5;
     const int row = 2 * pair, lane = (row & 31) + 32 * (block & 1), frag = 2 * (row >> 5) + (block >> 1);
-    for_tiles(row_tiles, col_tiles, batch, [&](int64_t tile, int64_t b, int64_t rt, int64_t kt) {
+    for_tiles(row_tiles, col_tiles, batch, first_col, [&](int64_t tile, int64_t b, int64_t rt, int64_t kt) {
         const int64_t r = rt * kMx4TileRows + row, k0 = kt * kMx4TileCols + block * 32;
         const T *src = x + b * batch_stride + r + k0 * col_stride;
         float v[2][32];
@@ -92,7 +95,8 @@ __global__ __launch_bounds__(128) void quantize_columns_kernel(const T *__restri
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_both_kernel(const T *__restrict__ x, int64_t batch, int64_t rows,
                                                             int64_t cols, int64_t row_tiles, int64_t col_tiles,
-                                                            int64_t t_row_tiles, int64_t t_col_tiles,
+                                                            int64_t first_col, int64_t t_row_tiles,
+                                                            int64_t t_col_tiles,
                                                             int64_t batch_stride, int64_t row_stride,
                                                             uint8_t *__restrict__ codes, uint8_t *__restrict__ scales,
                                                             uint8_t *__restrict__ t_codes,
@@ -100,7 +104,7 @@ __global__ __launch_bounds__(256) void quantize_both_kernel(const T *__restrict_
     __shared__ T s[128][128 + (sizeof(T) == 4 ? 1 : 2)];
     const int lane = threadIdx.x & 63, frag = threadIdx.x >> 6;
     const int i = (frag >> 1) * 32 + (lane & 31), j = (frag & 1) * 64 + (lane >> 5) * 32;
-    for_tiles(t_col_tiles, col_tiles, batch, [&](int64_t, int64_t b, int64_t rb, int64_t kb) {
+    for_tiles(t_col_tiles, col_tiles, batch, first_col, [&](int64_t, int64_t b, int64_t rb, int64_t kb) {
         auto put = [&](const float (&v)[32], uint8_t *c, uint8_t *sc, int64_t tile) {
             uint4 q;
             const uint32_t byte = encode_block(v, q);
@@ -131,17 +135,6 @@ __global__ __launch_bounds__(256) void quantize_both_kernel(const T *__restrict_
     });
 }
 
-template <typename T>
-void quantize(const T *x, int64_t batch, int64_t rows, int64_t cols, int64_t rt, int64_t kt, int64_t batch_stride,
-              int64_t row_stride, int64_t col_stride, uint8_t *codes, uint8_t *scales, dim3 grid, hipStream_t stream) {
-    if (col_stride == 1 || cols == 1)
-        quantize_rows_kernel<<<grid, 256, 0, stream>>>(x, batch, rows, cols, rt, kt, batch_stride, row_stride,
-                                                       codes, scales);
-    else
-        quantize_columns_kernel<<<grid, 128, 0, stream>>>(x, batch, rows, cols, rt, kt, batch_stride, col_stride,
-                                                          codes, scales);
-}
-
 // A tile per block of 256 threads, 16 bytes of output a thread and step, a
 // tile row's by neighbouring lanes: stores of whole lines (a block of 32 per
 // thread: 16-byte pieces of 64 rows at once, 2.5 TB/s).
@@ -149,12 +142,12 @@ template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restrict__ codes,
                                                          const uint8_t *__restrict__ scales, int64_t batch,
                                                          int64_t rows, int64_t cols, int64_t row_tiles,
-                                                         int64_t col_tiles, T *__restrict__ out, int64_t batch_stride,
-                                                         int64_t row_stride) {
+                                                         int64_t col_tiles, int64_t first_col, T *__restrict__ out,
+                                                         int64_t batch_stride, int64_t row_stride) {
     typedef float float2v __attribute__((ext_vector_type(2)));
     constexpr int kPer = 16 / sizeof(T), kLanes = kMx4TileCols / kPer, kRows = 256 / kLanes;
     const int col = static_cast<int>(threadIdx.x) % kLanes * kPer, block = col >> 5;
-    for_tiles(row_tiles, col_tiles, batch, [&](int64_t tile, int64_t b, int64_t rt, int64_t kt) {
+    for_tiles(row_tiles, col_tiles, batch, first_col, [&](int64_t tile, int64_t b, int64_t rt, int64_t kt) {
         const int64_t k = kt * kMx4TileCols + col;
 #pragma unroll
         for (int i = 0; i < kMx4TileRows; i += kRows) {
@@ -199,9 +192,16 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restri
     });
 }
 
-dim3 grid_for(int64_t batch, int64_t row_tiles, int64_t col_tiles) {
-    return dim3(static_cast<unsigned>(std::min<int64_t>(col_tiles, 1 << 22)), static_cast<unsigned>(std::min<int64_t>(row_tiles, 65535)),
-                static_cast<unsigned>(std::min<int64_t>(batch, 65535)));
+// Launches over all tiles: launch(grid, first column tile).
+template <typename F>
+bool for_grids(int64_t batch, int64_t row_tiles, int64_t col_tiles, F launch) {
+    constexpr int64_t kMost = 1 << 22;  // a grid's threads in one direction are below 2^32
+    for (int64_t k = 0; k < col_tiles; k += kMost)
+        launch(dim3(static_cast<unsigned>(std::min(col_tiles - k, kMost)),
+                    static_cast<unsigned>(std::min<int64_t>(row_tiles, 65535)),
+                    static_cast<unsigned>(std::min<int64_t>(batch, 65535))),
+               k);
+    return hipGetLastError() == hipSuccess;
 }
 
 }  // namespace
@@ -211,13 +211,17 @@ bool mx4_quantize_launch(const void *x, bool bf16, int64_t batch, int64_t rows, 
     const int64_t rt = mx4_row_tiles(rows), kt = mx4_col_tiles(cols);
     if (batch == 0 || rt == 0 || kt == 0) return true;
     auto *c = static_cast<uint8_t *>(codes), *s = static_cast<uint8_t *>(scales);
-    if (bf16)
-        quantize(static_cast<const uint16_t *>(x), batch, rows, cols, rt, kt, batch_stride, row_stride, col_stride, c, s,
-                 grid_for(batch, rt, kt), stream);
-    else
-        quantize(static_cast<const float *>(x), batch, rows, cols, rt, kt, batch_stride, row_stride, col_stride, c, s,
-                 grid_for(batch, rt, kt), stream);
-    return hipGetLastError() == hipSuccess;
+    auto go = [&](auto *p) {
+        return for_grids(batch, rt, kt, [&](dim3 grid, int64_t first) {
+            if (col_stride == 1 || cols == 1)
+                quantize_rows_kernel<<<grid, 256, 0, stream>>>(p, batch, rows, cols, rt, kt, first, batch_stride,
+                                                               row_stride, c, s);
+            else
+                quantize_columns_kernel<<<grid, 128, 0, stream>>>(p, batch, rows, cols, rt, kt, first, batch_stride,
+                                                                  col_stride, c, s);
+        });
+    };
+    return bf16 ? go(static_cast<const uint16_t *>(x)) : go(static_cast<const float *>(x));
 }
 
 bool mx4_quantize_both_launch(const void *x, bool bf16, int64_t batch, int64_t rows, int64_t cols,
@@ -227,15 +231,14 @@ bool mx4_quantize_both_launch(const void *x, bool bf16, int64_t batch, int64_t r
     const int64_t rt = mx4_row_tiles(rows), kt = mx4_col_tiles(cols), t_rt = mx4_row_tiles(cols),
                   t_kt = mx4_col_tiles(rows);
     auto go = [&](auto *p) {
-        quantize_both_kernel<<<grid_for(batch, t_kt, kt), 256, 0, stream>>>(
-            p, batch, rows, cols, rt, kt, t_rt, t_kt, batch_stride, row_stride, static_cast<uint8_t *>(codes),
-            static_cast<uint8_t *>(scales), static_cast<uint8_t *>(t_codes), static_cast<uint8_t *>(t_scales));
+        return for_grids(batch, t_kt, kt, [&](dim3 grid, int64_t first) {
+            quantize_both_kernel<<<grid, 256, 0, stream>>>(
+                p, batch, rows, cols, rt, kt, first, t_rt, t_kt, batch_stride, row_stride,
+                static_cast<uint8_t *>(codes), static_cast<uint8_t *>(scales), static_cast<uint8_t *>(t_codes),
+                static_cast<uint8_t *>(t_scales));
+        });
     };
-    if (bf16)
-        go(static_cast<const uint16_t *>(x));
-    else
-        go(static_cast<const float *>(x));
-    return hipGetLastError() == hipSuccess;
+    return bf16 ? go(static_cast<const uint16_t *>(x)) : go(static_cast<const float *>(x));
 }
 
 bool mx4_dequantize_launch(const void *codes, const void *scales, int64_t batch, int64_t rows, int64_t cols,
@@ -243,13 +246,13 @@ bool mx4_dequantize_launch(const void *codes, const void *scales, int64_t batch,
     const int64_t rt = mx4_row_tiles(rows), kt = mx4_col_tiles(cols);
     if (batch == 0 || rt == 0 || kt == 0) return true;
     auto *c = static_cast<const uint8_t *>(codes), *s = static_cast<const uint8_t *>(scales);
-    if (bf16)
-        dequantize_kernel<<<grid_for(batch, rt, kt), 256, 0, stream>>>(c, s, batch, rows, cols, rt, kt,
-                                                              static_cast<uint16_t *>(out), batch_stride, row_stride);
-    else
-        dequantize_kernel<<<grid_for(batch, rt, kt), 256, 0, stream>>>(c, s, batch, rows, cols, rt, kt,
-                                                              static_cast<float *>(out), batch_stride, row_stride);
-    return hipGetLastError() == hipSuccess;
+    auto go = [&](auto *to) {
+        return for_grids(batch, rt, kt, [&](dim3 grid, int64_t first) {
+            dequantize_kernel<<<grid, 256, 0, stream>>>(c, s, batch, rows, cols, rt, kt, first, to, batch_stride,
+                                                        row_stride);
+        });
+    };
+    return bf16 ? go(static_cast<uint16_t *>(out)) : go(static_cast<float *>(out));
 }
 
 }  // namespace fgd
