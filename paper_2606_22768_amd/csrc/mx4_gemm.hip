@@ -1,5 +1,10 @@
 // mx4_gemm.hip -- products of matrices in microscaled 4-bit floating point
 // (the format and its layout: mx4.hpp).
+//
+// out[i][j] = sum over k of a[i][k] w[j][k].  A product of two values is
+// exact in float32 (four significant bits); the matrix instruction multiplies
+// by both blocks' scales and adds in float32, and the sum is rounded once, to
+// the output's type.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -139,7 +144,10 @@ __device__ inline void store_rows(uint16_t *rows, int64_t stride, int64_t m, int
 // A block multiplies NW fragments of 32 rows of w by NA fragments of 32 rows
 // of a; its waves share out the columns, tile by tile in turn, and add their
 // sums through LDS in the waves' order.  Every operand goes straight from
-// memory to registers: w is read once, and a comes from L2.
+// memory to registers: w is read once, and a comes from L2.  Bound by the
+// read of w: 1 x 128256 x 2048 (140 MB) in 22 us, 6.3 TB/s; 9 x 16 x 32000 x
+// 1024 (157 MB, 18 written) in 26; 64 x 8192 x 8192 (36 MB) in 11, of which
+// the first loads, the sums and the launch are half.
 template <int NA>
 __device__ inline void products(float16v (&acc)[1][NA], const int4v (&x)[1][2], const int4v (&y)[NA][2], int sw, int sa) {
     acc[0][0] = mfma<0, 0>(x[0][0], y[0][0], acc[0][0], sw, sa);
