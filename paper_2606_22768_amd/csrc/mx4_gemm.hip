@@ -373,7 +373,10 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
               wa = wave / GN;
     // Blocks go to the eight dies in turn; each die takes a contiguous range
     // of the order below, in which 32 neighbours (a die's compute units) are
-    // 8 blocks of a by 4 of w: what its L2 serves to all of them is least.
+    // 4 blocks of a by 8 of w: what its L2 serves to all of them is least, as
+    // with 8 by 4, and the pieces of a row that are written at a time are
+    // longer (2048 x 131072 x 4096: 607 us for 668 with 8 by 4; rows of 128256:
+    // 672 and 675).
     const uint32_t per_batch = static_cast<uint32_t>(n_blocks) * a_blocks, first = (blockIdx.x & 7) * blocks_per_xcd;
     const int count = static_cast<int>(min(static_cast<int64_t>(blocks_per_xcd), batch * per_batch - first));
     const int stride = gridDim.x >> 3;
@@ -382,9 +385,9 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
         int64_t b, nb, ab;
     };
     auto place_of = [&](int item) {
-        const uint32_t id = first + item, b = id / per_batch, in_batch = id - b * per_batch, across = 8u * n_blocks;
-        const uint32_t strip = in_batch / across * 8, in_strip = in_batch % across,
-                       width = min(8u, static_cast<uint32_t>(a_blocks) - strip);
+        const uint32_t id = first + item, b = id / per_batch, in_batch = id - b * per_batch, across = 4u * n_blocks;
+        const uint32_t strip = in_batch / across * 4, in_strip = in_batch % across,
+                       width = min(4u, static_cast<uint32_t>(a_blocks) - strip);
         auto uniform = [](uint32_t v) { return static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(v)); };
         return Place{uniform(b), uniform(in_strip / width), uniform(strip + in_strip % width)};
     };
@@ -549,7 +552,7 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
 template <int GN, int GA, int WN, int WA, typename T>
 bool launch_tiled(const uint8_t *ac, const uint8_t *as, const uint8_t *wc, const uint8_t *ws, int64_t batch, int64_t m,
                   int64_t n, int64_t kt, T *out, int64_t batch_stride, int64_t row_stride, hipStream_t stream) {
-    // A die's range: whole groups of eight blocks.
+    // A die's range: whole groups of neighbours in either direction.
     const int64_t nb = (mx4_row_tiles(n) + GN * WN - 1) / (GN * WN), ab = (mx4_row_tiles(m) + GA * WA - 1) / (GA * WA);
     const int64_t per = (batch * nb * ab + 63) / 64 * 8;
     if (nb * ab > INT32_MAX / 8 || per > INT32_MAX / 8 || kt > INT32_MAX) return false;
