@@ -489,6 +489,28 @@ fgd_status fgd_mx4_linear(const void *x, int32_t x_dtype, int64_t x_batch_stride
 /* Device workspace fgd_mx4_linear needs: its quantised x.  Host only. */
 fgd_status fgd_mx4_linear_workspace_size(int32_t batch, int64_t tokens, int64_t k, int64_t *bytes);
 
+/* The gradients of such a layer, from 4-bit products: dx = dy w (tokens x k)
+ * and dw = dy^T x (n x k), with dy (tokens x n), x (tokens x k) and w
+ * quantised along the axis that each product sums over, as fgd_mx4_quantize
+ * and fgd_mx4_quantize_both would, giving the same bits as those calls and
+ * fgd_mx4_matmul.  dy, x, dx and dw have contiguous rows.
+ *   wt_codes, wt_scales   the transpose of w (k x n), quantised
+ *   workspace   device memory of at least
+ *               fgd_mx4_linear_grads_workspace_size bytes, 16-byte aligned,
+ *               overlapping none of the arrays; left undefined.  Calls that
+ *               share one must not run concurrently.
+ * Enqueued on `stream`. */
+fgd_status fgd_mx4_linear_grads(const void *dy, int32_t dy_dtype, int64_t dy_batch_stride, int64_t dy_row_stride,
+                                const void *x, int32_t x_dtype, int64_t x_batch_stride, int64_t x_row_stride,
+                                const void *wt_codes, const void *wt_scales, int32_t batch, int64_t tokens, int64_t n,
+                                int64_t k, void *dx, int32_t dx_dtype, int64_t dx_batch_stride, int64_t dx_row_stride,
+                                void *dw, int32_t dw_dtype, int64_t dw_batch_stride, int64_t dw_row_stride,
+                                void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Device workspace fgd_mx4_linear_grads needs: its quantised dy (along both
+ * axes) and x.  Host only. */
+fgd_status fgd_mx4_linear_grads_workspace_size(int32_t batch, int64_t tokens, int64_t n, int64_t k, int64_t *bytes);
+
 #define FGD_MAX_SAMPLE_VOCAB (1 << 22) /* largest vocab of fgd_sample */
 
 /* Settings of fgd_sample.  A *_rows array (device, one value per row) takes

@@ -89,6 +89,9 @@ def _load():
         "fgd_mx4_dequantize": (I32, [P, P, I32, I64, I64, P, I32, I64, I64, P]),
         "fgd_mx4_matmul": (I32, [P, P, P, P, I32, I64, I64, I64, P, I32, I64, I64, P]),
         "fgd_mx4_linear": (I32, [P, I32, I64, I64, P, P, I32, I64, I64, I64, P, I32, I64, I64, P, I64, P]),
+        "fgd_mx4_linear_grads": (I32, [P, I32, I64, I64, P, I32, I64, I64, P, P, I32, I64, I64, I64, P, I32, I64, I64,
+                                       P, I32, I64, I64, P, I64, P]),
+        "fgd_mx4_linear_grads_workspace_size": (I32, [I32, I64, I64, I64, ctypes.POINTER(I64)]),
         "fgd_mx4_linear_workspace_size": (I32, [I32, I64, I64, ctypes.POINTER(I64)]),
         "fgd_sample": (I32, [P, I32, I64, I64, I64, P, P, P, P, P, I64, P]),
         "fgd_sample_workspace_size": (I32, [I32, I64, I64, ctypes.POINTER(I64)]),
@@ -579,7 +582,8 @@ class Engine:
 
 # ------------------------------------- operators on matrices and logits
 
-from .mx4 import (Mx4, fgd_mx4_dequantize, fgd_mx4_linear, fgd_mx4_linear_workspace_size,  # noqa: E402
-                  fgd_mx4_matmul, fgd_mx4_quantize, fgd_mx4_quantize_both, fgd_mx4_size, mx4_dequantize, mx4_linear,
+from .mx4 import (Mx4, fgd_mx4_dequantize, fgd_mx4_linear, fgd_mx4_linear_grads,  # noqa: E402
+                  fgd_mx4_linear_grads_workspace_size, fgd_mx4_linear_workspace_size, fgd_mx4_matmul,
+                  fgd_mx4_quantize, fgd_mx4_quantize_both, fgd_mx4_size, mx4_dequantize, mx4_linear,
                   mx4_linear_grads, mx4_matmul, mx4_quantize, mx4_quantize_both)
 from .sampling import fgd_sample, fgd_sample_workspace_size, fgd_sampling, sample  # noqa: E402

@@ -95,7 +95,7 @@ fgd_status check_quantize_input(const char *what, const void *x, int32_t dtype, 
     if (fgd_status st =
             check_strided(what, x, dtype, batch, rows, cols, batch_stride, row_stride, col_stride, bytes))
         return st;
-    if (rows > 0 && cols > 0 && row_stride != 1 && col_stride != 1)
+    if (batch > 0 && rows > 0 && cols > 0 && row_stride != 1 && col_stride != 1)
         return api_fail(FGD_ERR_INVALID_ARG, "%s: its rows or its columns must be contiguous", what);
     return FGD_OK;
 }
@@ -255,6 +255,77 @@ fgd_status fgd_mx4_linear(const void *x, int32_t x_dtype, int64_t x_batch_stride
         !fgd::mx4_matmul_launch(codes, scales, w_codes, w_scales, batch, tokens, n, k, out, out_dtype == FGD_BF16,
                                 out_batch_stride, out_row_stride, static_cast<hipStream_t>(stream)))
         return api_fail(FGD_ERR_HIP, "4-bit layer launch failed");
+    return FGD_OK;
+}
+
+fgd_status fgd_mx4_linear_grads_workspace_size(int32_t batch, int64_t tokens, int64_t n, int64_t k, int64_t *bytes) {
+    fgd::api_clear();
+    if (!bytes) return api_fail(FGD_ERR_INVALID_ARG, "NULL bytes");
+    if (fgd_status st = check_matrix("dy", batch, tokens, n)) return st;
+    if (fgd_status st = check_matrix("dy", batch, n, tokens)) return st;
+    if (fgd_status st = check_matrix("x", batch, k, tokens)) return st;
+    *bytes = (fgd::mx4_tiles(batch, tokens, n) + fgd::mx4_tiles(batch, n, tokens) + fgd::mx4_tiles(batch, k, tokens)) *
+             (fgd::kMx4CodeBytes + fgd::kMx4ScaleBytes);
+    return FGD_OK;
+}
+
+fgd_status fgd_mx4_linear_grads(const void *dy, int32_t dy_dtype, int64_t dy_batch_stride, int64_t dy_row_stride,
+                                const void *x, int32_t x_dtype, int64_t x_batch_stride, int64_t x_row_stride,
+                                const void *wt_codes, const void *wt_scales, int32_t batch, int64_t tokens, int64_t n,
+                                int64_t k, void *dx, int32_t dx_dtype, int64_t dx_batch_stride, int64_t dx_row_stride,
+                                void *dw, int32_t dw_dtype, int64_t dw_batch_stride, int64_t dw_row_stride,
+                                void *workspace, int64_t workspace_bytes, void *stream) {
+    fgd::api_clear();
+    int64_t dy_bytes, x_bytes, dx_bytes, dw_bytes, need;
+    Spans w;
+    if (fgd_status st =
+            check_quantize_input("dy", dy, dy_dtype, batch, tokens, n, dy_batch_stride, dy_row_stride, 1, &dy_bytes))
+        return st;
+    if (fgd_status st =
+            check_quantize_input("x", x, x_dtype, batch, tokens, k, x_batch_stride, x_row_stride, 1, &x_bytes))
+        return st;
+    if (fgd_status st = fgd_mx4_linear_grads_workspace_size(batch, tokens, n, k, &need)) return st;
+    if (fgd_status st = check_product(wt_codes, wt_scales, batch, tokens, k, n, dx, dx_dtype, dx_batch_stride,
+                                      dx_row_stride, &w, &dx_bytes))
+        return st;
+    if (fgd_status st = check_dtype(dw_dtype)) return st;
+    if (static_cast<wide>(batch) * (static_cast<wide>(n) + 255) * (static_cast<wide>(k) + 255) > kMost)
+        return api_fail(FGD_ERR_INVALID_ARG, "dw: sizes are too large");
+    if (fgd_status st = check_output("dw", dw, dw_dtype, batch, n, k, dw_batch_stride, dw_row_stride, &dw_bytes))
+        return st;
+    if (need > 0 && !workspace) return api_fail(FGD_ERR_INVALID_ARG, "NULL workspace");
+    if (!aligned(workspace, 16)) return api_fail(FGD_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
+    if (workspace_bytes < need)
+        return api_fail(FGD_ERR_INVALID_ARG, "workspace of %lld bytes is below the %lld this call needs",
+                        static_cast<long long>(workspace_bytes), static_cast<long long>(need));
+    // What is written, then what is read.
+    const struct {
+        const void *p;
+        int64_t bytes;
+    } arrays[] = {{dx, dx_bytes}, {dw, dw_bytes},          {workspace, need},     {dy, dy_bytes},
+                  {x, x_bytes},   {wt_codes, w.codes}, {wt_scales, w.scales}};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 7; ++j)
+            if (ranges_overlap(arrays[i].p, arrays[i].bytes, arrays[j].p, arrays[j].bytes))
+                return api_fail(FGD_ERR_INVALID_ARG,
+                                "the gradients and the workspace must overlap neither each other nor an input");
+    const int64_t dy_tiles = fgd::mx4_tiles(batch, tokens, n), dyt_tiles = fgd::mx4_tiles(batch, n, tokens),
+                  xt_tiles = fgd::mx4_tiles(batch, k, tokens);
+    uint8_t *dy_codes = static_cast<uint8_t *>(workspace), *dyt_codes = dy_codes + dy_tiles * fgd::kMx4CodeBytes,
+            *xt_codes = dyt_codes + dyt_tiles * fgd::kMx4CodeBytes,
+            *dy_scales = xt_codes + xt_tiles * fgd::kMx4CodeBytes,
+            *dyt_scales = dy_scales + dy_tiles * fgd::kMx4ScaleBytes,
+            *xt_scales = dyt_scales + dyt_tiles * fgd::kMx4ScaleBytes;
+    const hipStream_t on = static_cast<hipStream_t>(stream);
+    if (!fgd::mx4_quantize_launch(x, x_dtype == FGD_BF16, batch, k, tokens, x_batch_stride, 1, x_row_stride, xt_codes,
+                                  xt_scales, on) ||
+        !fgd::mx4_quantize_both_launch(dy, dy_dtype == FGD_BF16, batch, tokens, n, dy_batch_stride, dy_row_stride,
+                                       dy_codes, dy_scales, dyt_codes, dyt_scales, on) ||
+        !fgd::mx4_matmul_launch(dy_codes, dy_scales, wt_codes, wt_scales, batch, tokens, k, n, dx,
+                                dx_dtype == FGD_BF16, dx_batch_stride, dx_row_stride, on) ||
+        !fgd::mx4_matmul_launch(dyt_codes, dyt_scales, xt_codes, xt_scales, batch, n, k, tokens, dw,
+                                dw_dtype == FGD_BF16, dw_batch_stride, dw_row_stride, on))
+        return api_fail(FGD_ERR_HIP, "4-bit gradients' launch failed");
     return FGD_OK;
 }
 

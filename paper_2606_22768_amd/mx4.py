@@ -73,6 +73,24 @@ def fgd_mx4_linear_workspace_size(batch, tokens, k) -> int:
     return n.value
 
 
+def fgd_mx4_linear_grads(dy, dy_dtype, dy_batch_stride, dy_row_stride, x, x_dtype, x_batch_stride, x_row_stride,
+                         wt_codes, wt_scales, batch, tokens, n, k, dx, dx_dtype, dx_batch_stride, dx_row_stride, dw,
+                         dw_dtype, dw_batch_stride, dw_row_stride, workspace, workspace_bytes, stream=None):
+    _check(lib.fgd_mx4_linear_grads(_dev(dy), DTYPES.get(dy_dtype, dy_dtype), dy_batch_stride, dy_row_stride, _dev(x),
+                                    DTYPES.get(x_dtype, x_dtype), x_batch_stride, x_row_stride, _dev(wt_codes),
+                                    _dev(wt_scales), batch, tokens, n, k, _dev(dx), DTYPES.get(dx_dtype, dx_dtype),
+                                    dx_batch_stride, dx_row_stride, _dev(dw), DTYPES.get(dw_dtype, dw_dtype),
+                                    dw_batch_stride, dw_row_stride, _dev(workspace), workspace_bytes,
+                                    _stream(stream)), "fgd_mx4_linear_grads")
+
+
+def fgd_mx4_linear_grads_workspace_size(batch, tokens, n, k) -> int:
+    size = _I64()
+    _check(lib.fgd_mx4_linear_grads_workspace_size(int(batch), int(tokens), int(n), int(k), ctypes.byref(size)),
+           "fgd_mx4_linear_grads_workspace_size")
+    return size.value
+
+
 # ----------------------------------------------------------- tensor level
 
 class Mx4:
@@ -191,8 +209,8 @@ def _packed(n, batch, rows, cols, device):
     import torch
 
     cb, sb = fgd_mx4_size(n, rows, cols)
-    pool = torch.empty(cb + sb, dtype=torch.uint8, device=device)
-    return Mx4(pool[:cb], pool[cb:], batch, rows, cols)
+    return Mx4(torch.empty(cb, dtype=torch.uint8, device=device), torch.empty(sb, dtype=torch.uint8, device=device),
+               batch, rows, cols)
 
 
 def mx4_quantize(x, stream=None) -> Mx4:
@@ -219,7 +237,7 @@ def mx4_quantize_both(x, stream=None):
     """(mx4_quantize(x), mx4_quantize(x.mT)) from one reading of x: what a
     matrix needs that takes part in a layer's product and in its gradients."""
     code, batch, rows, cols, bs, rs, cs = _matrix(x, "x")
-    if cols > 1 and rows and cs != 1:
+    if cols > 1 and x.numel() and cs != 1:
         if rs != 1:
             raise ValueError("x: its rows or its columns must be contiguous")
         t, q = mx4_quantize_both(x.mT, stream)
@@ -277,7 +295,7 @@ def mx4_linear(x, w, dtype=None, out=None, workspace=None, stream=None):
     _is_mx4(w, "w")
     if cols != w.cols or batch != w.batch:
         raise ValueError(f"x and w must share their batch and columns, got {tuple(x.shape)} and {w.shape}")
-    if cols > 1 and rows and cs != 1:
+    if cols > 1 and x.numel() and cs != 1:
         raise ValueError("x: rows must be contiguous")
     _on_gpu("x", x, w.device)
     n = 1 if batch is None else batch
@@ -313,17 +331,40 @@ def mx4_linear_grads(dy, x, w_t, dx_dtype=None, dw_dtype="f32", stream=None):
     through): dx [..][T][K] = dy w in dy's dtype (or dx_dtype) and dw
     [..][N][K] = dy^T x in dw_dtype.  dy [..][T][N]; x [..][T][K], or
     mx4_quantize(x.mT) kept from the forward pass; w_t = mx4_quantize(w.mT)."""
+    import torch
+
     _is_mx4(w_t, "w_t")
-    _matrix(dy, "dy")
-    x_t = x if isinstance(x, Mx4) else None
-    if x_t is None:
-        _matrix(x, "x")
-        if x.shape[:-1] != dy.shape[:-1] or x.shape[-1] != w_t.rows:
+    code, batch, T, N, bs, rs, cs = _matrix(dy, "dy")
+    dx_dtype = dy.dtype if dx_dtype is None else dx_dtype
+    if isinstance(x, Mx4):
+        x_t = x
+        if x_t.rows != w_t.rows:
+            raise ValueError(f"x: expected {w_t.rows} rows of its transpose, got shape {x_t.shape}")
+    else:
+        xcode, _, _, K, xbs, xrs, xcs = _matrix(x, "x")
+        if x.shape[:-1] != dy.shape[:-1] or K != w_t.rows:
             raise ValueError(f"x: expected shape {(*dy.shape[:-1], w_t.rows)}, got {tuple(x.shape)}")
+        if (cs == 1 or N == 1) and (xcs == 1 or K == 1):  # one call
+            if w_t.cols != N or w_t.batch != batch:
+                raise ValueError(f"dy and w_t must share their batch and columns, got {tuple(dy.shape)} and "
+                                 f"{w_t.shape}")
+            device = w_t.device
+            _on_gpu("dy", dy, device)
+            _on_gpu("x", x, device)
+            dims = () if batch is None else (batch,)
+            dx_t = _output_dtype(None, dx_dtype, None, device)
+            dw_t = _output_dtype(None, dw_dtype, None, device)
+            n = 1 if batch is None else batch
+            need = fgd_mx4_linear_grads_workspace_size(n, T, N, K)
+            with _on(device, stream):
+                dx, dxcode, dxbs, dxrs = _output(None, dx_t, (*dims, T, K), device)
+                dw, dwcode, dwbs, dwrs = _output(None, dw_t, (*dims, N, K), device)
+                workspace = torch.empty(need, dtype=torch.uint8, device=device)
+                fgd_mx4_linear_grads(dy, code, bs, rs, x, xcode, xbs, xrs, w_t.codes, w_t.scales, n, T, N, K, dx,
+                                     dxcode, dxbs, dxrs, dw, dwcode, dwbs, dwrs, workspace, need, _current(device))
+            return dx, dw
         x_t = mx4_quantize(x.mT, stream)
-    elif x_t.rows != w_t.rows:
-        raise ValueError(f"x: expected {w_t.rows} rows of its transpose, got shape {x_t.shape}")
     dy4, dy_t = mx4_quantize_both(dy, stream)
-    dx = mx4_matmul(dy4, w_t, dy.dtype if dx_dtype is None else dx_dtype, stream=stream)
+    dx = mx4_matmul(dy4, w_t, dx_dtype, stream=stream)
     dw = mx4_matmul(dy_t, x_t, dw_dtype, stream=stream)
     return dx, dw

@@ -435,3 +435,34 @@ def test_both_axes_in_one_reading(env, dtype):
     for shape in ((0, 5), (5, 0), (0, 0), (2, 0, 3)):
         q, t = fgd.mx4_quantize_both(torch.empty(shape, device="cuda"))
         assert q.shape == shape and t.shape == (*shape[:-2], shape[-1], shape[-2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mtnk", [(None, 1, 1, 1), (None, 1, 40, 64), (None, 257, 130, 1), (2, 77, 100, 210),
+                                  (None, 300, 513, 290), (None, 0, 5, 7), (3, 4, 0, 7), (None, 4, 5, 0), (0, 4, 5, 6)],
+                         ids=str)
+def test_gradients_in_one_call_are_those_of_its_parts(env, mtnk, dtype):
+    """The same bits, also from padded rows, from operands stored by columns
+    and from a kept transpose."""
+    fgd, torch = env
+    M, T, N, K = mtnk
+    lead = () if M is None else (M,)
+    print(f"[mx4] gradients in one call {mtnk} {dtype}", flush=True)
+    dy, x = _tensor(torch, _values((*lead, T, N), 3), dtype), _tensor(torch, _values((*lead, T, K), 4), dtype)
+    w_t = fgd.mx4_quantize(_tensor(torch, _values((*lead, K, N), 5), dtype))
+    want = (fgd.mx4_matmul(fgd.mx4_quantize(dy), w_t, dy.dtype),
+            fgd.mx4_matmul(fgd.mx4_quantize(dy.mT), fgd.mx4_quantize(x.mT), "f32"))
+
+    def padded(t):
+        wide = torch.full((*t.shape[:-1], t.shape[-1] + 5), 9.0, dtype=t.dtype, device="cuda")
+        wide[..., 2:2 + t.shape[-1]] = t
+        return wide[..., 2:2 + t.shape[-1]]
+
+    by_columns = lambda t: t.mT.contiguous().mT  # noqa: E731
+    for a, b in ((dy, x), (padded(dy), padded(x)), (by_columns(dy), x), (dy, by_columns(x)),
+                 (dy, fgd.mx4_quantize(x.mT))):
+        got = fgd.mx4_linear_grads(a, b, w_t)
+        for g, v in zip(got, want):
+            assert g.dtype == v.dtype and torch.equal(g, v)
+    got = fgd.mx4_linear_grads(dy, x, w_t, dx_dtype="f32", dw_dtype="bf16")
+    assert torch.equal(got[0].to(dy.dtype), want[0]) and torch.equal(got[1], want[1].bfloat16())

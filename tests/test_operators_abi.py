@@ -261,3 +261,43 @@ def test_quantising_both_axes_checks_its_arrays():
         call(rows=-1)
     with pytest.raises(fgd.FgdError, match="negative stride"):
         call(row_stride=-128)
+
+
+def test_mx4_linear_grads_refusals():
+    need = fgd.fgd_mx4_linear_grads_workspace_size(2, 70, 100, 200)
+    assert need == fgd.fgd_mx4_linear_workspace_size(2, 70, 100) + fgd.fgd_mx4_linear_workspace_size(2, 100, 70) + \
+        fgd.fgd_mx4_linear_workspace_size(2, 200, 70)
+    at = [i << 24 for i in range(1, 8)]
+
+    def f(dy=at[0], dt="bf16", dyrs=100, x=at[1], xt="f32", xrs=200, wc=at[2], ws=at[3], batch=2, t=70, n=100, k=200,
+          dx=at[4], dxt="bf16", dxrs=200, dw=at[5], dwt="f32", dwrs=200, dwbs=20000, work=at[6], size=need):
+        fgd.fgd_mx4_linear_grads(dy, dt, 7000, dyrs, x, xt, 14000, xrs, wc, ws, batch, t, n, k, dx, dxt, 14000, dxrs,
+                                 dw, dwt, dwbs, dwrs, work, size, 0)
+
+    for name in ("dt", "xt", "dxt", "dwt"):
+        refused(lambda: f(**{name: 3}), "dtype")
+    names = ("dy", "x", "wc", "ws", "dx", "dw", "work")
+    for name in names:
+        refused(lambda: f(**{name: None}), "NULL")
+    for name in ("wc", "ws", "work"):
+        refused(lambda: f(**{name: at[names.index(name)] + 8}), "aligned")
+    for out in ("dx", "dw", "work"):
+        for i, name in enumerate(names):
+            if name != out:
+                refused(lambda: f(**{out: at[i]}), "overlap")
+    for name in ("dyrs", "xrs"):
+        refused(lambda: f(**{name: -1}), "negative")
+    for name in ("batch", "t", "n", "k"):
+        refused(lambda: f(**{name: -1}), "negative")
+        refused(lambda: fgd.fgd_mx4_linear_grads_workspace_size(*(-1 if v == name else 2
+                                                                  for v in ("batch", "t", "n", "k"))), "negative")
+    refused(lambda: f(dxrs=199), "row_stride")
+    refused(lambda: f(dwrs=199), "row_stride")
+    refused(lambda: f(dwbs=19999), "batch_stride")
+    refused(lambda: f(size=need - 1), "below")
+    f(batch=0, dy=None, x=None, wc=None, ws=None, dx=None, dw=None, work=None, size=0)
+
+
+def test_an_empty_batch_may_have_any_strides():
+    fgd.fgd_mx4_quantize(None, "f32", 0, 4, 5, 0, 0, 0, None, None, 0)
+    fgd.fgd_mx4_quantize(None, "f32", 0, 4, 5, 7, 9, 3, None, None, 0)
