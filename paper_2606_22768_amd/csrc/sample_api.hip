@@ -60,6 +60,8 @@ fgd_status fgd_sample(const void *logits, int32_t dtype, int64_t num_rows, int64
         misaligned(settings->top_p_rows, 4) || misaligned(settings->min_p_rows, 4) || misaligned(workspace, 16))
         return api_fail(FGD_ERR_INVALID_ARG,
                         "arrays must be aligned to their element size and the workspace to 16 bytes");
+    const __int128 span = (static_cast<__int128>(num_rows - 1) * ldk + vocab) * es;
+    if (span > (INT64_C(1) << 60)) return api_fail(FGD_ERR_INVALID_ARG, "logits: sizes are too large");
     int64_t need = 0;
     if (fgd_status st = fgd_sample_workspace_size(dtype, num_rows, vocab, &need)) return st;
     if (workspace_bytes < need || (need > 0 && !workspace))
@@ -68,9 +70,9 @@ fgd_status fgd_sample(const void *logits, int32_t dtype, int64_t num_rows, int64
     const struct {
         const void *p;
         int64_t n;
-    } in[] = {{logits, ((num_rows - 1) * ldk + vocab) * es}, {uniform, num_rows * 4},
-              {settings->temperature_rows, num_rows * 4},    {settings->top_k_rows, num_rows * 4},
-              {settings->top_p_rows, num_rows * 4},          {settings->min_p_rows, num_rows * 4}},
+    } in[] = {{logits, static_cast<int64_t>(span)},       {uniform, num_rows * 4},
+              {settings->temperature_rows, num_rows * 4}, {settings->top_k_rows, num_rows * 4},
+              {settings->top_p_rows, num_rows * 4},       {settings->min_p_rows, num_rows * 4}},
       out[] = {{tokens_out, num_rows * 4}, {probs_out, num_rows * 4}, {workspace, need}};
     for (int i = 0; i < 3; ++i) {
         for (const auto &a : in)

@@ -301,3 +301,16 @@ def test_mx4_linear_grads_refusals():
 def test_an_empty_batch_may_have_any_strides():
     fgd.fgd_mx4_quantize(None, "f32", 0, 4, 5, 0, 0, 0, None, None, 0)
     fgd.fgd_mx4_quantize(None, "f32", 0, 4, 5, 7, 9, 3, None, None, 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_refuses_spans_past_every_address(dtype):
+    """(num_rows - 1) * ldk elements in full: neither a wrapped nor a negative
+    span may hide an overlap."""
+    def s(rows, ld, tok=C):
+        fgd.fgd_sample(A, dtype, rows, 1000, ld, B, settings(), tok, D, E, 1 << 40, 0)
+
+    for rows, ld in (((1 << 31) - 1, 1 << 40), ((1 << 23) + 1, 1 << 40), ((1 << 22) + 1, 1 << 40),
+                     ((1 << 31) - 1, 1 << 33)):
+        refused(lambda: s(rows, ld), "too large")
+    refused(lambda: s(1 << 20, 1 << 36, A + (1 << 50)), "overlap")  # in range: the tokens lie among the rows
