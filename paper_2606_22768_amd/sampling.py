@@ -72,7 +72,7 @@ def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, voca
     else:
         s.temperature, s.temperature_rows = _setting(temperature, "temperature", torch.float32, U, dev)
     if type(top_k) is int:
-        s.top_k = top_k
+        s.top_k = _top_k(top_k)
     else:
         s.top_k, s.top_k_rows = _setting(top_k, "top_k", torch.int32, U, dev)
     if type(top_p) is float:
@@ -110,7 +110,13 @@ def _setting(v, name, dtype, rows, device):
     if isinstance(v, torch.Tensor):
         _rows(v, name, dtype, rows, device)
         return 0, v.data_ptr() or None
-    return (int(v) if dtype == torch.int32 else float(v)), None
+    return (_top_k(int(v)) if dtype == torch.int32 else float(v)), None
+
+
+def _top_k(k):
+    """k in the C type's range: a number above every vocabulary keeps all
+    tokens, as one that is not above 0 does."""
+    return min(max(k, 0), 0x7fffffff)
 
 
 def _rows(t, name, dtype, rows, device):

@@ -349,3 +349,14 @@ def test_many_long_bf16_rows(env):
                          **{k: v[lo:lo + 8] for k, v in kw.items()})
         for a, b in zip(got, few):
             assert torch.equal(torch.nan_to_num(a[lo:lo + 8], nan=-9.0), torch.nan_to_num(b, nan=-9.0))
+
+
+def test_top_k_of_any_size(env):
+    """A Python number past 32 bits keeps all tokens, whatever its lower bits."""
+    fgd, torch = env
+    V = 1000
+    z = torch.zeros((8, V), device="cuda")
+    u = torch.full((8,), 0.875, device="cuda")
+    for k in (0, -1, -2 ** 31, -2 ** 31 - 5, 2 ** 31 - 1, 2 ** 31 + 5, 2 ** 32 + 5, 2 ** 70, np.int64(2 ** 32 + 5)):
+        tok, prob = fgd.sample(z, u, top_k=k)
+        assert (tok == 875).all() and (prob == float(np.float32(1 / V))).all(), k
