@@ -238,7 +238,7 @@ def mx4_quantize_both(x, stream=None):
     matrix needs that takes part in a layer's product and in its gradients."""
     code, batch, rows, cols, bs, rs, cs = _matrix(x, "x")
     if cols > 1 and x.numel() and cs != 1:
-        if rs != 1:
+        if rs != 1 and rows > 1:  # a single row's elements are columns of their own
             raise ValueError("x: its rows or its columns must be contiguous")
         t, q = mx4_quantize_both(x.mT, stream)
         return q, t

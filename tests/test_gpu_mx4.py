@@ -466,3 +466,23 @@ def test_gradients_in_one_call_are_those_of_its_parts(env, mtnk, dtype):
             assert g.dtype == v.dtype and torch.equal(g, v)
     got = fgd.mx4_linear_grads(dy, x, w_t, dx_dtype="f32", dw_dtype="bf16")
     assert torch.equal(got[0].to(dy.dtype), want[0]) and torch.equal(got[1], want[1].bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_one_row_of_strided_columns(env, dtype):
+    """A matrix of one row (or column) has no other to be apart from: every
+    call that takes it contiguous takes it with any stride."""
+    fgd, torch = env
+    pool = _tensor(torch, _values((3, 5, 600), 2), dtype)
+    for x in (pool[0, :1, ::3], pool[0, 1:2, 1::2], pool[:, 2:3, ::3], pool[:, :, 7:8], pool[1, :, 5:6],
+              pool[0, :1, ::3].mT, pool[:, 1:2, 1::2].mT):
+        q, t = fgd.mx4_quantize_both(x)
+        plain = x.contiguous()
+        for got, want in ((q, fgd.mx4_quantize(plain)), (t, fgd.mx4_quantize(plain.mT.contiguous())),
+                          (fgd.mx4_quantize(x), q), (fgd.mx4_quantize(x.mT), t)):
+            assert got.shape == want.shape
+            assert torch.equal(got.codes, want.codes) and torch.equal(got.scales, want.scales)
+    dy, x = pool[0, :1, ::3], pool[1, :1, 1::2]  # the gradients of one token
+    w_t = fgd.mx4_quantize(_tensor(torch, _values((300, 200), 3), dtype))
+    for got, want in zip(fgd.mx4_linear_grads(dy, x, w_t), fgd.mx4_linear_grads(dy.contiguous(), x.contiguous(), w_t)):
+        assert torch.equal(got, want)
