@@ -96,11 +96,27 @@ def fgd_mx4_linear_grads_workspace_size(batch, tokens, n, k) -> int:
 class Mx4:
     """A matrix [rows][cols], or a batch of them, in microscaled 4-bit
     floating point: the device arrays `codes` and `scales` (uint8, laid out
-    as fgd.h says) and the sizes.  `batch` is None for a single matrix."""
+    as fgd.h says) and the sizes.  `batch` is None for a single matrix.
+    Made from arrays that were kept (a checkpoint's), these are checked: the
+    kernels read as many bytes as the sizes say."""
 
     __slots__ = ("codes", "scales", "batch", "rows", "cols")
 
     def __init__(self, codes, scales, batch, rows, cols):
+        import torch
+
+        need = fgd_mx4_size(1 if batch is None else batch, rows, cols)
+        for name, t, size in (("codes", codes, need[0]), ("scales", scales, need[1])):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+            if t.dtype != torch.uint8:
+                raise TypeError(f"{name}: expected uint8, got {t.dtype}")
+            if t.numel() != size:
+                raise ValueError(f"{name}: expected {size} bytes, got {t.numel()}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name}: must be contiguous")
+        if scales.device != codes.device:
+            raise ValueError(f"scales: expected a tensor on {codes.device}, got {scales.device}")
         self.codes, self.scales, self.batch, self.rows, self.cols = codes, scales, batch, rows, cols
 
     @property
@@ -209,8 +225,11 @@ def _packed(n, batch, rows, cols, device):
     import torch
 
     cb, sb = fgd_mx4_size(n, rows, cols)
-    return Mx4(torch.empty(cb, dtype=torch.uint8, device=device), torch.empty(sb, dtype=torch.uint8, device=device),
-               batch, rows, cols)
+    q = Mx4.__new__(Mx4)  # what it is given needs no check
+    q.codes = torch.empty(cb, dtype=torch.uint8, device=device)
+    q.scales = torch.empty(sb, dtype=torch.uint8, device=device)
+    q.batch, q.rows, q.cols = batch, rows, cols
+    return q
 
 
 def mx4_quantize(x, stream=None) -> Mx4:

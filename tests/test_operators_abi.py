@@ -314,3 +314,29 @@ def test_sample_refuses_spans_past_every_address(dtype):
                      ((1 << 31) - 1, 1 << 33)):
         refused(lambda: s(rows, ld), "too large")
     refused(lambda: s(1 << 20, 1 << 36, A + (1 << 50)), "overlap")  # in range: the tokens lie among the rows
+
+
+def test_kept_codes_and_scales_are_checked():
+    """The kernels read what the sizes say: arrays that are shorter, of
+    another type, strided or apart are refused where they become a matrix."""
+    c, s = fgd.fgd_mx4_size(2, 70, 200)
+    codes, scales = torch.zeros(c, dtype=torch.uint8), torch.zeros(s, dtype=torch.uint8)
+    q = fgd.Mx4(codes, scales, 2, 70, 200)
+    assert q.shape == (2, 70, 200) and q.nbytes == c + s and q.codes is codes and q.scales is scales
+    assert fgd.Mx4(codes[:c // 2], scales[:s // 2], None, 70, 200).shape == (70, 200)
+    for args, error, text in (((codes[:-1], scales), ValueError, "codes: expected"),
+                              ((codes, scales[1:]), ValueError, "scales: expected"),
+                              ((scales, codes), ValueError, "codes: expected"),
+                              ((codes.char(), scales), TypeError, "codes: expected uint8"),
+                              ((codes, scales.float()), TypeError, "scales: expected uint8"),
+                              ((None, scales), TypeError, "codes: expected a torch tensor"),
+                              ((codes, b"0" * s), TypeError, "scales: expected a torch tensor"),
+                              ((torch.zeros(2 * c, dtype=torch.uint8)[::2], scales), ValueError, "contiguous"),
+                              ((codes, scales.to("meta")), ValueError, "scales: expected a tensor on cpu")):
+        with pytest.raises(error, match=text):
+            fgd.Mx4(*args, 2, 70, 200)
+    for sizes in ((3, 70, 200), (2, 129, 200), (2, 70, 257), (None, 70, 200)):
+        with pytest.raises(ValueError, match="codes: expected"):
+            fgd.Mx4(codes, scales, *sizes)
+    with pytest.raises(fgd.FgdError, match="negative"):
+        fgd.Mx4(codes, scales, 2, -70, 200)
