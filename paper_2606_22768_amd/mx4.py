@@ -29,6 +29,8 @@ _I64 = ctypes.c_int64
 
 def fgd_mx4_size(batch, rows, cols):
     """(bytes of the codes, bytes of the scales)."""
+    if batch > 0x7fffffff:  # ctypes would take its lower 32 bits
+        raise ValueError(f"batch: {batch} is above 2^31 - 1")
     c, s = _I64(), _I64()
     _check(lib.fgd_mx4_size(int(batch), int(rows), int(cols), ctypes.byref(c), ctypes.byref(s)), "fgd_mx4_size")
     return c.value, s.value

@@ -340,3 +340,13 @@ def test_kept_codes_and_scales_are_checked():
             fgd.Mx4(codes, scales, *sizes)
     with pytest.raises(fgd.FgdError, match="negative"):
         fgd.Mx4(codes, scales, 2, -70, 200)
+
+
+def test_a_batch_past_32_bits_is_refused():
+    """A broadcast tensor can have one; its lower bits must not stand for it."""
+    for n in (1 << 31, (1 << 32) + 1):
+        with pytest.raises(ValueError, match="batch"):
+            fgd.fgd_mx4_size(n, 1, 1)
+        with pytest.raises(ValueError, match="batch"):
+            fgd.Mx4(torch.zeros(4096, dtype=torch.uint8), torch.zeros(256, dtype=torch.uint8), n, 1, 1)
+    assert fgd.fgd_mx4_size((1 << 31) - 1, 1, 1) == (((1 << 31) - 1) * 4096, ((1 << 31) - 1) * 256)
