@@ -187,9 +187,9 @@ struct Bins {
     uint32_t found;
     float wave_max[TH / 64];
 };
-template <int TH>
+template <int TH, int ROOM = kRoom>
 struct Shared : Bins<TH> {
-    __attribute__((aligned(16))) u64 list[kRoom];  // key, then ~index: the larger is the earlier in the order
+    __attribute__((aligned(16))) u64 list[ROOM];  // key, then ~index: the larger is the earlier in the order
     u64 total;
     uint32_t listed, first, last;
     Wanted wanted;
@@ -309,8 +309,8 @@ __device__ inline uint32_t first_key(int bin, float top, float c) {
 // step's total, with which the next one works, is known to a range lo..hi:
 // of top-k's cut its bin is wanted, of top-p's and the draw's the bins from
 // one end's to the other's.  kept: the mass that min-p keeps.
-template <int TH>
-__device__ inline void find_wanted(Shared<TH> &s, const Settings &set, float u, u64 kept, float top) {
+template <int TH, int ROOM>
+__device__ inline void find_wanted(Shared<TH, ROOM> &s, const Settings &set, float u, u64 kept, float top) {
     if (threadIdx.x >= 64) return;
     int first[3] = {0, 0, 0}, last[3] = {-1, -1, -1};  // none
     u64 lo = s.mass[kBins], hi = lo;
@@ -360,17 +360,17 @@ __device__ inline void sort_list(u64 *list, int n) {
 
 // Finds the token among those collected, which are all of the wanted bins':
 // at most one a thread, each against each.
-template <int TH>
-__device__ inline void finish_few(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
+template <int TH, int ROOM>
+__device__ inline void finish_few(Shared<TH, ROOM> &s, const Settings &set, float u, u64 kept, float top, int listed,
                                   int32_t *token, float *prob) {
-    static_assert(4 * TH <= kRoom, "the pairs' room");
+    static_assert(4 * TH <= ROOM, "the pairs' room");
     const int i = threadIdx.x;
     const bool some = i < listed;
     const u64 own = some ? s.list[i] : 0;
     const float t = scaled(logit_of(static_cast<uint32_t>(own >> 32)), top, set.c);
     const uint32_t m = some ? mass_of(weight(t)) : 0, bin = some ? bin_of(t) : kBins;
     // Beside each other: a token, its bin and mass.
-    u64 *pairs = s.list + kRoom / 2;
+    u64 *pairs = s.list + ROOM / 2;
     if (some) pairs[2 * i] = own, pairs[2 * i + 1] = static_cast<u64>(bin) << 32 | m;
     __syncthreads();
     u64 before = s.mass[bin];
@@ -406,8 +406,8 @@ __device__ inline void finish_few(Shared<TH> &s, const Settings &set, float u, u
 }
 
 // The same, of any number, sorted by the block.
-template <int TH>
-__device__ inline void finish(Shared<TH> &s, const Settings &set, float u, u64 kept, float top, int listed,
+template <int TH, int ROOM>
+__device__ inline void finish(Shared<TH, ROOM> &s, const Settings &set, float u, u64 kept, float top, int listed,
                               int32_t *token, float *prob) {
     if (listed <= TH) {
         finish_few(s, set, u, kept, top, listed, token, prob);
@@ -649,6 +649,45 @@ __device__ inline void slice_collect(const T *row, int lo, int hi, const Wanted 
     });
 }
 
+// A row's histogram and token, where its largest logit is finite.  ONE_LOOP:
+// one form of the histogram's loop for all settings, in fewer registers.
+template <bool ONE_LOOP, int TH, int ROOM, typename T>
+__device__ inline void sample_row_by_bins(Shared<TH, ROOM> &s, const T *row, int vocab, const Settings &set, float u,
+                                          float top, int32_t *token, float *prob) {
+    clear_bins<TH>(s);
+    u64 kept = 0, none = 0, t0, t1;
+    if constexpr (ONE_LOOP)
+        kept = add_slice<TH, true, true>(s, row, 0, vocab, top, set.c, set.min_p);
+    else
+        kept = slice_histogram<TH>(s, row, 0, vocab, top, set, set.k < vocab);
+    __syncthreads();
+    u64 m[kBins / TH];
+    uint32_t c[kBins / TH];
+#pragma unroll
+    for (int i = 0; i < kBins / TH; ++i)
+        m[i] = s.mass[threadIdx.x * (kBins / TH) + i], c[i] = s.count[threadIdx.x * (kBins / TH) + i];
+    scan_bins<TH>(s, m, c);
+    if (set.min_p > 0.0f) {
+        scan_threads<TH>(s, kept, none, t0, t1);
+        kept = t0;
+    } else {
+        kept = s.mass[kBins];
+    }
+    find_wanted(s, set, u, kept, top);
+    if (threadIdx.x == 0) s.listed = 0;
+    __syncthreads();
+    slice_collect<TH>(row, 0, vocab, s.wanted, [&](u64 v) {
+        const uint32_t at = atomicAdd(&s.listed, 1u);
+        if (at < ROOM) s.list[at] = v;
+    });
+    __syncthreads();
+    const uint32_t listed = s.listed;
+    if (listed <= ROOM)
+        finish(s, set, u, kept, top, listed, token, prob);
+    else
+        search_row<TH>(s, row, vocab, set, u, top, token, prob);
+}
+
 // -------------------------------------------------------------- block a row
 //
 // The three steps of a row, one after the other: two blocks of 512 threads a
@@ -679,34 +718,7 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(const T *__res
             search_row<TH>(s, row, vocab, set, u, top, tokens + r, prob);
             continue;
         }
-        clear_bins<TH>(s);
-        u64 kept = slice_histogram<TH>(s, row, 0, vocab, top, set, set.k < vocab), none = 0, t0, t1;
-        __syncthreads();
-        u64 m[kBins / TH];
-        uint32_t c[kBins / TH];
-#pragma unroll
-        for (int i = 0; i < kBins / TH; ++i)
-            m[i] = s.mass[threadIdx.x * (kBins / TH) + i], c[i] = s.count[threadIdx.x * (kBins / TH) + i];
-        scan_bins<TH>(s, m, c);
-        if (set.min_p > 0.0f) {
-            scan_threads<TH>(s, kept, none, t0, t1);
-            kept = t0;
-        } else {
-            kept = s.mass[kBins];
-        }
-        find_wanted(s, set, u, kept, top);
-        if (threadIdx.x == 0) s.listed = 0;
-        __syncthreads();
-        slice_collect<TH>(row, 0, vocab, s.wanted, [&](u64 v) {
-            const uint32_t at = atomicAdd(&s.listed, 1u);
-            if (at < kRoom) s.list[at] = v;
-        });
-        __syncthreads();
-        const uint32_t listed = s.listed;
-        if (listed <= kRoom)
-            finish(s, set, u, kept, top, listed, tokens + r, prob);
-        else
-            search_row<TH>(s, row, vocab, set, u, top, tokens + r, prob);
+        sample_row_by_bins<false>(s, row, vocab, set, u, top, tokens + r, prob);
         __syncthreads();
     }
 }
@@ -730,11 +742,12 @@ constexpr uint32_t kSmallest = 95 << 7, kBeyond = kSmallest + kValues, kInfinity
 // negative groups; padded.
 constexpr int kZeroPlace = kGroups, kPlaces = 512;
 
+typedef Shared<kThreads, 4 * kThreads> BinsBeside;  // three blocks a compute unit fit
 struct ValueShared {
     union {
         uint32_t counts[kValues + 64];  // the last: of each lane's tokens elsewhere, unused
         uint32_t matches[kValues];      // a bit per token beside the row's ends: it has the drawn value
-        Bins<kThreads> search;
+        BinsBeside bins;
     };
     u64 mass[kPlaces + 1];  // sums before each place
     uint32_t count[kPlaces + 1];
@@ -792,6 +805,25 @@ __device__ inline Found find_value(const ValueShared &s, const U *before, float 
     const int l = __ffsll(static_cast<u64>(__ballot(x < (sizeof(U) == 8 ? im : ic)))) - 1;
     return {static_cast<uint32_t>(__shfl(v.bits, l)), static_cast<uint32_t>(__shfl(m, l)), __shfl(ic - gc, l),
             __shfl(im - gm, l)};
+}
+
+// A row that the counts cannot tell, by bins: four reads of it in all (2048 x
+// 128256 with 60% at -100: 783 us, of which half are counts on one address;
+// by radix descent 1565; with -inf for -100, counted, 239).  A function of its
+// own keeps its registers out of the counting loops.
+__device__ __noinline__ void sample_row_apart(BinsBeside &s, const uint16_t *row, int vocab, Settings set, float u,
+                                              int32_t *token, float *prob) {
+    const float top = slice_max<kThreads>(s, row, 0, vocab);
+    if (!(top > -__builtin_inff())) {
+        if (threadIdx.x == 0) {
+            *token = -1;
+            if (prob) *prob = top != top ? top : 0.0f;
+        }
+    } else if (top == __builtin_inff()) {
+        search_row<kThreads>(s, row, vocab, set, u, top, token, prob);
+    } else {
+        sample_row_by_bins<true>(s, row, vocab, set, u, top, token, prob);
+    }
 }
 
 __global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(const uint16_t *__restrict__ logits, int64_t rows,
@@ -887,13 +919,7 @@ __global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(const uint16
         if (__builtin_amdgcn_readfirstlane(s.sum + s.outside != static_cast<uint32_t>(vocab) || s.odd ||
                                            s.sum + s.zeros == 0 || scaled(-0x1p32f, top, set.c) > -33.0f)) {
             __syncthreads();
-            const float best = slice_max<TH>(s.search, row, 0, vocab);
-            if (best > -__builtin_inff()) {
-                search_row<TH>(s.search, row, vocab, set, u, best, tokens + r, prob);
-            } else if (tid == 0) {
-                tokens[r] = -1;
-                if (prob) *prob = best != best ? best : 0.0f;
-            }
+            sample_row_apart(s.bins, row, vocab, set, u, tokens + r, prob);
             __syncthreads();
             continue;
         }

@@ -360,3 +360,46 @@ def test_top_k_of_any_size(env):
     for k in (0, -1, -2 ** 31, -2 ** 31 - 5, 2 ** 31 - 1, 2 ** 31 + 5, 2 ** 32 + 5, 2 ** 70, np.int64(2 ** 32 + 5)):
         tok, prob = fgd.sample(z, u, top_k=k)
         assert (tok == 875).all() and (prob == float(np.float32(1 / V))).all(), k
+
+
+def _time(torch, f, calls=10):
+    """The least time of a call, in us, of five runs of `calls`."""
+    f()
+    best = float("inf")
+    for _ in range(5):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        a.record()
+        for _ in range(calls):
+            f()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b) / calls * 1e3)
+    return best
+
+
+def _masked(torch, U, V, value, seed=1):
+    """(bf16 logits of which 60% are masked with `value`, the same with -inf)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    z = torch.randn((U, V), generator=g, device="cuda") * 2
+    forbidden = torch.rand((U, V), generator=g, device="cuda") < 0.6
+    return [z.masked_fill(forbidden, v).bfloat16() for v in (value, -float("inf"))]
+
+
+def test_more_of_a_value_than_a_counter_holds(env):
+    """Long bf16 rows in which over 65535 tokens share a value without mass:
+    the tokens are those of rows masked with -inf, and such rows are read four
+    times for two (with atomics on one address beside that), not by the dozen."""
+    fgd, torch = env
+    U, V = 64, 128256
+    z, plain = _masked(torch, U, V, -100.0)
+    u = torch.rand(U, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    settings = (dict(top_p=0.9), dict(top_k=50, top_p=0.9), dict(temperature=0.7), dict(min_p=0.05),
+                dict(top_k=1000, top_p=0.95, min_p=0.001))
+    for kw in settings:
+        print(f"[sample] over 65535 of a value {kw}", flush=True)
+        for a, b in zip(fgd.sample(z, u, **kw), fgd.sample(plain, u, **kw)):
+            assert torch.equal(a, b), kw
+    for kw in settings[:2]:
+        t, t_plain = (_time(torch, lambda: fgd.sample(v, u, **kw)) for v in (z, plain))
+        assert t < 5 * t_plain, (t, t_plain)
