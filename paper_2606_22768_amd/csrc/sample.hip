@@ -732,12 +732,15 @@ __global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(const T *__res
 // another's sums (the row held in registers, read once, at a block a compute
 // unit: 330 us for the 200 of 2048 x 128256; four blocks of 64 registers, 214).
 
-// A dword counts a magnitude, from 2^-32 to 2^32: the positive value in its
+// A dword counts a magnitude, from 2^-55 to 2^9: the positive value in its
 // lower half, the negative in its upper.  A count that overflows its half
-// shows in the sum of all.  Zeros are counted apart; values of -2^32 and
-// below are taken for masks.
+// shows in the sum of all.  Zeros are counted apart; values of -2^9 and below
+// are taken for masks, without counters, where they have no mass beside the
+// largest (counted, a mask's atomics meet on one address: 64 x 128256 with 60%
+// at -1e4 137 us for 48).
 constexpr int kValues = 64 * 128, kGroups = kValues / 64;
-constexpr uint32_t kSmallest = 95 << 7, kBeyond = kSmallest + kValues, kInfinity = 0x7f80;
+constexpr uint32_t kSmallest = 72 << 7, kBeyond = kSmallest + kValues, kInfinity = 0x7f80;
+constexpr float kMask = -0x1p9f;
 // Places in the order of the values: the positive groups downwards, zero, the
 // negative groups; padded.
 constexpr int kZeroPlace = kGroups, kPlaces = 512;
@@ -809,7 +812,7 @@ __device__ inline Found find_value(const ValueShared &s, const U *before, float 
 
 // A row that the counts cannot tell, by bins: four reads of it in all (2048 x
 // 128256 with 60% at -100: 783 us, of which half are counts on one address;
-// by radix descent 1565; with -inf for -100, counted, 239).  A function of its
+// by radix descent 1565; with -inf for -100, counted, 230).  A function of its
 // own keeps its registers out of the counting loops.
 __device__ __noinline__ void sample_row_apart(BinsBeside &s, const uint16_t *row, int vocab, Settings set, float u,
                                               int32_t *token, float *prob) {
@@ -915,9 +918,10 @@ __global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(const uint16
         const float top = uniform_value(logit_of_bits(top_bits));
         float *prob = probs ? probs + r : nullptr;
         // Rows that the counts cannot tell: over 65535 tokens of a value,
-        // values without a counter, none with one, or masks that have mass.
+        // values without a counter, none with one, or masks that may have mass.
         if (__builtin_amdgcn_readfirstlane(s.sum + s.outside != static_cast<uint32_t>(vocab) || s.odd ||
-                                           s.sum + s.zeros == 0 || scaled(-0x1p32f, top, set.c) > -33.0f)) {
+                                           s.sum + s.zeros == 0 ||
+                                           (s.outside > s.zeros && !(scaled(kMask, top, set.c) <= -33.0f)))) {
             __syncthreads();
             sample_row_apart(s.bins, row, vocab, set, u, tokens + r, prob);
             __syncthreads();

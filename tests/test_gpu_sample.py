@@ -403,3 +403,78 @@ def test_more_of_a_value_than_a_counter_holds(env):
     for kw in settings[:2]:
         t, t_plain = (_time(torch, lambda: fgd.sample(v, u, **kw)) for v in (z, plain))
         assert t < 5 * t_plain, (t, t_plain)
+
+
+def test_finite_masks(env):
+    """Long bf16 rows masked with the usual finite values, also far more
+    tokens than a counter holds: the tokens and, to a factor of two (measured:
+    one), the time of rows masked with -inf."""
+    fgd, torch = env
+    U, V = 64, 128256
+    u = torch.rand(U, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    for value in (-1e3, -1e4, -65504.0, -1e9, -1e30, -float(torch.finfo(torch.bfloat16).max)):
+        z, plain = _masked(torch, U, V, value, 4)
+        print(f"[sample] masked with {value}", flush=True)
+        for kw in (dict(top_p=0.9), dict(top_k=50, top_p=0.9), dict(temperature=1.3, min_p=0.01), dict()):
+            for a, b in zip(fgd.sample(z, u, **kw), fgd.sample(plain, u, **kw)):
+                assert torch.equal(a, b), (value, kw)
+        t, t_plain = (_time(torch, lambda: fgd.sample(v, u, top_p=0.9)) for v in (z, plain))
+        assert t < 2 * t_plain, (value, t, t_plain)
+
+
+def test_large_logits_that_have_mass(env):
+    """Long bf16 rows at a temperature so high that logits of hundreds and
+    thousands, tiny ones and masks weigh alike: c = 2^-8, logits of multiples
+    of 2^8, so that every weight is a power of two."""
+    fgd, torch = env
+    n, V = 40, 70001
+    rng = np.random.default_rng(21)
+    T = float(np.float32(UNIT_T * 256))
+    assert (np.float32(1) / np.float32(T)) * np.float32(np.log2(np.e)) == np.float32(2.0 ** -8)
+    z = (rng.integers(-12, 2, (n, V)) * 256).astype(np.float32)  # down to -12 2^8, up to 2^8
+    z[1] = np.where(rng.random(V) < 0.95, -1024.0, z[1])
+    z[2, 77] = 512.0
+    z[3, 65000] = 4096.0
+    z[4] = np.where(rng.random(V) < 0.5, -np.inf, np.minimum(z[4], 0))
+    z[5] = -512.0
+    z[6] = -768.0
+    z[6, 5] = -512.0
+    z[7] = -np.inf
+    z[7, ::9] = -2.0 ** 20
+    z[8] = -256.0
+    z[9] = 256.0
+    z[10, 3] = 2.0 ** -60  # as good as zero, but before it in the order
+    z[10] = np.minimum(z[10], 2.0 ** -60)
+    u = rng.random(n).astype(np.float32)
+    print("[sample] large logits", flush=True)
+    settings = [SETTINGS[i % len(SETTINGS)] for i in range(n)]
+    get = lambda k, d: _rows(torch, [s.get(k, d) for s in settings],  # noqa: E731
+                             np.int32 if k == "top_k" else np.float32)
+    kw = dict(top_k=get("top_k", 0), top_p=get("top_p", 1.0), min_p=get("min_p", 0.0))
+    tok, prob = _run(env, z, u, "bf16", temperature=T, **kw)
+    z = _host_of_bf16(torch, z)
+    for i, s in enumerate(settings):
+        t, mass, total, _, _, _ = ref.sample(z[i], u[i], T, **s)
+        assert tok[i] == t, (i, s, u[i])
+        assert prob[i] == np.float32(np.float32(mass) / np.float32(total)), (i, s)
+
+
+def test_flat_rows_at_no_temperature(env):
+    """1 / T = 0: every token that is not masked by -inf weighs the same."""
+    fgd, torch = env
+    rng = np.random.default_rng(22)
+    for U, V, dtype in ((3, 5000, "f32"), (40, 40000, "bf16"), (2, 70001, "f32")):
+        z = (rng.standard_normal((U, V)) * 3).astype(np.float32)
+        z[rng.random((U, V)) < 0.3] = -np.inf
+        u = rng.random(U).astype(np.float32)
+        z = _host_of_bf16(torch, z) if dtype == "bf16" else z
+        for s in (dict(), dict(top_k=100), dict(top_p=0.25), dict(min_p=1.0)):
+            tok, prob = _run(env, z, u, dtype, temperature=float("inf"), **s)
+            for i in range(U):
+                t, mass, total, _, _, _ = ref.sample(z[i], u[i], float("inf"), **s)
+                assert tok[i] == t, (U, i, s)
+                assert prob[i] == np.float32(np.float32(mass) / np.float32(total))
+
+
+def _host_of_bf16(torch, a):
+    return torch.from_numpy(a).bfloat16().float().numpy()
