@@ -517,7 +517,7 @@ fgd_status fgd_mx4_linear_grads_workspace_size(int32_t batch, int64_t tokens, in
  * the place of the scalar before it; NULL: the scalar holds for every row. */
 typedef struct {
     uint32_t struct_size;          /* sizeof(fgd_sampling), checked for equality */
-    float temperature;             /* T; not above 0 (or NaN, or 1/T infinite): the most likely token */
+    float temperature;             /* T; not above 0 (or NaN, or (1/T) log2(e) infinite): the most likely token */
     const float *temperature_rows;
     float top_p;                   /* below 1: keep the likeliest tokens whose mass reaches top_p */
     float min_p;                   /* above 0: keep tokens at least min_p times as likely as the likeliest */
@@ -532,7 +532,9 @@ typedef struct {
  * row.  The tokens of a row stand in descending order of their logits (equal
  * logits: the lower index first); a token's weight is w = 2^t, t = (z - max
  * z) * ((1 / T) * log2(e)), each operation rounded to float32, and its mass
- * the whole number floor(w 2^31 + 1/2), so that all sums are exact.  top_k
+ * the whole part of w 2^31 + 1/2, that sum rounded to float32 as well (so that
+ * of whole numbers w 2^31 in [2^23, 2^24) the odd ones are raised by 1); masses
+ * are whole numbers, and all their sums exact.  top_k
  * keeps the first top_k tokens; of these top_p keeps the tokens before which
  * less than ceil(top_p * mass of the kept) lies (the first at least; a value
  * of 1 or more, or NaN, keeps all); of these min_p keeps those with w >=

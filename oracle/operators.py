@@ -50,16 +50,24 @@ def order(z):
     return np.lexsort((np.arange(z.size), -z))
 
 
+def mass_of(w):
+    """The masses of float32 weights: the whole part of w 2^31 + 1/2, rounded to
+    float32 (both terms and the sum before its rounding are exact in float64
+    wherever the result is not 0)."""
+    return np.floor((np.asarray(w, np.float32).astype(np.float64) * 2.0 ** 31 + 0.5).astype(np.float32)).astype(np.int64)
+
+
 def sample_masses(z, temperature):
-    """Whole-number masses of one row's tokens: the scaled logits in float32,
-    operation by operation, the power and the rounding in float64."""
+    """Whole-number masses of one row's tokens, and their weights: the scaled
+    logits in float32, operation by operation, the power in float64, rounded to
+    float32."""
     z = np.asarray(z, np.float32)
     top = z.max()
     with np.errstate(over="ignore", invalid="ignore", divide="ignore"):
         c = (np.float32(1.0) / np.float32(temperature)) * np.float32(np.log2(np.e))
         t = np.where(z == top, np.float32(0), (z - top) * c).astype(np.float64)
-        w = np.where(z == -np.inf, 0.0, np.exp2(np.where(np.isnan(t), -np.inf, t)))
-    return np.floor(w * 2.0 ** 31 + 0.5).astype(np.int64), w
+        w = np.where(z == -np.inf, 0.0, np.exp2(np.where(np.isnan(t), -np.inf, t))).astype(np.float32)
+    return mass_of(w), w
 
 
 def sample(z, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):

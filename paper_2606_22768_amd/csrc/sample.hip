@@ -2,8 +2,8 @@
 // and min-p, from given random numbers.
 //
 // A token's weight is w = 2^t, t = (z - max z) c, c = (1 / T) log2(e), each
-// operation rounded to float32, and its mass the whole number
-// floor(w 2^31 + 1/2).  Masses add exactly in any order, so a row's token
+// operation rounded to float32, and its mass the whole part of w 2^31 + 1/2,
+// rounded to float32.  Masses add exactly in any order, so a row's token
 // depends on its logits, settings and random number alone: not on the batch,
 // the number of blocks or the order of their sums.  2^-31 of the largest
 // probability is far below the 2^-24 that separates float32 random numbers.
@@ -74,6 +74,8 @@ __device__ inline float scaled(float z, float top, float c) {
 __device__ inline float scaled_any(float z, float top, float c) { return z == top ? 0.0f : scaled(z, top, c); }
 // 2^t; where the instruction flushes its result (t < -126) there is no mass.
 __device__ inline float weight(float t) { return __builtin_amdgcn_exp2f(t); }
+// w 2^31 is exact, its sum with 1/2 rounded: a whole number from 2^23 to 2^24
+// and a half is a tie, which goes to the even one.
 __device__ inline uint32_t mass_of(float w) { return static_cast<uint32_t>(fmaf(w, 0x1p31f, 0.5f)); }
 // The bin of a token that has mass (t >= -32).
 __device__ inline uint32_t bin_of(float t) {

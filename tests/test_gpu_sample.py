@@ -478,3 +478,33 @@ def test_flat_rows_at_no_temperature(env):
 
 def _host_of_bf16(torch, a):
     return torch.from_numpy(a).bfloat16().float().numpy()
+
+
+def test_masses_bit_by_bit(env):
+    """Rows of two tokens whose logits differ by -t at c = 1.  The second is
+    kept up to min_p = w, which gives the kernel's own weight w = 2^t to the bit;
+    its probability is then that of the mass that the definition gives w, also
+    where w 2^31 is a whole number and w 2^31 + 1/2 a tie."""
+    fgd, torch = env
+    rng = np.random.default_rng(31)
+    t = np.concatenate([-7 - rng.random(500), -20 * rng.random(300)]).astype(np.float32)
+    near = np.exp2(t.astype(np.float64)).astype(np.float32)
+    steps = np.arange(-6, 7, dtype=np.int32)
+    cand = (near.view(np.int32)[:, None] + steps).view(np.float32)  # neighbouring float32 values
+    z = np.zeros((t.size, 2), np.float32)
+    z[:, 1] = t
+    below_1 = np.nextafter(np.float32(1), np.float32(0))
+    tok, _ = _run(env, np.repeat(z, steps.size, 0), np.full(cand.size, below_1), temperature=UNIT_T,
+                  min_p=_rows(torch, cand.reshape(-1)))
+    kept = tok.reshape(cand.shape) == 1
+    assert kept[:, 0].all() and not kept[:, -1].any() and (kept[:, :-1] >= kept[:, 1:]).all()
+    w = cand[np.arange(t.size), kept.sum(1) - 1]
+    m = ref.mass_of(w)
+    tok, prob = _run(env, z, np.full(t.size, below_1), temperature=UNIT_T)
+    assert (tok == 1).all()
+    f32 = np.float32
+    assert np.array_equal(prob, (m.astype(f32) / (m + 2 ** 31).astype(f32)).astype(f32))
+    whole = (w.astype(np.float64) * 2 ** 31).astype(np.int64)
+    tie = (whole >= 2 ** 23) & (whole < 2 ** 24) & (whole % 2 == 1)
+    other = (whole.astype(f32) / (whole + 2 ** 31).astype(f32)).astype(f32)
+    assert (tie & (prob != other)).sum() > 50  # the two can be told apart
