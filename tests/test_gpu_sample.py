@@ -508,3 +508,53 @@ def test_masses_bit_by_bit(env):
     tie = (whole >= 2 ** 23) & (whole < 2 ** 24) & (whole % 2 == 1)
     other = (whole.astype(f32) / (whole + 2 ** 31).astype(f32)).astype(f32)
     assert (tie & (prob != other)).sum() > 50  # the two can be told apart
+
+
+@pytest.mark.parametrize("V", [28671, 28672, 28679, 262143, 262144, 262145])
+def test_counted_rows_at_the_ends_of_their_range(env, V):
+    """bf16 rows on both sides of the shortest and of the longest that are
+    counted (and of the last word of their matches' bits), starting on and off
+    16 bytes; the token drawn lies in the head, the first and the last vectors,
+    the last word, and the tail."""
+    fgd, torch = env
+    n = 40
+    rng = np.random.default_rng(V)
+    z = rng.integers(-24, -12, (n, V)).astype(np.float32)
+    places = [0, 1, 7, 8, 9, 255, V // 2, V - 264, V - 256, V - 33, V - 17, V - 16, V - 10, V - 9, V - 8, V - 7, V - 2, V - 1]
+    for i in range(n):  # rows of one heavy token, then of two alike
+        z[i, places[i % len(places)]] = 8.0
+        z[i, places[(i + i // len(places)) % len(places)]] = 8.0
+    z[n - 1] = -2.0  # more of a value than a counter holds, where the row is long
+    u = ((np.arange(n) + 0.5) / n).astype(np.float32)
+    want = [ref.sample(z[i], u[i], UNIT_T, top_p=0.99) for i in range(n)]
+    full = [ref.sample(z[i], u[i], UNIT_T) for i in range(n)]
+    wide = torch.full((n, V + 9), 9.0, dtype=torch.bfloat16, device="cuda")
+    for shift in (0, 1, 7):
+        print(f"[sample] ends of the counted range V={V} shift {shift}", flush=True)
+        wide.fill_(9.0)
+        rows = wide[:, shift:shift + V]
+        rows.copy_(_cuda(torch, z, "bf16"))
+        for refs, kw in ((want, dict(top_p=0.99)), (full, dict())):
+            tok, prob = fgd.sample(rows, _rows(torch, u), UNIT_T, **kw)
+            tok, prob = tok.tolist(), prob.cpu().numpy()
+            for i, r in enumerate(refs):
+                assert tok[i] == r[0], (i, kw)
+                assert prob[i] == np.float32(np.float32(r[1]) / np.float32(r[2])), (i, kw)
+
+
+@pytest.mark.parametrize("U, V, dtype", [(3, 70001, "f32"), (3, 70001, "bf16"), (40, 30001, "bf16")], ids=str)
+def test_far_long_rows(env, U, V, dtype):
+    """Rows that start past 2^32 bytes, split over blocks and counted."""
+    fgd, torch = env
+    es = 4 if dtype == "f32" else 2
+    ld = (9 * 2 ** 30 // es // (U - 1)) | 1
+    rng = np.random.default_rng(V)
+    z = np.minimum(rng.geometric(0.3, (U, V)), 30).astype(np.float32)
+    print(f"[sample] far rows {U} x {V} {dtype}", flush=True)
+    pool = torch.zeros((U - 1) * ld + V, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda")
+    view = pool.as_strided((U, V), (ld, 1))
+    view.copy_(_cuda(torch, z, dtype))
+    u = rng.random(U).astype(np.float32)
+    for kw in (dict(), dict(top_k=50, top_p=0.9)):
+        tok, _ = fgd.sample(view, _rows(torch, u), UNIT_T, **kw)
+        assert tok.tolist() == [ref.sample(z[i], u[i], UNIT_T, **kw)[0] for i in range(U)]
