@@ -1181,13 +1181,19 @@ __global__ __launch_bounds__(kThreads, 4) void slice_token_kernel(const T *__res
 }
 
 // Blocks per row; 1: a block per row and one kernel.  Three kernels and the
-// blocks' meeting cost 6 us over one, a block reads 3000 tokens a us: rows are
-// split where that saves more than 16384 tokens, over one block a compute
-// unit (1 x 128256 f32: 16 us for 50; 64 x 50257: 25 for 26; 128 x 32000: 29
-// for 24, so not).
+// blocks' meeting cost 6 us over one, and more the more blocks there are; a
+// block reads 3000 tokens a us.  So rows are split where that takes 16384
+// tokens from a block, and 128 more for every row up to 64.  Split / whole in
+// us, f32, top-k 50 and top-p 0.9, top-p 0.95: 1 x 16384: 15 / 13, 16 / 14; 1 x
+// 32000: 15 / 18, 16 / 18; 1 x 128256: 16 / 48, 25 / 60; 8 x 24000: 16 / 17, 19 /
+// 20; 32 x 32000: 20 / 19, 23 / 25; 64 x 24000: 22 / 17, 24 / 22; 64 x 32000: 23
+// / 19, 26 / 26; 64 x 50257: 24 / 25, 31 / 36; 85 x 32000: 23 / 19, 27 / 26; 100 x
+// 50257: 26 / 25, 36 / 37; 128 x 40000: 27 / 22, 31 / 30; 128 x 50257: 29 / 32, 37
+// / 40; 128 x 128256: 52 / 68, 68 / 90.
 int slices_of(int64_t rows, int32_t vocab) {
     const int64_t slices = std::min<int64_t>({256 / rows, vocab / 4096, kMostSlices});
-    return slices > 1 && vocab - vocab / slices >= 16384 ? static_cast<int>(slices) : 1;
+    const int64_t pays = 16384 + 128 * std::min<int64_t>(rows, 64);
+    return slices > 1 && vocab - vocab / slices >= pays ? static_cast<int>(slices) : 1;
 }
 
 // Whether a row's values are counted, with a block a row.  That costs some

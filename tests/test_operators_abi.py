@@ -350,3 +350,15 @@ def test_a_batch_past_32_bits_is_refused():
         with pytest.raises(ValueError, match="batch"):
             fgd.Mx4(torch.zeros(4096, dtype=torch.uint8), torch.zeros(256, dtype=torch.uint8), n, 1, 1)
     assert fgd.fgd_mx4_size((1 << 31) - 1, 1, 1) == (((1 << 31) - 1) * 4096, ((1 << 31) - 1) * 256)
+
+
+def test_sampled_rows_are_split_where_that_pays():
+    """Only rows that are split over blocks need a workspace: those that
+    measure faster so, not those that a block each takes in less time."""
+    size = fgd.fgd_sample_workspace_size
+    for rows, vocab in ((1, 16384), (4, 16384), (64, 24000), (64, 32000), (85, 32000), (128, 33000), (128, 40000),
+                        (129, 128256), (2048, 128256), (0, 128256)):
+        assert size("f32", rows, vocab) == 0, (rows, vocab)
+    for rows, vocab in ((1, 32000), (1, 128256), (16, 32000), (16, 50257), (64, 50257), (64, 128256), (128, 80000),
+                        (128, 128256)):
+        assert size("f32", rows, vocab) > 0, (rows, vocab)
