@@ -486,3 +486,41 @@ def test_one_row_of_strided_columns(env, dtype):
     w_t = fgd.mx4_quantize(_tensor(torch, _values((300, 200), 3), dtype))
     for got, want in zip(fgd.mx4_linear_grads(dy, x, w_t), fgd.mx4_linear_grads(dy.contiguous(), x.contiguous(), w_t)):
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("mnk", PRODUCTS + [(2100, 2100, 200), (1100, 17000, 385)], ids=str)
+def test_products_whose_sums_are_exact(env, mnk):
+    """Operands on the grid with scales of 1: products are multiples of 1/4 and
+    sums of up to 9000 of them stay below 2^24 quarters, so that every order of
+    float32 additions gives the exact result."""
+    fgd, torch = env
+    m, n, k = mnk
+    print(f"[mx4] exact sums {mnk}", flush=True)
+
+    def grid(rows, seed):
+        rng = np.random.default_rng(seed)
+        a = rng.choice(ref.GRID, (rows, k)) * rng.choice([-1.0, 1.0], (rows, k))
+        for j in range(0, k, 32):  # one of the largest binade in every block
+            a[np.arange(rows), j + rng.integers(0, min(32, k - j), rows)] = rng.choice([4.0, 6.0, -6.0], rows)
+        return torch.from_numpy(a).cuda()
+
+    x, w = grid(m, m + k), grid(n, n + k + 1)
+    assert 36 * k * 4 < 2 ** 24
+    want = x @ w.T.contiguous()
+    w4 = fgd.mx4_quantize(w.float())
+    assert torch.equal(fgd.mx4_linear(x.float(), w4).double(), want)
+    assert torch.equal(fgd.mx4_matmul(fgd.mx4_quantize(x.float()), w4, "f32").double(), want)
+
+
+@pytest.mark.parametrize("mnk", PRODUCTS + [(2100, 2100, 200), (1100, 17000, 385)], ids=str)
+def test_products_within_their_instructions_rounding(env, mnk):
+    """The matrix instruction sums 64 terms and adds them to what it holds: K /
+    64 additions over the steps, 64 within one, and 8 of the waves' sums."""
+    fgd, torch = env
+    m, n, k = mnk
+    print(f"[mx4] rounding {mnk}", flush=True)
+    x, w = _tensor(torch, _values((m, k), m + k + 5), "f32"), _tensor(torch, _values((n, k), n + k + 6, 1.0), "f32")
+    x4, w4 = fgd.mx4_quantize(x), fgd.mx4_quantize(w)
+    p, q = fgd.mx4_dequantize(x4).double(), fgd.mx4_dequantize(w4).double().T.contiguous()
+    off = (fgd.mx4_matmul(x4, w4, "f32").double() - p @ q).abs_()
+    assert bool((off <= (k / 64 + 64 + 8) * 2.0 ** -24 * (p.abs() @ q.abs())).all())
