@@ -24,7 +24,7 @@ __device__ inline void for_tiles(int64_t row_tiles, int64_t col_tiles, int64_t b
 
 // Rows contiguous: a 64 x 128 tile per block of 256 threads, a thread per
 // block of 32: no sum or maximum crosses lanes, and a wave stores a whole
-// fragment.  Bound by memory: 128256 x 2048 bf16 in 132 us, 5.0 TB/s.
+// fragment.  Bound by memory: 128256 x 2048 bf16 in 128 us, 5.2 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T *__restrict__ x, int64_t batch, int64_t rows,
                                                             int64_t cols, int64_t row_tiles, int64_t col_tiles,
@@ -93,8 +93,8 @@ __global__ __launch_bounds__(128) void quantize_columns_kernel(const T *__restri
 // block of 256 threads, quantised along the rows on their way to LDS and along
 // the columns from there.  An LDS row's odd stride in dwords keeps the lanes of
 // both passes, rows of one column and columns of one row, on banks of their own.
-// Bound by memory: 4096 x 8192 bf16 in 20.7 us, 5.0 TB/s (14.6 and 16.3 one by
-// one).
+// Bound by memory: 4096 x 8192 bf16 in 27 us, 3.8 TB/s (20.7 with x in the
+// last-level cache, for 14.6 and 16.3 one by one).
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_both_kernel(const T *__restrict__ x, int64_t batch, int64_t rows,
                                                             int64_t cols, int64_t row_tiles, int64_t col_tiles,
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void quantize_both_kernel(const T *__restrict_
 // A tile per block of 256 threads, 16 bytes of output a thread and step, a
 // tile row's by neighbouring lanes: stores of whole lines (a block of 32 per
 // thread: 16-byte pieces of 64 rows at once, 2.5 TB/s).  Bound by the stores:
-// 128256 x 2048 to bf16 in 95 us, 7.0 TB/s; in 119 right after the
+// 128256 x 2048 to bf16 in 95 us, 7.0 TB/s; in 121 right after the
 // quantisation, whose codes have yet to leave the caches.
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(const uint8_t *__restrict__ codes,

@@ -145,9 +145,10 @@ __device__ inline void store_rows(uint16_t *rows, int64_t stride, int64_t m, int
 // of a; its waves share out the columns, tile by tile in turn, and add their
 // sums through LDS in the waves' order.  Every operand goes straight from
 // memory to registers: w is read once, and a comes from L2.  Bound by the
-// read of w: 1 x 128256 x 2048 (140 MB) in 22 us, 6.3 TB/s; 9 x 16 x 32000 x
-// 1024 (157 MB, 18 written) in 26; 64 x 8192 x 8192 (36 MB) in 11, of which
-// the first loads, the sums and the launch are half.
+// read of w: 1 x 128256 x 2048 (140 MB) in 25 us, 5.5 TB/s (22 with w in the
+// last-level cache); 9 x 16 x 32000 x 1024 (157 MB, 18 written) in 34 (26); 64 x
+// 8192 x 8192 (36 MB) in 11, of which the first loads, the sums and the launch
+// are half.
 template <int NA>
 __device__ inline void products(float16v (&acc)[1][NA], const int4v (&x)[1][2], const int4v (&y)[NA][2], int sw, int sa) {
     acc[0][0] = mfma<0, 0>(x[0][0], y[0][0], acc[0][0], sw, sa);
@@ -351,11 +352,13 @@ __device__ inline void interleave() {
 // GN x GA waves, each holding WN x WA tiles of 64 x 64 outputs (rows of w by
 // rows of a) in registers.  A block takes block after block of the outputs,
 // as one run of steps: the first tiles of the next are on their way while the
-// last products of one are stored (2048 x 128256 x 4096 to bf16: 652 us for
-// 695 with a block each; 8192^3: 255 for 263).  Bound by the matrix unit's
-// power over the steps (8192^3 without loads and reads: 240 us of 255, 4.3
-// PFLOP/s) and by the memory's writes between them, which the steps do not
-// hide: 2048 x 128256 x 4096 without stores takes 531 us.
+// last products of one are stored (6% less time than a block each at 2048 x
+// 128256 x 4096 to bf16, 3% at 8192^3).  8192^3 takes 255 to 270 us, 4.1 to 4.3
+// PFLOP/s, 2048 x 128256 x 4096 to bf16 564 to 591, from card to card.  Bound by
+// the matrix units: busy for 57% of the cycles of a clock that their power
+// lowers to 1.8 GHz (operands of zeros: 181 us at 2.46 GHz; without a step's
+// loads and reads: 232 to 242), and, where n is large, by stores that the steps
+// do not hide (without them 2048 x 128256 x 4096 takes 7% less).
 template <int GN, int GA, int WN, int WA, typename T>
 __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_kernel(
     const uint8_t *__restrict__ a_codes, const uint8_t *__restrict__ a_scales, const uint8_t *__restrict__ w_codes,
@@ -375,8 +378,8 @@ __global__ __launch_bounds__(64 * GN * GA, (WN * WA >= 4 ? 1 : 2)) void tiled_ke
     // of the order below, in which 32 neighbours (a die's compute units) are
     // 4 blocks of a by 8 of w: what its L2 serves to all of them is least, as
     // with 8 by 4, and the pieces of a row that are written at a time are
-    // longer (2048 x 131072 x 4096: 607 us for 668 with 8 by 4; rows of 128256:
-    // 672 and 675).
+    // longer (2048 x 131072 x 4096: 607 us for 668 with 8 by 4 on one card; the
+    // same time at 128256, whose rows start off the lines).
     const uint32_t per_batch = static_cast<uint32_t>(n_blocks) * a_blocks, first = (blockIdx.x & 7) * blocks_per_xcd;
     const int count = static_cast<int>(min(static_cast<int64_t>(blocks_per_xcd), batch * per_batch - first));
     const int stride = gridDim.x >> 3;

@@ -31,10 +31,9 @@
 // second pass finds the token.
 //
 // Bound by the reads of the logits: three passes over a row (two for counted
-// ones), of which the first comes from memory and the others partly from the
-// caches.  2048 x 128256 f32: 455 us (6.9 TB/s over the three); bf16: 200 us
-// (5.2 TB/s over the two), 321 in three; one pass of copying's rate would be
-// 219 and 109.
+// ones), none of which the L2s serve: 2048 x 128256 f32 reads 3.16 GB for 1.05
+// in 455 to 476 us (6.6 to 6.9 TB/s); bf16 1.08 for 0.53 in 196 us (5.5), 321
+// in three passes; one read at 6.6 TB/s would be 159 and 80.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1045,7 +1044,7 @@ __global__ __launch_bounds__(kThreads, 6) void sample_values_kernel(const uint16
 //
 // Three kernels: the slices' maxima; the row's histogram, of the slices'; the
 // wanted tokens of each slice, and from all of them the row's.  Bound by
-// latency: 1 x 128256 f32 takes 5, 5 and 10 us, the last one's for reading the
+// latency: 1 x 128256 f32 takes 3, 5 and 10 us, the last one's for reading the
 // histogram and its sums (2.3), the search of the bins (2.2), the slice (1.2),
 // the meeting (1.7) and the token (1.3).
 
@@ -1184,7 +1183,8 @@ __global__ __launch_bounds__(kThreads, 4) void slice_token_kernel(const T *__res
 // blocks' meeting cost 6 us over one, and more the more blocks there are; a
 // block reads 3000 tokens a us.  So rows are split where that takes 16384
 // tokens from a block, and 128 more for every row up to 64.  Split / whole in
-// us, f32, top-k 50 and top-p 0.9, top-p 0.95: 1 x 16384: 15 / 13, 16 / 14; 1 x
+// us, f32, one set of logits again and again, top-k 50 and top-p 0.9, top-p
+// 0.95: 1 x 16384: 15 / 13, 16 / 14; 1 x
 // 32000: 15 / 18, 16 / 18; 1 x 128256: 16 / 48, 25 / 60; 8 x 24000: 16 / 17, 19 /
 // 20; 32 x 32000: 20 / 19, 23 / 25; 64 x 24000: 22 / 17, 24 / 22; 64 x 32000: 23
 // / 19, 26 / 26; 64 x 50257: 24 / 25, 31 / 36; 85 x 32000: 23 / 19, 27 / 26; 100 x
