@@ -558,3 +558,38 @@ def test_far_long_rows(env, U, V, dtype):
     for kw in (dict(), dict(top_k=50, top_p=0.9)):
         tok, _ = fgd.sample(view, _rows(torch, u), UNIT_T, **kw)
         assert tok.tolist() == [ref.sample(z[i], u[i], UNIT_T, **kw)[0] for i in range(U)]
+
+
+def test_every_binade_of_counted_logits(env):
+    """Long bf16 rows with logits of every binade and either sign, on both
+    sides of the ranges that are counted, below a top beside which the small
+    ones vanish: c = 2^-8, so that every weight is a power of two."""
+    fgd, torch = env
+    V = 30011
+    rng = np.random.default_rng(41)
+    T = float(np.float32(UNIT_T * 256))
+    ends = [2.0 ** e for e in (-133, -126, -56, -55, -54, -33, -32, -31)]
+    large = [2.0 ** e for e in range(8, 13)]
+    rows = []
+    for top in (256.0, 4096.0, 2.0 ** 20, 2.0 ** 31, 2.0 ** 33):
+        small = rng.choice(ends + [2.0 ** e for e in range(-60, -20)] + [0.0], V) * rng.choice([-1.0, 1.0], V)
+        z = np.where(rng.random(V) < 0.3, -rng.choice(large, V), small)
+        z[rng.integers(0, V, 5)] = top
+        rows.append(z)                             # some above, masks among them
+        rows.append(np.where(z > 0, -z, z))        # none above zero
+        rows.append(np.where(np.abs(z) < 1, z, -np.inf))
+        rows.append(np.where(z == 0, top, -np.abs(z)))
+    z = np.stack(rows * 2).astype(np.float32)      # 40 rows
+    z = _host_of_bf16(torch, z)
+    n = z.shape[0]
+    u = rng.random(n).astype(np.float32)
+    settings = [SETTINGS[(i + i // 20) % len(SETTINGS)] for i in range(n)]
+    get = lambda k, d: _rows(torch, [s.get(k, d) for s in settings],  # noqa: E731
+                             np.int32 if k == "top_k" else np.float32)
+    print("[sample] every binade", flush=True)
+    tok, prob = _run(env, z, u, "bf16", temperature=T, top_k=get("top_k", 0), top_p=get("top_p", 1.0),
+                     min_p=get("min_p", 0.0))
+    for i, s in enumerate(settings):
+        t, mass, total, _, _, _ = ref.sample(z[i], u[i], T, **s)
+        assert tok[i] == t, (i, s, u[i])
+        assert prob[i] == np.float32(np.float32(mass) / np.float32(total)), (i, s)
