@@ -511,6 +511,201 @@ fgd_status fgd_mx4_linear_grads(const void *dy, int32_t dy_dtype, int64_t dy_bat
  * axes) and x.  Host only. */
 fgd_status fgd_mx4_linear_grads_workspace_size(int32_t batch, int64_t tokens, int64_t n, int64_t k, int64_t *bytes);
 
+/* ---------------------------------------------------------------------
+ * Attention over paged caches in 4 bits: heads normed and rotated, keys and
+ * values written into pages, attention over them, and the pages' tables.
+ *
+ * Dense arrays of heads are [tokens][heads][head_dim] (or [batch][tokens]
+ * [heads][head_dim]) with element strides of all axes but the last, whose
+ * elements are contiguous; they need their element's alignment only. */
+#define FGD_MAX_HEADS 65535
+#define FGD_MAX_HEAD_DIM 512
+
+/* Sizes and settings of fgd_rotate_heads. */
+typedef struct {
+    uint32_t struct_size;     /* sizeof(fgd_heads), checked for equality */
+    int32_t dtype;            /* of q, k, their outputs and gradients */
+    int32_t batch;            /* for instance the workers */
+    int32_t q_heads, k_heads; /* either may be 0 */
+    int32_t head_dim;         /* even, in [2, FGD_MAX_HEAD_DIM] */
+    int32_t rot_dim;          /* even, in [0, head_dim]: elements of a head that are rotated */
+    int32_t interleaved;      /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2 i, 2 i + 1) */
+    int64_t tokens;
+    int64_t position_stride;  /* elements between batch entries' positions; 0: they share them */
+    int64_t weight_stride;    /* elements between batch entries' weights; 0: they share them */
+    float eps;                /* finite, not negative */
+    int32_t weight_dtype;
+} fgd_heads;
+
+/* Norms and rotates queries and keys, head by head: y = R (x / sqrt(mean(x^2)
+ * + eps) * w), R turning pair i of the first rot_dim elements by position *
+ * freqs[i]: (a, b) to (a cos - b sin, a sin + b cos).  Angles are float64,
+ * all else float32, with one rounding to dtype.  An input without weights is
+ * rotated without a norm.
+ *   q, k             device, dtype, batch x tokens x heads x head_dim;
+ *                    *_strides: int64_t[3] of batch, token and head (host)
+ *   positions        device int32 [tokens], or of every batch entry
+ *   freqs            device double[rot_dim / 2], radians per position
+ *   q_weight,        device, weight_dtype [head_dim], or of every batch
+ *   k_weight         entry; NULL: no norm
+ *   q_out, k_out     may be the input itself with the same strides (in
+ *                    place); no other overlap
+ * Enqueued on `stream`. */
+fgd_status fgd_rotate_heads(const fgd_heads *sizes, const void *q, const int64_t *q_strides, const void *k,
+                            const int64_t *k_strides, const int32_t *positions, const double *freqs,
+                            const void *q_weight, const void *k_weight, void *q_out, const int64_t *q_out_strides,
+                            void *k_out, const int64_t *k_out_strides, void *stream);
+
+/* Its gradients, from those of its outputs (dq, dk) and its inputs: q_grad
+ * and k_grad in dtype, and q_weight_grad and k_weight_grad (float32,
+ * [head_dim] where batch entries share the weights: the sum over all of
+ * them; else [batch][head_dim]), each given with its weight.  q and k may be
+ * NULL where they have no weight.  Sums run in an order that the sizes fix.
+ *   workspace   device memory of at least
+ *               fgd_rotate_heads_grads_workspace_size bytes, 16-byte aligned,
+ *               overlapping none of the arrays; left undefined.  Calls that
+ *               share one must not run concurrently.
+ * Enqueued on `stream`. */
+fgd_status fgd_rotate_heads_grads(const fgd_heads *sizes, const void *dq, const int64_t *dq_strides, const void *dk,
+                                  const int64_t *dk_strides, const void *q, const int64_t *q_strides, const void *k,
+                                  const int64_t *k_strides, const int32_t *positions, const double *freqs,
+                                  const void *q_weight, const void *k_weight, void *q_grad,
+                                  const int64_t *q_grad_strides, void *k_grad, const int64_t *k_grad_strides,
+                                  float *q_weight_grad, float *k_weight_grad, void *workspace,
+                                  int64_t workspace_bytes, void *stream);
+
+/* Device workspace fgd_rotate_heads_grads needs with weights for both inputs
+ * (without any it needs none).  Host only. */
+fgd_status fgd_rotate_heads_grads_workspace_size(const fgd_heads *sizes, int64_t *bytes);
+
+/* A paged cache of keys and values: `pages` pages of `page` tokens, each
+ * token's heads in blocks of 32 elements in the 4-bit format above, so 17
+ * bytes for 32 elements.  Slot s is token s % page of page s / page.
+ *
+ * A head's 16 consecutive tokens lie in a group of 17 head_dim bytes; the
+ * group of token t of page p, head h is at index (p heads + h) (page / 16) +
+ * t / 16.  With D = head_dim, NB = D / 32, in that order: the keys' codes (8
+ * D bytes; element (h D / 4 + j) of token i is nibble j % 2, low first, of
+ * byte (i + 16 h) D / 8 + j / 2), the values' codes (8 D bytes; element 32 b
+ * + 2 n + o of token i is nibble o of byte (n + 16 (i / 4)) D / 8 + 4 b + i %
+ * 4), the keys' scales (byte i NB + b) and the values' (byte (i / 4) 4 NB + 4
+ * b + i % 4).  A cache's bytes need no initial value. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(fgd_mx4_cache), checked for equality */
+    int32_t page;         /* tokens, a power of two in [16, 65536] */
+    int32_t heads;        /* of keys, in [1, FGD_MAX_HEADS] */
+    int32_t head_dim;     /* a multiple of 32 in [32, 256] */
+    int64_t pages;        /* below 2^31 */
+    void *data;           /* device, fgd_mx4_cache_size bytes, 16-byte aligned */
+    int64_t reserved;     /* 0 */
+} fgd_mx4_cache;
+
+/* Bytes of the cache's data.  Host only. */
+fgd_status fgd_mx4_cache_size(const fgd_mx4_cache *cache, int64_t *bytes);
+
+/* Writes tokens' keys and values to their slots.
+ *   k, v    device, dtype, tokens x heads x head_dim
+ *   slots   device int64[tokens]; a token whose slot is negative or past the
+ *           cache is not written (padding); tokens of one call that share a
+ *           slot leave it undefined
+ * Enqueued on `stream`. */
+fgd_status fgd_mx4_cache_write(const fgd_mx4_cache *cache, const void *k, int64_t k_token_stride,
+                               int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                               int32_t dtype, int64_t tokens, const int64_t *slots, void *stream);
+
+/* Writes the values that slots hold to k and v, exactly; zeros for a slot
+ * that is negative or past the cache.  Enqueued on `stream`. */
+fgd_status fgd_mx4_cache_read(const fgd_mx4_cache *cache, const int64_t *slots, int64_t tokens, void *k,
+                              int64_t k_token_stride, int64_t k_head_stride, void *v, int64_t v_token_stride,
+                              int64_t v_head_stride, int32_t dtype, void *stream);
+
+/* Sizes and settings of fgd_mx4_attend. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(fgd_attention), checked for equality */
+    int32_t dtype;        /* of q and out */
+    int32_t sequences;
+    int32_t table_width;  /* entries of a sequence's table; table_width * page below 2^31 */
+    int32_t q_heads;      /* a multiple of the cache's heads: neighbouring ones share a head of keys */
+    int32_t window;       /* above 0: a query sees the last `window` keys up to its own; 0: all of them */
+    int64_t tokens;       /* rows of q */
+    int64_t most_queries; /* of a sequence, as far as the program knows: steers the launch, results do not need it */
+    float scale;          /* above 0; of the scores */
+    int32_t reserved;     /* 0 */
+} fgd_attention;
+
+/* Attention over the cache: o = sum_j p_j v_j, p the softmax of scale q.k_j
+ * over the keys that the query sees.  Sequence b has lengths[b] keys (those
+ * of its queries among them), in the slots that its table's pages hold, and
+ * the queries [starts[b], starts[b + 1]), the last of which stands at its
+ * last key: query i of n sees the keys j <= lengths[b] - n + i, and j >
+ * lengths[b] - n + i - window with a window.  What a query does not see never
+ * reaches its output, whatever it holds.  A query that sees nothing, or whose
+ * scores are all -inf, gives zeros.
+ *   q, out     device, dtype, tokens x q_heads x head_dim
+ *   tables     device int32, sequence b's page numbers at b * table_stride;
+ *              entries past a sequence's length are not read
+ *   lengths    device int32[sequences]; a negative one counts as 0
+ *   starts     device int32[sequences + 1], ascending within [0, tokens];
+ *              NULL: one query per sequence (tokens == sequences).  Rows of
+ *              no sequence are left as they were
+ *   workspace  device memory of at least fgd_mx4_attend_workspace_size
+ *              bytes, 16-byte aligned (may be NULL where that is 0),
+ *              overlapping none of the arrays; left undefined.  Calls that
+ *              share one must not run concurrently.
+ * The outputs of a sequence with a length past its table are NaN; a page
+ * number outside [0, pages) where a query sees keys makes its output NaN, and
+ * may make those of the sequence's other queries.  Equal calls on one device give equal bits; the order
+ * of the sums depends on the sizes.  Enqueued on `stream`. */
+fgd_status fgd_mx4_attend(const fgd_mx4_cache *cache, const fgd_attention *sizes, const void *q,
+                          int64_t q_token_stride, int64_t q_head_stride, const int32_t *tables, int64_t table_stride,
+                          const int32_t *lengths, const int32_t *starts, void *out, int64_t out_token_stride,
+                          int64_t out_head_stride, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Device workspace fgd_mx4_attend needs for these sizes.  Host only. */
+fgd_status fgd_mx4_attend_workspace_size(const fgd_mx4_cache *cache, const fgd_attention *sizes, int64_t *bytes);
+
+/* What a program keeps of a cache's pages, on the GPU: every request's table
+ * and length, and a stack of free pages. */
+typedef struct {
+    uint32_t struct_size; /* sizeof(fgd_pages), checked for equality */
+    int32_t page;         /* tokens, in [1, 65536] */
+    int32_t requests, table_width;
+    int64_t table_stride;
+    int32_t *tables;      /* device, request b's page numbers at b * table_stride */
+    int32_t *lengths;     /* device [requests] */
+    int32_t *free;        /* device [capacity]: the first *free_count entries are free pages */
+    int32_t *free_count;  /* device [1] */
+    int32_t capacity;
+    int32_t reserved;     /* 0 */
+} fgd_pages;
+
+/* Makes room for counts[b] further tokens of every request, in the requests'
+ * order: its pages are taken from the top of the stack and added to its
+ * table, its length grows, and its new tokens' positions and slots are listed.
+ * A request is served wholly or not at all: not where its table is too short,
+ * where the pages that it and the requests before it ask for (served or not,
+ * but for those with too short a table) are more than are free, or where
+ * their tokens are more than `tokens`; one that needs no page is not held up
+ * by the pages of others.  One that is not served keeps its table and length
+ * and has no new tokens (starts[b + 1] == starts[b]).
+ *   counts      device int32[requests]; below 0 counts as 0
+ *   starts      device int32[requests + 1]: where each request's new tokens
+ *               begin among all; the last is how many there are
+ *   positions   device int32[tokens]: each token's place in its request; 0
+ *               behind the last
+ *   slots       device int64[tokens]: its slot in the cache; -1 behind the
+ *               last, and in a table's entry below 0
+ * Enqueued on `stream`. */
+fgd_status fgd_extend_pages(const fgd_pages *pages, const int32_t *counts, int64_t tokens, int32_t *starts,
+                            int32_t *positions, int64_t *slots, void *stream);
+
+/* Shortens requests to keep[b] tokens (0: a request that is done; its length
+ * or more: nothing happens).  Pages that no token is left in go back on the
+ * stack, and their entries in the tables become -1.  Taking back all that one
+ * fgd_extend_pages gave leaves the stack as it was.  Pages that would pass the
+ * stack's capacity are dropped.  Enqueued on `stream`. */
+fgd_status fgd_truncate_pages(const fgd_pages *pages, const int32_t *keep, void *stream);
+
 #define FGD_MAX_SAMPLE_VOCAB (1 << 22) /* largest vocab of fgd_sample */
 
 /* Settings of fgd_sample.  A *_rows array (device, one value per row) takes

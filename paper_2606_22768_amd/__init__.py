@@ -27,6 +27,7 @@ FGD_REWEIGHT_NONE, FGD_REWEIGHT_METROPOLIS, FGD_REWEIGHT_SELF = 0, 1, 2
 FGD_MAX_WORKERS, FGD_MAX_ROUNDS, FGD_MAX_SUBSET_SEGMENTS = 64, 8, 4096
 FGD_MAX_JS_TOPK, FGD_MAX_JS_WORKERS = 1024, 4096
 FGD_MX4_BLOCK, FGD_MAX_SAMPLE_VOCAB = 32, 1 << 22
+FGD_MAX_HEADS, FGD_MAX_HEAD_DIM = 65535, 512
 
 DTYPES = {"f32": FGD_F32, "bf16": FGD_BF16}
 KINDS = {"identity": FGD_W_IDENTITY, "global": FGD_W_GLOBAL_MEAN, "csr": FGD_W_CSR}
@@ -95,6 +96,16 @@ def _load():
         "fgd_mx4_linear_workspace_size": (I32, [I32, I64, I64, ctypes.POINTER(I64)]),
         "fgd_sample": (I32, [P, I32, I64, I64, I64, P, P, P, P, P, I64, P]),
         "fgd_sample_workspace_size": (I32, [I32, I64, I64, ctypes.POINTER(I64)]),
+        "fgd_rotate_heads": (I32, [P] * 14),
+        "fgd_rotate_heads_grads": (I32, [P] * 20 + [I64, P]),
+        "fgd_rotate_heads_grads_workspace_size": (I32, [P, ctypes.POINTER(I64)]),
+        "fgd_mx4_cache_size": (I32, [P, ctypes.POINTER(I64)]),
+        "fgd_mx4_cache_write": (I32, [P, P, I64, I64, P, I64, I64, I32, I64, P, P]),
+        "fgd_mx4_cache_read": (I32, [P, P, I64, P, I64, I64, P, I64, I64, I32, P]),
+        "fgd_mx4_attend": (I32, [P, P, P, I64, I64, P, I64, P, P, P, I64, I64, P, I64, P]),
+        "fgd_mx4_attend_workspace_size": (I32, [P, P, ctypes.POINTER(I64)]),
+        "fgd_extend_pages": (I32, [P, P, I64, P, P, P, P]),
+        "fgd_truncate_pages": (I32, [P, P, P]),
         "fgd_stream_js_pattern": (I32, [P, P, I32, I32, I64, I64, I64, P, I64, P]),
         "fgd_status_string": (ctypes.c_char_p, [I32]),
         "fgd_last_error": (ctypes.c_char_p, []),
@@ -580,10 +591,16 @@ class Engine:
         return fgd_read_timing(self.handle)
 
 
-# ------------------------------------- operators on matrices and logits
+# ------------------------------ operators on matrices, logits and caches
 
 from .mx4 import (Mx4, fgd_mx4_dequantize, fgd_mx4_linear, fgd_mx4_linear_grads,  # noqa: E402
                   fgd_mx4_linear_grads_workspace_size, fgd_mx4_linear_workspace_size, fgd_mx4_matmul,
                   fgd_mx4_quantize, fgd_mx4_quantize_both, fgd_mx4_size, mx4_dequantize, mx4_linear,
                   mx4_linear_grads, mx4_matmul, mx4_quantize, mx4_quantize_both)
 from .sampling import fgd_sample, fgd_sample_workspace_size, fgd_sampling, sample  # noqa: E402
+from .heads import (fgd_heads, fgd_rotate_heads, fgd_rotate_heads_grads,  # noqa: E402
+                    fgd_rotate_heads_grads_workspace_size, rotate_heads, rotate_heads_grads)
+from .cache import (Mx4Cache, extend_pages, fgd_attention, fgd_extend_pages, fgd_mx4_attend,  # noqa: E402
+                    fgd_mx4_attend_workspace_size, fgd_mx4_cache, fgd_mx4_cache_read, fgd_mx4_cache_size,
+                    fgd_mx4_cache_write, fgd_pages, fgd_truncate_pages, mx4_attend, mx4_cache_read, mx4_cache_write,
+                    truncate_pages)

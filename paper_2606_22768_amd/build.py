@@ -33,7 +33,8 @@ HIP_SOURCES = ["engine.hip", "kernels_f32.hip", "kernels_bf16.hip", "kernels_f32
                "kernels_f32_split.hip", "kernels_bf16_split.hip", "kernels_f32_class.hip", "kernels_bf16_class.hip",
                "kernels_f32_ms_class.hip", "kernels_bf16_ms_class.hip", "kernels_f32_split_class.hip",
                "kernels_bf16_split_class.hip", "kernels_wg.hip", "kernels_common.hip",
-               "js.hip", "js_api.hip", "mx4.hip", "mx4_gemm.hip", "mx4_api.hip", "sample.hip", "sample_api.hip"]
+               "js.hip", "js_api.hip", "mx4.hip", "mx4_gemm.hip", "mx4_api.hip", "sample.hip", "sample_api.hip",
+               "heads.hip", "heads_api.hip", "cache.hip", "attend.hip", "pages.hip", "cache_api.hip"]
 CXX_SOURCES = ["topology.cpp"]
 
 ARCH = "gfx950"
@@ -45,9 +46,10 @@ CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
 
 HASH_COMPONENTS = ("all", "step", "js")
 JS_SOURCES = ("js.hip", "js.hpp", "js_api.hip")
-# Operators on matrices and logits: in the whole library's hash alone.
+# Operators on matrices, logits and caches: in the whole library's hash alone.
 OPERATOR_SOURCES = ("mx4.hip", "mx4.hpp", "mx4_block.hpp", "mx4_gemm.hip", "mx4_api.hip", "sample.hip",
-                    "sample.hpp", "sample_api.hip")
+                    "sample.hpp", "sample_api.hip", "api_args.hpp", "heads.hip", "heads.hpp", "heads_api.hip",
+                    "cache.hip", "cache.hpp", "attend.hip", "pages.hip", "pages.hpp", "cache_api.hip")
 
 
 def source_hashes(root: str = ROOT) -> dict:
