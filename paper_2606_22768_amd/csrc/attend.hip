@@ -96,18 +96,23 @@ struct __attribute__((packed, aligned(4))) Words {
 };
 
 template <int NB>
-__device__ inline void load_group(const uint8_t *g, int lane, int u, Raw<NB> &r) {
-    constexpr int D = 32 * NB;
-    const int h = lane >> 4;
+__device__ inline void load_keys(const uint8_t *g, int lane, int u, Raw<NB> &r) {
     const auto k = *reinterpret_cast<const Words<NB> *>(g + lane * 4 * NB);
-    const auto v = *reinterpret_cast<const Words<NB> *>(g + 8 * D + lane * 4 * NB);
-    const auto s = *reinterpret_cast<const Words<NB> *>(g + 16 * D + D / 2 + h * 4 * NB);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) r.k[u][i] = k.w[i], r.v[u][i] = v.w[i], r.vs[u][i] = s.w[i];
-    const uint8_t *ks = g + 16 * D + (lane & 15) * NB;
-    const int first = h * NB / 4;
+    for (int i = 0; i < NB; ++i) r.k[u][i] = k.w[i];
+    const uint8_t *ks = g + 16 * 32 * NB + (lane & 15) * NB;
+    const int first = (lane >> 4) * NB / 4;
 #pragma unroll
     for (int i = 0; i < kKeyScales<NB>; ++i) r.ks[u][i] = ks[min(first + i, NB - 1)];
+}
+
+template <int NB>
+__device__ inline void load_values(const uint8_t *g, int lane, int u, Raw<NB> &r) {
+    constexpr int D = 32 * NB;
+    const auto v = *reinterpret_cast<const Words<NB> *>(g + 8 * D + lane * 4 * NB);
+    const auto s = *reinterpret_cast<const Words<NB> *>(g + 16 * D + D / 2 + (lane >> 4) * 4 * NB);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) r.v[u][i] = v.w[i], r.vs[u][i] = s.w[i];
 }
 
 // A wave's state: R tiles of 16 rows.
@@ -152,12 +157,9 @@ struct Rows {
         }
     }
 
-    // One step over 32 keys from `first`; c = scale log2(e).  kMasked: not
-    // every row sees all of them.
-    template <bool kMasked>
-    __device__ void step(Raw<NB> &x, int first, int lane, float c) {
+    // The scores of 32 keys with all rows.
+    __device__ void scores(const Raw<NB> &x, int lane, f32x4 (&s)[R][2]) const {
         const int h = lane >> 4;
-        f32x4 s[R][2];
 #pragma unroll
         for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -182,46 +184,53 @@ struct Rows {
                     for (int j = kQ - 1; j >= 0; --j) s[r][u] = mfma(a, q[r][j][p], s[r][u]);
             }
         }
-        if constexpr (kMasked) {
-            uint32_t seen[R];  // bit 4 u + i: the lane's row sees key first + 16 u + 4 h + i
+    }
+
+    // Scores of keys that a row does not see become -inf.  A weight of 0 does
+    // not take away a NaN or an infinity (bytes above 252, which no finite
+    // block has): such values are taken out as well and kept in mind for the
+    // rows that see them.
+    __device__ void mask(Raw<NB> &x, int first, int lane, f32x4 (&s)[R][2]) {
+        const int h = lane >> 4;
+        uint32_t seen[R];  // bit 4 u + i: the lane's row sees key first + 16 u + 4 h + i
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                seen[r] = 0;
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int key = first + 16 * u + 4 * h + i;
-                        const bool v = key >= lo[r] && key < hi[r];
-                        seen[r] |= static_cast<uint32_t>(v) << (4 * u + i);
-                        if (!v) s[r][u][i] = -INFINITY;
-                    }
-            }
-            // A weight of 0 does not take away a NaN or an infinity (bytes
-            // above 252, which no finite block has): such values are taken
-            // out here and kept in mind for the rows that see them.
-            uint32_t bad = 0;
+        for (int r = 0; r < R; ++r) {
+            seen[r] = 0;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const uint32_t w = x.vs[u][b];
-                    bad |= ((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u;
+                for (int i = 0; i < 4; ++i) {
+                    const int key = first + 16 * u + 4 * h + i;
+                    const bool v = key >= lo[r] && key < hi[r];
+                    seen[r] |= static_cast<uint32_t>(v) << (4 * u + i);
+                    if (!v) s[r][u][i] = -INFINITY;
                 }
-            if (__any(bad != 0)) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if ((x.vs[u][b] >> (8 * i) & 255) > 252) {
-                                x.vs[u][b] &= ~(255u << (8 * i));
-#pragma unroll
-                                for (int r = 0; r < R; ++r) poison[r] |= (seen[r] >> (4 * u + i) & 1) << b;
-                            }
-            }
         }
+        uint32_t bad = 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t w = x.vs[u][b];
+                bad |= ((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u;
+            }
+        if (!__any(bad != 0)) return;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if ((x.vs[u][b] >> (8 * i) & 255) > 252) {
+                        x.vs[u][b] &= ~(255u << (8 * i));
+#pragma unroll
+                        for (int r = 0; r < R; ++r) poison[r] |= (seen[r] >> (4 * u + i) & 1) << b;
+                    }
+    }
+
+    // Scores to weights, as the parts that the second product takes; c =
+    // scale log2(e).
+    __device__ void weights(const f32x4 (&s)[R][2], float c, u32x4 (&p)[R][kP]) {
         bool move = false;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -245,7 +254,6 @@ struct Rows {
                 for (int b = 0; b < NB; ++b) o[r][b][0] *= f, o[r][b][1] *= f;
             }
         }
-        u32x4 p[R][kP];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             // s - m before the factor: the largest weight is 1 exactly, and
@@ -264,6 +272,9 @@ struct Rows {
                 }
             }
         }
+    }
+
+    __device__ void add(const Raw<NB> &x, const u32x4 (&p)[R][kP]) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             uint32_t w[8];  // (element 2 n, element 2 n + 1) of the lane's keys
@@ -287,6 +298,8 @@ struct Rows {
                     o[r][b][0] = mfma(even, p[r][j], o[r][b][0]);
                     o[r][b][1] = mfma(odd, p[r][j], o[r][b][1]);
                 }
+            // Else the scheduler converts all blocks first, in twice the registers.
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
@@ -342,8 +355,18 @@ struct Place {
 // kShared: the block's four waves share 16 R rows and split their keys
 // between them (and the grid splits them again, where splits > 1); else each
 // wave has rows of its own.
+// Waves of a SIMD that the registers are kept few enough for: a row tile's
+// sums and queries, a step's codes and scales, and about 70 more.
+template <typename T, int NB, int R>
+constexpr int kRegisters = R * NB * (8 + 4 * Parts<T>::q) + 6 * NB + 60 + 10 * R;
+template <typename T, int NB, int R>
+constexpr int kOccupancy = kRegisters<T, NB, R> <= 110   ? 4
+                           : kRegisters<T, NB, R> <= 150 ? 3
+                           : kRegisters<T, NB, R> <= 235 ? 2
+                                                         : 1;
+
 template <typename T, int NB, int R, bool kShared>
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a, int splits, float *parts, float2 *stats) {
+__global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void attend_kernel(AttendArgs a, int splits, float *parts, float2 *stats) {
     constexpr int D = 32 * NB;
     using State = Rows<T, NB, R>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -399,37 +422,41 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a, int splits, f
             // one may be outside, and the nearest is read in its place.
             const int group0 = lo_any / kCacheGroup, group1 = (hi_any - 1) / kCacheGroup;
             auto group_of = [&](int t, int u) { return min(max(2 * t + u, group0), group1); };
-            auto pages_of = [&](int t, int (&page)[2]) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) page[u] = table[group_of(t, u) >> gshift];
+            auto base_of = [&](int t, int u) {
+                const int g = group_of(t, u);
+                int64_t p = table[g >> gshift];
+                if (p < 0 || p >= a.cache.pages) bad = true, p = 0;
+                return a.cache.group(p, kh, g & ((1 << gshift) - 1));
             };
-            auto load = [&](int t, const int (&page)[2], Raw<NB> &x) {
+            // A step's keys and values are read into the registers of the
+            // step before as soon as those are free: the keys before the
+            // weights and the second product, the values after it.
+            if (t0 < t1) {
+                Raw<NB> x;
+                int64_t base[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int g = group_of(t, u);
-                    int64_t p = page[u];
-                    if (p < 0 || p >= a.cache.pages) bad = true, p = 0;
-                    load_group<NB>(a.cache.data + a.cache.group(p, kh, g & ((1 << gshift) - 1)), lane, u, x);
+                    base[u] = base_of(t0, u);
+                    load_keys<NB>(a.cache.data + base[u], lane, u, x);
+                    load_values<NB>(a.cache.data + base[u], lane, u, x);
                 }
-            };
-            if (t0 < t1) {
-                Raw<NB> x, next;
-                int page[2];
-                pages_of(t0, page);
-                load(t0, page, x);
-                pages_of(min(t0 + step, t1 - 1), page);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) base[u] = base_of(min(t0 + step, t1 - 1), u);
                 for (int t = t0; t < t1; t += step) {
-                    const bool more = t + step < t1;
-                    if (more) {
-                        load(t + step, page, next);
-                        pages_of(min(t + 2 * step, t1 - 1), page);
-                    }
+                    f32x4 s[R][2];
+                    u32x4 p[R][State::kP];
+                    st.scores(x, lane, s);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) load_keys<NB>(a.cache.data + base[u], lane, u, x);
                     const int first = t * kTile;
-                    if (first >= lo_all && first + kTile <= hi_all)
-                        st.template step<false>(x, first, lane, c);
-                    else
-                        st.template step<true>(x, first, lane, c);
-                    if (more) x = next;
+                    if (first < lo_all || first + kTile > hi_all) st.mask(x, first, lane, s);
+                    st.weights(s, c, p);
+                    st.add(x, p);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        load_values<NB>(a.cache.data + base[u], lane, u, x);
+                        base[u] = base_of(min(t + 2 * step, t1 - 1), u);
+                    }
                 }
             }
             if (bad) {
@@ -518,45 +545,65 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a, int splits, f
     }
 }
 
-// The splits' parts of every row, joined: a wave per row of D elements.
-template <typename T>
+// The splits' parts of every row, joined: a block per row, its threads
+// four elements of every (256 / (D / 4))th split each, so that the parts are
+// read at once (a wave per row, split after split: 51 us for 64 splits of 32
+// rows of 128).
+template <typename T, int NB>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int splits, const float *__restrict__ parts,
                                                    const float2 *__restrict__ stats) {
-    const int D = a.cache.dim, lane = threadIdx.x & 63;
+    constexpr int D = 32 * NB, kQuads = D / 4, kSlots = 256 / kQuads;
+    __shared__ float4 sums[kSlots][kQuads];
+    __shared__ float totals[kSlots];
+    const int quad = threadIdx.x % kQuads, slot = threadIdx.x / kQuads, lane = threadIdx.x & 63;
     const float c = a.scale * kLog2e;
     int64_t first = 0, end = a.tokens;
     if (a.starts) {  // rows behind the last sequence stay as they are
         first = min(max(static_cast<int64_t>(a.starts[0]), INT64_C(0)), a.tokens);
         end = min(max(static_cast<int64_t>(a.starts[a.sequences]), first), a.tokens);
     }
-    const int64_t rows = (end - first) * a.q_heads, all = a.tokens * a.q_heads;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); i < rows;
-         i += static_cast<int64_t>(gridDim.x) * 4) {
-        const int64_t row = first * a.q_heads + i;
-        float m = -INFINITY, sum = 0;
-        for (int s = 0; s < splits; ++s) m = fmaxf(m, stats[s * all + row].x);
-        float v[4] = {0, 0, 0, 0};
-        for (int s = 0; s < splits; ++s) {
-            const float2 x = stats[s * all + row];
-            if (x.x == -INFINITY && x.y == 0) continue;  // no keys
-            const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f((x.x - m) * c);
-            sum += f * x.y;
+    const int64_t all = a.tokens * a.q_heads;
+    for (int64_t row = first * a.q_heads + blockIdx.x; row < end * a.q_heads; row += gridDim.x) {
+        float m = -INFINITY;
+        for (int s = lane; s < splits; s += 64) m = fmaxf(m, stats[s * all + row].x);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (lane + 64 * j < D) v[j] += f * parts[(s * all + row) * D + lane + 64 * j];
+        for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+        float4 v = make_float4(0, 0, 0, 0);
+        float sum = 0;
+        if (slot < kSlots) {
+            for (int s = slot; s < splits; s += kSlots) {
+                const float2 x = stats[s * all + row];
+                if (x.x == -INFINITY && x.y == 0) continue;  // no keys
+                const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f((x.x - m) * c);
+                const float4 p = *reinterpret_cast<const float4 *>(parts + (s * all + row) * D + 4 * quad);
+                sum += f * x.y;
+                v.x += f * p.x, v.y += f * p.y, v.z += f * p.z, v.w += f * p.w;
+            }
+            sums[slot][quad] = v;
+            if (quad == 0) totals[slot] = sum;
         }
-        const float inv = sum == 0 ? 0.0f : 1.0f / sum;
-        const int64_t token = row / a.q_heads;
-        T *dst = static_cast<T *>(a.out.p) + token * a.out.token_stride +
-                 (row - token * a.q_heads) * a.out.head_stride;
+        __syncthreads();
+        if (slot == 0) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (lane + 64 * j >= D) continue;
-            if constexpr (sizeof(T) == 4)
-                dst[lane + 64 * j] = v[j] * inv;
-            else
-                dst[lane + 64 * j] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v[j] * inv));
+            for (int i = 1; i < kSlots; ++i) {
+                const float4 p = sums[i][quad];
+                v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+                sum += totals[i];
+            }
+            const float inv = sum == 0 ? 0.0f : 1.0f / sum;
+            const int64_t token = row / a.q_heads;
+            T *dst = static_cast<T *>(a.out.p) + token * a.out.token_stride +
+                     (row - token * a.q_heads) * a.out.head_stride + 4 * quad;
+            const float o[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(T) == 4)
+                    dst[j] = o[j];
+                else
+                    dst[j] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(o[j]));
+            }
         }
+        __syncthreads();
     }
 }
 
@@ -600,7 +647,7 @@ void launch(const AttendArgs &a, const Plan &p, float *parts, float2 *stats, hip
                                                                                                  stats);
         if (p.splits > 1) {
             const int64_t rows = a.tokens * a.q_heads;
-            join_kernel<T><<<static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, 1 << 20)), 256, 0, stream>>>(
+            join_kernel<T, NB><<<static_cast<unsigned>(std::min<int64_t>(rows, 1 << 20)), 256, 0, stream>>>(
                 a, p.splits, parts, stats);
         }
     } else {
