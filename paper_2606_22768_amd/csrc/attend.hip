@@ -91,7 +91,7 @@ struct Raw {
 };
 
 template <int N>
-struct __attribute__((packed, aligned(4))) Words {
+struct __attribute__((aligned(N % 4 == 0 ? 16 : N % 2 == 0 ? 8 : 4))) Words {
     uint32_t w[N];
 };
 
@@ -352,9 +352,6 @@ struct Place {
     int head;
 };
 
-// kShared: the block's four waves share 16 R rows and split their keys
-// between them (and the grid splits them again, where splits > 1); else each
-// wave has rows of its own.
 // Waves of a SIMD that the registers are kept few enough for: a row tile's
 // sums and queries, a step's codes and scales, and about 70 more.
 template <typename T, int NB, int R>
@@ -365,84 +362,96 @@ constexpr int kOccupancy = kRegisters<T, NB, R> <= 110   ? 4
                            : kRegisters<T, NB, R> <= 235 ? 2
                                                          : 1;
 
-template <typename T, int NB, int R, bool kShared>
-__global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void attend_kernel(AttendArgs a, int splits, float *parts, float2 *stats) {
-    constexpr int D = 32 * NB;
+// The keys that rows of a sequence see, from the first's first to the last's last.
+struct Keys {
+    int lo, hi;
+};
+__device__ inline Keys keys_of(const AttendArgs &a, const Span &s, int query0, int query1) {
+    const int past = s.length - s.n;  // keys before the first query's own
+    return {a.window > 0 ? max(max(past + query0 + 1, 0) - a.window, 0) : 0,
+            min(max(past + query1 + 1, 0), s.length)};
+}
+
+// A wave's rows from `row0`: its queries, and the keys that each sees.
+template <typename T, int NB, int R>
+__device__ inline void load_rows(const AttendArgs &a, const Span &seq, int kh, int group, int rows, int row0, int lane,
+                                 Rows<T, NB, R> &st, Place (&at)[R], bool (&real)[R]) {
+    st.clear();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + 16 * r + (lane & 15);
+        real[r] = row < rows;
+        const int i = real[r] ? row / group : 0;
+        at[r].token = seq.first + i;
+        at[r].head = kh * group + (real[r] ? row - i * group : 0);
+        const Keys k = keys_of(a, seq, i, i);
+        st.lo[r] = k.lo;
+        st.hi[r] = real[r] ? k.hi : 0;
+        st.load_query(r,
+                      static_cast<const T *>(a.q.p) + at[r].token * a.q.token_stride + at[r].head * a.q.head_stride,
+                      lane, real[r]);
+    }
+}
+
+// Where a step's two groups of 16 keys lie.  A group outside of what the rows
+// see is not read, but the nearest in its place; a bad page is not read
+// either.
+struct Groups {
+    const int32_t *table;
+    int first, last, shift;  // groups that hold keys which some row sees; groups of a page
+    int kh;
+    bool bad;
+    __device__ void aim(const CacheView &c, int t, int64_t (&base)[2]) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int g = min(max(2 * t + u, first), last);
+            int64_t p = table[g >> shift];
+            if (p < 0 || p >= c.pages) bad = true, p = 0;
+            base[u] = c.group(p, kh, g & ((1 << shift) - 1));
+        }
+    }
+};
+
+// Rows of their own for each wave, which goes through the keys by itself: its
+// four waves' rows are neighbours and read the same keys at about the same
+// time, from the first-level cache.  (From one ring in LDS, a barrier a step:
+// 473 us for 428 at 4 x 512 queries, 32 heads of 128 over 8 of 8192 keys.)
+template <typename T, int NB, int R>
+__global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(AttendArgs a) {
     using State = Rows<T, NB, R>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int group = a.q_heads / a.cache.heads, kh = blockIdx.y;
-    const int split = kShared ? blockIdx.x % splits : 0;
-    const int tiles_at_once = kShared ? gridDim.x / splits : gridDim.x * kWaves;
     const float c = a.scale * kLog2e;
-    const int gshift = a.cache.page_shift - 4;
     for (int b = blockIdx.z; b < a.sequences; b += gridDim.z) {
         const Span seq = span_of(a, b);
-        const int64_t rows = static_cast<int64_t>(seq.n) * group;
-        const int64_t row_tiles = (rows + 16 * R - 1) / (16 * R);
-        const int32_t *table = a.tables + b * a.table_stride;
-        for (int64_t tile = kShared ? blockIdx.x / splits : blockIdx.x * kWaves + wave; tile < row_tiles;
-             tile += tiles_at_once) {
+        const int rows = seq.n * group;  // the launcher holds tokens x q_heads below 2^31
+        const int row_tiles = (rows - 1) / (16 * R) + (rows > 0);
+        for (int tile = blockIdx.x * kWaves + wave; tile < row_tiles; tile += gridDim.x * kWaves) {
+            const int row0 = tile * 16 * R, row1 = min(rows - row0, 16 * R) + row0 - 1;
+            const Keys any = keys_of(a, seq, row0 / group, row1 / group);
+            const int lo_all = keys_of(a, seq, row1 / group, row1 / group).lo,
+                      hi_all = keys_of(a, seq, row0 / group, row0 / group).hi;
             State st;
-            st.clear();
-            int64_t row[R];
             Place at[R];
-            const int past = seq.length - seq.n;  // keys before the first query's own
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                row[r] = tile * (16 * R) + 16 * r + (lane & 15);
-                const bool real = row[r] < rows;
-                const int i = real ? static_cast<int>(row[r] / group) : 0;
-                at[r].token = seq.first + i;
-                at[r].head = kh * group + (real ? static_cast<int>(row[r] - static_cast<int64_t>(i) * group) : 0);
-                st.hi[r] = real ? min(max(past + i + 1, 0), seq.length) : 0;
-                st.lo[r] = a.window > 0 ? max(max(past + i + 1, 0) - a.window, 0) : 0;
-                st.load_query(r,
-                              static_cast<const T *>(a.q.p) + at[r].token * a.q.token_stride +
-                                  at[r].head * a.q.head_stride,
-                              lane, real);
-            }
-            // The keys that any of the rows sees, and those that all see.
-            const int64_t last_row = min(tile * (16 * R) + 16 * R, rows) - 1;
-            const int i0 = static_cast<int>(tile * (16 * R) / group), i1 = static_cast<int>(last_row / group);
-            const int lo_any = a.window > 0 ? max(max(past + i0 + 1, 0) - a.window, 0) : 0,
-                      hi_any = min(max(past + i1 + 1, 0), seq.length);
-            const int lo_all = a.window > 0 ? max(max(past + i1 + 1, 0) - a.window, 0) : 0, hi_all = past + i0 + 1;
-            int t0 = lo_any / kTile, t1 = (hi_any + kTile - 1) / kTile;
-            if (t1 < t0) t1 = t0;
-            int step = 1;
-            if (kShared) {
-                const int64_t n = t1 - t0;
-                const int e = t0 + static_cast<int>(n * (split + 1) / splits);
-                t0 += static_cast<int>(n * split / splits) + wave;
-                t1 = e;
-                step = kWaves;
-            }
-            bool bad = seq.bad;
-            // The groups that hold keys which some row sees: of a step's two
-            // one may be outside, and the nearest is read in its place.
-            const int group0 = lo_any / kCacheGroup, group1 = (hi_any - 1) / kCacheGroup;
-            auto group_of = [&](int t, int u) { return min(max(2 * t + u, group0), group1); };
-            auto base_of = [&](int t, int u) {
-                const int g = group_of(t, u);
-                int64_t p = table[g >> gshift];
-                if (p < 0 || p >= a.cache.pages) bad = true, p = 0;
-                return a.cache.group(p, kh, g & ((1 << gshift) - 1));
-            };
+            bool real[R];
+            load_rows(a, seq, kh, group, rows, row0, lane, st, at, real);
+            const int t0 = any.lo / kTile, t1 = (any.hi + kTile - 1) / kTile;
+            Groups groups = {a.tables + b * a.table_stride, any.lo / kCacheGroup, (any.hi - 1) / kCacheGroup,
+                             a.cache.page_shift - 4, kh, seq.bad};
             // A step's keys and values are read into the registers of the
             // step before as soon as those are free: the keys before the
             // weights and the second product, the values after it.
-            if (t0 < t1) {
+            if (any.lo < any.hi) {
                 Raw<NB> x;
                 int64_t base[2];
+                groups.aim(a.cache, t0, base);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    base[u] = base_of(t0, u);
                     load_keys<NB>(a.cache.data + base[u], lane, u, x);
                     load_values<NB>(a.cache.data + base[u], lane, u, x);
                 }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) base[u] = base_of(min(t0 + step, t1 - 1), u);
-                for (int t = t0; t < t1; t += step) {
+                groups.aim(a.cache, min(t0 + 1, t1 - 1), base);
+                for (int t = t0; t < t1; ++t) {
                     f32x4 s[R][2];
                     u32x4 p[R][State::kP];
                     st.scores(x, lane, s);
@@ -453,108 +462,303 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void attend_kernel(Att
                     st.weights(s, c, p);
                     st.add(x, p);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        load_values<NB>(a.cache.data + base[u], lane, u, x);
-                        base[u] = base_of(min(t + 2 * step, t1 - 1), u);
-                    }
+                    for (int u = 0; u < 2; ++u) load_values<NB>(a.cache.data + base[u], lane, u, x);
+                    groups.aim(a.cache, min(t + 2, t1 - 1), base);
                 }
             }
-            if (bad) {
-#pragma unroll
-                for (int r = 0; r < R; ++r) st.sum[r] = NAN;
-            }
-            float total[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                total[r] = st.sum[r] + __shfl_xor(st.sum[r], 16);
-                total[r] += __shfl_xor(total[r], 32);
+                float total = groups.bad ? NAN : st.sum[r];
+                total += __shfl_xor(total, 16);
+                total += __shfl_xor(total, 32);
                 st.poison[r] |= __shfl_xor(st.poison[r], 16);
                 st.poison[r] |= __shfl_xor(st.poison[r], 32);
-            }
-            const int d0 = 8 * (lane >> 4);  // within each block
-            if constexpr (!kShared) {
+                if (!real[r]) continue;
+                const float inv = total == 0 ? 0.0f : 1.0f / total;
+                T *dst = static_cast<T *>(a.out.p) + at[r].token * a.out.token_stride + at[r].head * a.out.head_stride +
+                         8 * (lane >> 4);
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if (row[r] >= rows) continue;
-                    const float inv = total[r] == 0 ? 0.0f : 1.0f / total[r];
-                    T *dst = static_cast<T *>(a.out.p) + at[r].token * a.out.token_stride +
-                             at[r].head * a.out.head_stride + d0;
+                for (int n = 0; n < NB; ++n) {
+                    float v[8];
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-                        float v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            v[i] = st.poison[r] >> n & 1 ? NAN : st.o[r][n][i & 1][i >> 1] * inv;
-                        store_eight(dst + 32 * n, v);
-                    }
+                    for (int i = 0; i < 8; ++i)
+                        v[i] = st.poison[r] >> n & 1 ? NAN : st.o[r][n][i & 1][i >> 1] * inv;
+                    store_eight(dst + 32 * n, v);
                 }
-            } else {
-                // The waves' parts are brought to one maximum and added.
-                static_assert(!kShared || R == 1, "waves that share rows have one tile of them");
-                __shared__ float all_m[kWaves][16], all_sum[kWaves][16];
-                __shared__ float all_o[kWaves][16][D + 4];
-                if (lane < 16) all_m[wave][lane] = st.m[0], all_sum[wave][lane] = total[0];
-                const bool real = row[0] < rows;
-                if (real) {
-#pragma unroll
-                    for (int n = 0; n < NB; ++n)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            all_o[wave][lane & 15][32 * n + d0 + i] =
-                                st.poison[0] >> n & 1 ? NAN : st.o[0][n][i & 1][i >> 1];
-                }
-                __syncthreads();
-                // A thread takes some of a row's elements.
-                constexpr int kPer = D / 16;
-                const int rr = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * kPer;
-                const int64_t rw = tile * 16 + rr;
-                if (rw < rows) {
-                    float m = all_m[0][rr], f[kWaves], sum = 0;
-#pragma unroll
-                    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, all_m[w][rr]);
-#pragma unroll
-                    for (int w = 0; w < kWaves; ++w) {
-                        f[w] = all_m[w][rr] == m ? 1.0f : __builtin_amdgcn_exp2f((all_m[w][rr] - m) * c);
-                        sum += f[w] * all_sum[w][rr];
-                    }
-                    const int i = static_cast<int>(rw / group);
-                    const int64_t token = seq.first + i;
-                    const int head = kh * group + static_cast<int>(rw - static_cast<int64_t>(i) * group);
-                    const float inv = splits > 1 ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
-                    const int64_t part = (split * a.tokens + token) * a.q_heads + head;
-                    if (splits > 1 && (threadIdx.x & 15) == 0) stats[part] = make_float2(m, sum);
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j) {
-                        float v = 0;
-#pragma unroll
-                        for (int w = 0; w < kWaves; ++w) v += f[w] * all_o[w][rr][e0 + j];
-                        v *= inv;
-                        if (splits > 1)
-                            parts[part * D + e0 + j] = v;
-                        else if constexpr (sizeof(T) == 4)
-                            static_cast<T *>(a.out.p)[token * a.out.token_stride + head * a.out.head_stride + e0 + j] =
-                                v;
-                        else
-                            static_cast<T *>(a.out.p)[token * a.out.token_stride + head * a.out.head_stride + e0 + j] =
-                                __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-                    }
-                }
-                __syncthreads();
             }
         }
     }
 }
 
-// The splits' parts of every row, joined: a block per row, its threads
-// four elements of every (256 / (D / 4))th split each, so that the parts are
-// read at once (a wave per row, split after split: 51 us for 64 splits of 32
-// rows of 128).
+// A step's two groups as they lie in the cache, in LDS, and how many steps
+// are on their way there: what fits beside the waves that the registers allow.
+template <int NB>
+constexpr int kStage = 2 * 544 * NB;
+template <int NB>
+constexpr int kSlots = NB <= 2 ? 4 : NB <= 4 ? 3 : 2;
+
+// LDS of a block: its waves' rings, or their parts of the output, and maxima and sums.
+template <int NB>
+constexpr int kLineLds = 512 + kWaves * (kStage<NB> * kSlots<NB> > 16 * (32 * NB + 4) * 4 ? kStage<NB> * kSlots<NB>
+                                                                                      : 16 * (32 * NB + 4) * 4);
+
+// Waits until at most N of this wave's loads are on their way.
+template <int N>
+__device__ inline void outstanding() {
+    static_assert(N < 64, "the counter's range");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | 15 << 8 | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
+}
+
+// All steps of a call in one line: sequence after sequence, its row tiles and
+// heads of keys one after the other (an item each), and an item's steps of 32
+// keys.  Each of `count` blocks takes an equal stretch of it, whatever the
+// sequences' lengths.  Beginning an item and joining its waves takes a block
+// about as long as kItemCost steps, which stand before its first one in the
+// line (without them 64 sequences of 500 to 8192 keys: blocks done after 55
+// to 106 us).
+struct Line {
+    int64_t total;  // steps
+    int count;      // blocks
+    __device__ int64_t from(int i) const { return total * i / count; }
+    __device__ int block_of(int64_t w) const { return static_cast<int>(((w + 1) * count - 1) / total); }
+};
+constexpr int kItemCost = 16;  // 64 sequences of 500 to 8192 keys: 86 us (8: 90, 12: 87, 24: 87, 40: 94)
+// The least stretch of a block: short calls have fewer blocks, each of which
+// costs the rest a part to join (17 sequences of up to 3001 keys, 5 queries
+// and a window of 1000: 13 us; 4: 14, 16: 15, 40: 23).
+constexpr int kLeast = 8;
+
+// An item's length for sequence s (a step where its rows see no key: they are
+// written as well), and its items.
+__device__ inline int length_of(const AttendArgs &a, const Span &s) {
+    const Keys k = keys_of(a, s, 0, s.n - 1);
+    return kItemCost + (k.lo < k.hi ? (k.hi + kTile - 1) / kTile - k.lo / kTile : 1);
+}
+__device__ inline int items_of(const AttendArgs &a, const Span &s, int group) {
+    return (s.n * group + 15) / 16 * a.cache.heads;
+}
+
+// Which blocks hold the parts of a row's output: `parts` of them from `first`
+// on (none: the output is written), as row `row` of their tiles.
+struct Parts16 {
+    int first, parts, row, pad;
+};
+
 template <typename T, int NB>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int splits, const float *__restrict__ parts,
-                                                   const float2 *__restrict__ stats) {
-    constexpr int D = 32 * NB, kQuads = D / 4, kSlots = 256 / kQuads;
-    __shared__ float4 sums[kSlots][kQuads];
-    __shared__ float totals[kSlots];
+__global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(AttendArgs a, float *parts, float2 *stats,
+                                                                          Parts16 *where) {
+    constexpr int D = 32 * NB;
+    using State = Rows<T, NB, 1>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kLineLds<NB> - 512];
+    __shared__ float all_m[kWaves][16], all_sum[kWaves][16];
+    auto all_o = reinterpret_cast<float(*)[16][D + 4]>(lds);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int group = a.q_heads / a.cache.heads;
+    const float c = a.scale * kLog2e;
+    // The line's length, 64 sequences at a time (the last 64 stay in registers).
+    Line line = {0, 0};
+    int64_t mine = 0;
+    for (int b = lane; b < (a.sequences + 63) / 64 * 64; b += 64) {
+        mine = 0;
+        if (b < a.sequences) {
+            const Span s = span_of(a, b);
+            mine = static_cast<int64_t>(items_of(a, s, group)) * length_of(a, s);
+        }
+        int64_t sum = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(static_cast<long long>(sum), o);
+        line.total += sum;
+    }
+    if (line.total == 0) return;
+    line.count = static_cast<int>(min(max(line.total / kLeast, INT64_C(1)), static_cast<int64_t>(gridDim.x)));
+    const int block = blockIdx.x;
+    if (block >= line.count) return;
+    int64_t w = line.from(block);
+    const int64_t w_end = line.from(block + 1);
+    // The sequence that w is in, and where that begins.
+    int b = 0;
+    int64_t begin = 0;
+    for (int b0 = 0; b0 < a.sequences; b0 += 64) {
+        if (a.sequences > 64) {
+            mine = 0;
+            if (b0 + lane < a.sequences) {
+                const Span s = span_of(a, b0 + lane);
+                mine = static_cast<int64_t>(items_of(a, s, group)) * length_of(a, s);
+            }
+        }
+        int64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t v = __shfl_up(static_cast<long long>(upto), o);
+            if (lane >= o) upto += v;
+        }
+        const uint64_t past = __ballot(begin + upto > w);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            b = b0 + l;
+            begin += __shfl(static_cast<long long>(upto - mine), l);
+            break;
+        }
+        begin += __shfl(static_cast<long long>(upto), 63);
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    while (w < w_end) {
+        const Span seq = span_of(a, b);
+        const int length = length_of(a, seq), items = items_of(a, seq, group), rows = seq.n * group;
+        const int64_t of_sequence = static_cast<int64_t>(items) * length;
+        if (w >= begin + of_sequence) {  // its rows are through, or it has none
+            begin += of_sequence;
+            ++b;
+            continue;
+        }
+        const int item = static_cast<int>((w - begin) / length), kh = item % a.cache.heads, row0 = item / a.cache.heads * 16;
+        const int64_t item_begin = begin + static_cast<int64_t>(item) * length;
+        // The block's steps of the item, [n0, n1).
+        const int n0 = max(static_cast<int>(w - item_begin) - kItemCost, 0),
+                  n1 = static_cast<int>(min(w_end - item_begin, static_cast<int64_t>(length))) - kItemCost;
+        w = min(w_end, item_begin + length);
+        if (n0 >= n1) continue;
+        const int row1 = min(rows - row0, 16) + row0 - 1;
+        const Keys all = keys_of(a, seq, 0, seq.n - 1), any = keys_of(a, seq, row0 / group, row1 / group);
+        const int lo_all = keys_of(a, seq, row1 / group, row1 / group).lo,
+                  hi_all = keys_of(a, seq, row0 / group, row0 / group).hi;
+        // This wave's steps: every fourth of the block's.
+        const int t0 = all.lo / kTile + n0 + wave, t1 = all.lo / kTile + n1;
+        Groups groups = {a.tables + b * a.table_stride, any.lo / kCacheGroup, (any.hi - 1) / kCacheGroup,
+                         a.cache.page_shift - 4, kh, seq.bad};
+        // Copies a step straight to LDS, 16 bytes a lane, as it lies.  Past
+        // the last step that one is copied again (a branch around the loads
+        // would cost more).
+        constexpr int kGroupChunks = 34 * NB, kLoads = (2 * kGroupChunks + 63) / 64;
+        uint8_t *ring = lds + wave * kStage<NB> * kSlots<NB>;
+        int64_t base[2];
+        auto fetch = [&](int slot) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int chunk = i * 64 + lane;
+                const bool second = chunk >= kGroupChunks;
+                const uint8_t *src = a.cache.data + (second ? base[1] : base[0]) +
+                                     (chunk - (second ? kGroupChunks : 0)) * 16;
+                if (chunk < 2 * kGroupChunks)
+                    __builtin_amdgcn_global_load_lds(
+                        (const __attribute__((address_space(1))) void *)src,
+                        (__attribute__((address_space(3))) void *)(ring + slot * kStage<NB> + i * 1024), 16, 0, 0);
+            }
+        };
+        const bool work = any.lo < any.hi && t0 < t1;
+        if (work) {
+#pragma unroll
+            for (int i = 0; i < kSlots<NB>; ++i) {
+                groups.aim(a.cache, min(t0 + i * kWaves, t1 - 1), base);
+                fetch(i);
+            }
+            groups.aim(a.cache, min(t0 + kSlots<NB> * kWaves, t1 - 1), base);
+        }
+        State st;
+        Place at[1];
+        bool real[1];
+        load_rows(a, seq, kh, group, rows, row0, lane, st, at, real);
+        if (work) {
+            outstanding<0>();  // the queries are not counted below
+            int slot = 0;
+            for (int t = t0; t < t1; t += kWaves) {
+                outstanding<(kSlots<NB> - 1) * kLoads>();
+                const uint8_t *stage = ring + slot * kStage<NB>;
+                Raw<NB> x;
+                f32x4 s[1][2];
+                u32x4 p[1][State::kP];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) load_keys<NB>(stage + u * 544 * NB, lane, u, x);
+                st.scores(x, lane, s);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) load_values<NB>(stage + u * 544 * NB, lane, u, x);
+                const int first = t * kTile;
+                if (first < lo_all || first + kTile > hi_all) st.mask(x, first, lane, s);
+                st.weights(s, c, p);
+                // The step is in registers: its slot is free.
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch(slot);
+                groups.aim(a.cache, min(t + (kSlots<NB> + 1) * kWaves, t1 - 1), base);
+                st.add(x, p);
+                slot = slot == kSlots<NB> - 1 ? 0 : slot + 1;
+            }
+            outstanding<0>();  // the ring's memory is used again
+        }
+        // The waves' parts are brought to one maximum and added.
+        float total = groups.bad ? NAN : st.sum[0];
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        st.poison[0] |= __shfl_xor(st.poison[0], 16);
+        st.poison[0] |= __shfl_xor(st.poison[0], 32);
+        if (lane < 16) all_m[wave][lane] = st.m[0], all_sum[wave][lane] = total;
+        __syncthreads();  // all waves are through with their rings
+        if (real[0]) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float4 *dst = reinterpret_cast<float4 *>(&all_o[wave][lane & 15][32 * n + 8 * (lane >> 4)]);
+                const bool nan = st.poison[0] >> n & 1;
+                const f32x4 e = st.o[0][n][0], o = st.o[0][n][1];
+                dst[0] = nan ? make_float4(NAN, NAN, NAN, NAN) : make_float4(e[0], o[0], e[1], o[1]);
+                dst[1] = nan ? make_float4(NAN, NAN, NAN, NAN) : make_float4(e[2], o[2], e[3], o[3]);
+            }
+        }
+        __syncthreads();
+        // A thread takes some of a row's elements.
+        constexpr int kPer = D / 16;
+        const int rr = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * kPer, rw = row0 + rr;
+        const bool whole = n0 == 0 && n1 == length - kItemCost;
+        if (rw < rows) {
+            float m = all_m[0][rr], f[kWaves], sum = 0;
+#pragma unroll
+            for (int v = 1; v < kWaves; ++v) m = fmaxf(m, all_m[v][rr]);
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) {
+                f[v] = all_m[v][rr] == m ? 1.0f : __builtin_amdgcn_exp2f((all_m[v][rr] - m) * c);
+                sum += f[v] * all_sum[v][rr];
+            }
+            const int i = rw / group;
+            const int64_t token = seq.first + i;
+            const int head = kh * group + rw - i * group;
+            const int64_t slot = (2 * block + (n0 == 0)) * 16 + rr;  // where a part goes
+            if ((threadIdx.x & 15) == 0) {
+                if (!whole) stats[slot] = make_float2(m, sum);
+                if (n0 == 0)
+                    where[token * a.q_heads + head] =
+                        Parts16{block, whole ? 0 : line.block_of(item_begin + length - 1) - block + 1, rr, 0};
+            }
+            const float inv = !whole ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
+            T *dst = static_cast<T *>(a.out.p) + token * a.out.token_stride + head * a.out.head_stride + e0;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                float v = 0;
+#pragma unroll
+                for (int u = 0; u < kWaves; ++u) v += f[u] * all_o[u][rr][e0 + j];
+                v *= inv;
+                if (!whole)
+                    parts[slot * D + e0 + j] = v;
+                else if constexpr (sizeof(T) == 4)
+                    dst[j] = v;
+                else
+                    dst[j] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Rows whose items several blocks share, joined: a block per row, its threads
+// four elements of every (256 / (D / 4))th part each, so that the parts are
+// read at once (a wave per row, part after part: 51 us for 64 parts of 32 rows
+// of 128).
+template <typename T, int NB>
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, const float *__restrict__ parts,
+                                                   const float2 *__restrict__ stats,
+                                                   const Parts16 *__restrict__ where) {
+    constexpr int D = 32 * NB, kQuads = D / 4, kJoinSlots = 256 / kQuads;
+    __shared__ float4 sums[kJoinSlots][kQuads];
+    __shared__ float totals[kJoinSlots];
     const int quad = threadIdx.x % kQuads, slot = threadIdx.x / kQuads, lane = threadIdx.x & 63;
     const float c = a.scale * kLog2e;
     int64_t first = 0, end = a.tokens;
@@ -562,22 +766,26 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int splits, con
         first = min(max(static_cast<int64_t>(a.starts[0]), INT64_C(0)), a.tokens);
         end = min(max(static_cast<int64_t>(a.starts[a.sequences]), first), a.tokens);
     }
-    const int64_t all = a.tokens * a.q_heads;
     for (int64_t row = first * a.q_heads + blockIdx.x; row < end * a.q_heads; row += gridDim.x) {
+        const Parts16 at = where[row];
+        if (at.parts == 0) continue;
+        auto part = [&](int i) { return (2 * static_cast<int64_t>(at.first + i) + (i == 0)) * 16 + at.row; };
         float m = -INFINITY;
-        for (int s = lane; s < splits; s += 64) m = fmaxf(m, stats[s * all + row].x);
+        for (int i = lane; i < at.parts; i += 64) m = fmaxf(m, stats[part(i)].x);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
         float4 v = make_float4(0, 0, 0, 0);
         float sum = 0;
-        if (slot < kSlots) {
-            for (int s = slot; s < splits; s += kSlots) {
-                const float2 x = stats[s * all + row];
-                if (x.x == -INFINITY && x.y == 0) continue;  // no keys
+        if (slot < kJoinSlots) {
+#pragma unroll 4
+            for (int i = slot; i < at.parts; i += kJoinSlots) {
+                const int64_t p = part(i);
+                const float2 x = stats[p];
+                const float4 y = *reinterpret_cast<const float4 *>(parts + p * D + 4 * quad);
+                // A part that saw no key has a maximum of -inf, and zeros.
                 const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f((x.x - m) * c);
-                const float4 p = *reinterpret_cast<const float4 *>(parts + (s * all + row) * D + 4 * quad);
                 sum += f * x.y;
-                v.x += f * p.x, v.y += f * p.y, v.z += f * p.z, v.w += f * p.w;
+                v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
             }
             sums[slot][quad] = v;
             if (quad == 0) totals[slot] = sum;
@@ -585,7 +793,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int splits, con
         __syncthreads();
         if (slot == 0) {
 #pragma unroll
-            for (int i = 1; i < kSlots; ++i) {
+            for (int i = 1; i < kJoinSlots; ++i) {
                 const float4 p = sums[i][quad];
                 v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
                 sum += totals[i];
@@ -608,12 +816,37 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int splits, con
 }
 
 struct Plan {
-    bool shared;
-    int splits, tiles;  // splits of the keys; row tiles (of 16 or 32 rows) of a sequence that the grid covers at once
-    size_t parts_bytes, stats_bytes;
+    bool own;        // waves have rows of their own
+    int64_t tiles;   // own: row tiles (of 32 rows) of a sequence that the grid covers at once
+    int blocks;      // else: of the line
+    int64_t parts_bytes, stats_bytes, where_bytes;
 };
 
 constexpr int kOwnTiles = 2;  // R of waves with rows of their own
+
+// Blocks of a line that the card holds at once, by their registers and LDS.
+template <typename T, int NB>
+constexpr int kLineBlocks = 256 * std::min(kOccupancy<T, NB, 1>, 163840 / kLineLds<NB>);
+int line_blocks(const AttendArgs &a) {
+    switch (a.cache.dim / 32 * 2 + a.bf16) {
+        case 2: return kLineBlocks<float, 1>;
+        case 3: return kLineBlocks<uint16_t, 1>;
+        case 4: return kLineBlocks<float, 2>;
+        case 5: return kLineBlocks<uint16_t, 2>;
+        case 6: return kLineBlocks<float, 3>;
+        case 7: return kLineBlocks<uint16_t, 3>;
+        case 8: return kLineBlocks<float, 4>;
+        case 9: return kLineBlocks<uint16_t, 4>;
+        case 10: return kLineBlocks<float, 5>;
+        case 11: return kLineBlocks<uint16_t, 5>;
+        case 12: return kLineBlocks<float, 6>;
+        case 13: return kLineBlocks<uint16_t, 6>;
+        case 14: return kLineBlocks<float, 7>;
+        case 15: return kLineBlocks<uint16_t, 7>;
+        case 16: return kLineBlocks<float, 8>;
+        default: return kLineBlocks<uint16_t, 8>;
+    }
+}
 
 Plan plan_of(const AttendArgs &a) {
     Plan p{};
@@ -621,72 +854,65 @@ Plan plan_of(const AttendArgs &a) {
     const int64_t rows = std::max<int64_t>(1, a.most_queries) * group;
     const int64_t seqs = std::max(1, a.sequences), heads = a.cache.heads;
     const int64_t own = (rows + 16 * kOwnTiles - 1) / (16 * kOwnTiles);
-    p.shared = own * heads * seqs < 1024;
-    p.splits = 1;
-    if (!p.shared) {
-        p.tiles = static_cast<int>(std::min<int64_t>(own, 1 << 20));
+    p.own = rows > 16 && own * heads * seqs >= 1024;
+    if (p.own) {
+        p.tiles = std::min<int64_t>(own, 1 << 20);
         return p;
     }
-    p.tiles = static_cast<int>((rows + 15) / 16);
-    const int64_t blocks = p.tiles * heads * seqs;
-    const int64_t keys = static_cast<int64_t>(a.width) << a.cache.page_shift;
-    const int64_t most = std::max<int64_t>(1, keys / (kTile * kWaves * 2));
-    p.splits = static_cast<int>(std::clamp<int64_t>(768 / blocks, 1, std::min<int64_t>(most, 64)));
-    if (p.splits > 1) {
-        p.parts_bytes = static_cast<size_t>(p.splits) * a.tokens * a.q_heads * a.cache.dim * 4;
-        p.stats_bytes = static_cast<size_t>(p.splits) * a.tokens * a.q_heads * 8;
-    }
+    p.blocks = line_blocks(a);
+    p.parts_bytes = static_cast<int64_t>(p.blocks) * 2 * 16 * a.cache.dim * 4;
+    p.stats_bytes = static_cast<int64_t>(p.blocks) * 2 * 16 * 8;
+    p.where_bytes = a.tokens * a.q_heads * static_cast<int64_t>(sizeof(Parts16));
     return p;
 }
 
 template <typename T, int NB>
-void launch(const AttendArgs &a, const Plan &p, float *parts, float2 *stats, hipStream_t stream) {
-    const unsigned z = std::min(a.sequences, 65535);
-    if (p.shared) {
-        attend_kernel<T, NB, 1, true><<<dim3(p.splits * p.tiles, a.cache.heads, z), 256, 0, stream>>>(a, p.splits, parts,
-                                                                                                 stats);
-        if (p.splits > 1) {
-            const int64_t rows = a.tokens * a.q_heads;
-            join_kernel<T, NB><<<static_cast<unsigned>(std::min<int64_t>(rows, 1 << 20)), 256, 0, stream>>>(
-                a, p.splits, parts, stats);
-        }
-    } else {
+void launch(const AttendArgs &a, const Plan &p, char *workspace, hipStream_t stream) {
+    if (p.own) {
         constexpr int R = sizeof(T) == 4 ? 1 : kOwnTiles;
         const unsigned x = static_cast<unsigned>((p.tiles * (kOwnTiles / R) + kWaves - 1) / kWaves);
-        attend_kernel<T, NB, R, false><<<dim3(x, a.cache.heads, z), 256, 0, stream>>>(a, 1, nullptr, nullptr);
+        rows_kernel<T, NB, R>
+            <<<dim3(x, a.cache.heads, static_cast<unsigned>(std::min(a.sequences, 65535))), 256, 0, stream>>>(a);
+        return;
     }
+    auto *parts = reinterpret_cast<float *>(workspace);
+    auto *stats = reinterpret_cast<float2 *>(workspace + p.parts_bytes);
+    auto *where = reinterpret_cast<Parts16 *>(workspace + p.parts_bytes + p.stats_bytes);
+    line_kernel<T, NB><<<p.blocks, 256, 0, stream>>>(a, parts, stats, where);
+    const int64_t rows = a.tokens * a.q_heads;
+    join_kernel<T, NB>
+        <<<static_cast<unsigned>(std::min<int64_t>(rows, 1 << 20)), 256, 0, stream>>>(a, parts, stats, where);
 }
 
 template <typename T>
-void launch(const AttendArgs &a, const Plan &p, float *parts, float2 *stats, hipStream_t stream) {
+void launch(const AttendArgs &a, const Plan &p, char *workspace, hipStream_t stream) {
     switch (a.cache.dim / 32) {
-        case 1: return launch<T, 1>(a, p, parts, stats, stream);
-        case 2: return launch<T, 2>(a, p, parts, stats, stream);
-        case 3: return launch<T, 3>(a, p, parts, stats, stream);
-        case 4: return launch<T, 4>(a, p, parts, stats, stream);
-        case 5: return launch<T, 5>(a, p, parts, stats, stream);
-        case 6: return launch<T, 6>(a, p, parts, stats, stream);
-        case 7: return launch<T, 7>(a, p, parts, stats, stream);
-        default: return launch<T, 8>(a, p, parts, stats, stream);
+        case 1: return launch<T, 1>(a, p, workspace, stream);
+        case 2: return launch<T, 2>(a, p, workspace, stream);
+        case 3: return launch<T, 3>(a, p, workspace, stream);
+        case 4: return launch<T, 4>(a, p, workspace, stream);
+        case 5: return launch<T, 5>(a, p, workspace, stream);
+        case 6: return launch<T, 6>(a, p, workspace, stream);
+        case 7: return launch<T, 7>(a, p, workspace, stream);
+        default: return launch<T, 8>(a, p, workspace, stream);
     }
 }
 
 }  // namespace
 
 int64_t attend_workspace_bytes(const AttendArgs &a) {
+    if (a.sequences == 0 || a.tokens == 0) return 0;
     const Plan p = plan_of(a);
-    return static_cast<int64_t>(p.parts_bytes + p.stats_bytes);
+    return p.parts_bytes + p.stats_bytes + p.where_bytes;
 }
 
 bool attend_launch(const AttendArgs &a, void *workspace, hipStream_t stream) {
     if (a.sequences == 0 || a.tokens == 0) return true;
     const Plan p = plan_of(a);
-    auto *parts = static_cast<float *>(workspace);
-    auto *stats = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.parts_bytes);
     if (a.bf16)
-        launch<uint16_t>(a, p, parts, stats, stream);
+        launch<uint16_t>(a, p, static_cast<char *>(workspace), stream);
     else
-        launch<float>(a, p, parts, stats, stream);
+        launch<float>(a, p, static_cast<char *>(workspace), stream);
     return hipGetLastError() == hipSuccess;
 }
 

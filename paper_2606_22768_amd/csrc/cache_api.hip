@@ -94,7 +94,7 @@ fgd_status check_attention(const fgd_mx4_cache *cache, const fgd_attention *s, b
         return api_fail(FGD_ERR_INVALID_ARG, "table_width times page must be below 2^31");
     if (cache->pages == 0 && s->table_width > 0)
         return api_fail(FGD_ERR_INVALID_ARG, "a cache without pages has tables of width 0 only");
-    if (static_cast<fgd::wide>(s->tokens) * s->q_heads * cache->head_dim >= fgd::kMostBytes / 1024)
+    if (s->tokens * s->q_heads > INT32_MAX)
         return api_fail(FGD_ERR_INVALID_ARG, "attention: sizes are too large");
     a->tokens = s->tokens;
     a->sequences = s->sequences;

@@ -158,15 +158,16 @@ def test_exact_where_one_key_is_seen(env, shared, dtype):
     fgd, torch = env
     n = 3 if shared else 70
     b = Batch(env, [40] * n, [5] * n, 16, 16, 96, 16, dtype, seed=9)
-    got = _np(b.run(window=1, max_q=5))
+    got = _np(b.run(window=1, max_q=5 if shared else 40))
     for i in range(n):
         assert np.array_equal(got[5 * i:5 * i + 5], b.v[i][35:])
+
     # All keys equal: the mean of values that are whole numbers.
     def keys(_, k, v):
         k[:] = k[:1]
         v[:] = torch.randint(-2, 3, v.shape).float().cuda() * 2
     b = Batch(env, [64] * n, [1] * n, 16, 16, 96, 16, dtype, seed=9, keys=keys)
-    got = _np(b.run(starts=False))
+    got = _np(b.run(max_q=1 if shared else 40))
     for i in range(n):
         assert np.array_equal(got[i], _round(torch, b.v[i].mean(0), dtype))
 
@@ -243,16 +244,17 @@ def test_bad_pages_and_lengths(env, shared):
     fgd, torch = env
     n = 4 if shared else 70
     b = Batch(env, [50] * n, [1] * n, 16, 16, 64, 16, seed=6, spare=1)
-    want = _np(b.run(starts=False))
+    most = 1 if shared else 40
+    want = _np(b.run(max_q=most))
     b.tables[1, 2] = -1
     b.tables[2, 0] = b.cache.pages
     b.lengths[3] = 5 * 16 + 1  # past its table
-    got = _np(b.run(starts=False))
+    got = _np(b.run(max_q=most))
     assert np.isnan(got[1:4]).all()
     assert np.array_equal(got[0], want[0]) and np.array_equal(got[4:], want[4:])
-    assert np.isfinite(_np(b.run(starts=False, window=2))[1:3]).all()  # the bad page is not among those it needs
+    assert np.isfinite(_np(b.run(max_q=most, window=2))[1:3]).all()  # the bad page is not among those it needs
     b.lengths[3] = -3
-    assert (_np(b.run(starts=False))[3] == 0).all()
+    assert (_np(b.run(max_q=most))[3] == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
