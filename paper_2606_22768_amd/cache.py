@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 
 from . import DTYPES, FGD_F32, _check, _dev, _stream, lib
-from .heads import _array, _axes, _heads
+from .heads import _array, _at, _form, _heads, _keep, _known
 from .mx4 import _check_workspace, _current, _on, _on_gpu
 
 _I64 = ctypes.c_int64
@@ -118,7 +118,7 @@ class Mx4Cache:
     (uint8, laid out as fgd.h says), allocated when not given; its bytes need
     no initial value."""
 
-    __slots__ = ("data", "pages", "page", "heads", "dim", "_c")
+    __slots__ = ("data", "pages", "page", "heads", "dim", "_c", "_form")
 
     def __init__(self, pages, page, heads, dim, device=None, data=None):
         import torch
@@ -134,6 +134,7 @@ class Mx4Cache:
                 raise ValueError(f"data: expected {need} bytes, got {data.numel()}")
         self.data, self.pages, self.page, self.heads, self.dim = data, pages, page, heads, dim
         self._c = fgd_mx4_cache(page, heads, dim, pages, data.data_ptr())
+        self._form = (pages, page, heads, dim, data.device)
 
     @property
     def device(self):
@@ -146,6 +147,9 @@ class Mx4Cache:
     def __repr__(self):
         return (f"Mx4Cache(pages={self.pages}, page={self.page}, heads={self.heads}, dim={self.dim}, "
                 f"device={self.device})")
+
+
+_SETTINGS = (type(None), float, int)  # of which equal values mean equal calls
 
 
 def _is_cache(c):
@@ -178,6 +182,18 @@ def mx4_cache_write(cache, k, v, slots, stream=None):
     page s // page).  A slot outside the cache, as -1, is passed over; slots
     that are written must differ."""
     _is_cache(cache)
+    key = None
+    if stream is None:
+        try:
+            key = (cache._form, _form(k), _form(v), _form(slots), "write")
+            plan = _known(key)
+        except AttributeError:  # no tensors: the checks say so
+            key = plan = None
+        if plan is not None:
+            index, code, T, kt, kh, vt, vh = plan
+            _check(lib.fgd_mx4_cache_write(ctypes.byref(cache._c), k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, code, T,
+                                           slots.data_ptr(), _current(index)), "fgd_mx4_cache_write")
+            return
     code, T, heads = _tokens("k", k, cache)
     _tokens("v", v, cache, k)
     for name, t in (("k", k), ("v", v)):
@@ -189,6 +205,8 @@ def mx4_cache_write(cache, k, v, slots, stream=None):
     with _on(cache.device, stream):
         fgd_mx4_cache_write(cache._c, k, k.stride(0), k.stride(1), v, v.stride(0), v.stride(1), code, T, slots,
                             _current(cache.device))
+    if key is not None:
+        _keep(key, cache.device.index, code, T, k.stride(0), k.stride(1), v.stride(0), v.stride(1))
 
 
 def mx4_cache_read(cache, slots, dtype="f32", stream=None):
@@ -206,7 +224,8 @@ def mx4_cache_read(cache, slots, dtype="f32", stream=None):
     _slots(slots, T, cache.device)
     _on_gpu("cache", cache.data, None)
     with _on(cache.device, stream):
-        k, v = (torch.empty((T, cache.heads, cache.dim), dtype=t, device=cache.device) for _ in range(2))
+        both = torch.empty((2, T, cache.heads, cache.dim), dtype=t, device=cache.device)
+        k, v = both.unbind()
         fgd_mx4_cache_read(cache._c, slots, T, k, k.stride(0), k.stride(1), v, v.stride(0), v.stride(1),
                            "f32" if t == torch.float32 else "bf16", _current(cache.device))
     return k, v
@@ -256,6 +275,22 @@ def mx4_attend(q, cache, tables, lengths, starts=None, max_q=None, scale=None, w
     import torch
 
     _is_cache(cache)
+    key = None
+    if out is None and workspace is None and stream is None and type(window) is int and \
+            type(scale) in _SETTINGS and type(max_q) in _SETTINGS:
+        try:
+            key = (cache._form, _form(q), _form(tables), _form(lengths), _form(starts), max_q, scale, window, "attend")
+            plan = _known(key)
+        except AttributeError:  # no tensors: the checks say so
+            key = plan = None
+        if plan is not None:
+            index, sizes, need, qt, qh, stride, ot, oh = plan
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            work = q.new_empty(need, dtype=torch.uint8) if need else None
+            _check(lib.fgd_mx4_attend(ctypes.byref(cache._c), ctypes.byref(sizes), q.data_ptr(), qt, qh,
+                                      tables.data_ptr(), stride, lengths.data_ptr(), _at(starts), out.data_ptr(), ot,
+                                      oh, _at(work), need, _current(index)), "fgd_mx4_attend")
+            return out
     code, T, heads = _tokens("q", q, cache)
     dev = cache.device
     if heads == 0 or heads % cache.heads:
@@ -290,10 +325,20 @@ def mx4_attend(q, cache, tables, lengths, starts=None, max_q=None, scale=None, w
         fgd_mx4_attend(cache._c, sizes, q, q.stride(0), q.stride(1), tables, stride, lengths, starts, out,
                        out.stride(0), out.stride(1), workspace,
                        0 if workspace is None else workspace.numel() * workspace.element_size(), _current(dev))
+    if key is not None:
+        _keep(key, dev.index, sizes, need, q.stride(0), q.stride(1), stride, out.stride(0), out.stride(1))
     return out
 
 
+def _state(plan, tables, lengths, free, free_count):
+    """The C structure of a plan's sizes with these arrays."""
+    page, B, W, stride, capacity = plan
+    return fgd_pages(page, B, W, stride, tables.data_ptr(), lengths.data_ptr(), free.data_ptr(), free_count.data_ptr(),
+                     capacity)
+
+
 def _pages(tables, lengths, free, free_count, page):
+    """(device, requests, sizes) of the state, checked."""
     import torch
 
     if not isinstance(lengths, torch.Tensor):
@@ -305,8 +350,7 @@ def _pages(tables, lengths, free, free_count, page):
     if free.dim() != 1:
         raise ValueError(f"free: expected one axis, got shape {tuple(free.shape)}")
     _ints("free_count", free_count, 1, dev)
-    return dev, B, fgd_pages(_int("page", page, 1, 0x7fffffff), B, W, stride, tables.data_ptr(),
-                             lengths.data_ptr(), free.data_ptr(), free_count.data_ptr(), free.shape[0])
+    return dev, B, (_int("page", page, 1, 0x7fffffff), B, W, stride, free.shape[0])
 
 
 def extend_pages(tables, lengths, counts, free, free_count, page, tokens, stream=None):
@@ -320,7 +364,22 @@ def extend_pages(tables, lengths, counts, free, free_count, page, tokens, stream
     positions are 0 and slots -1, which mx4_cache_write passes over."""
     import torch
 
-    dev, B, pages = _pages(tables, lengths, free, free_count, page)
+    key = None
+    if stream is None and type(page) is int and type(tokens) is int:
+        try:
+            key = (_form(tables), _form(lengths), _form(counts), _form(free), _form(free_count), page, tokens, "extend")
+            plan = _known(key)
+        except AttributeError:  # no tensors: the checks say so
+            key = plan = None
+        if plan is not None:
+            index, B, sizes = plan
+            starts, positions, slots = counts.new_empty(B + 1), counts.new_empty(tokens), \
+                counts.new_empty(tokens, dtype=torch.int64)
+            _check(lib.fgd_extend_pages(ctypes.byref(_state(sizes, tables, lengths, free, free_count)),
+                                        counts.data_ptr(), tokens, starts.data_ptr(), positions.data_ptr(),
+                                        slots.data_ptr(), _current(index)), "fgd_extend_pages")
+            return starts, positions, slots
+    dev, B, sizes = _pages(tables, lengths, free, free_count, page)
     _ints("counts", counts, B, dev)
     tokens = _int("tokens", tokens, 0, 0x7fffffff)
     _on_gpu("lengths", lengths, None)
@@ -328,7 +387,10 @@ def extend_pages(tables, lengths, counts, free, free_count, page, tokens, stream
         starts = torch.empty(B + 1, dtype=torch.int32, device=dev)
         positions = torch.empty(tokens, dtype=torch.int32, device=dev)
         slots = torch.empty(tokens, dtype=torch.int64, device=dev)
-        fgd_extend_pages(pages, counts, tokens, starts, positions, slots, _current(dev))
+        fgd_extend_pages(_state(sizes, tables, lengths, free, free_count), counts, tokens, starts, positions, slots,
+                         _current(dev))
+    if key is not None:
+        _keep(key, dev.index, B, sizes)
     return starts, positions, slots
 
 
@@ -336,8 +398,22 @@ def truncate_pages(tables, lengths, keep, free, free_count, page, stream=None):
     """Shortens requests to keep[b] (int32 [B]) tokens, in place: 0 for one that
     is done, its length or more for one that stays as it is.  Pages without a
     token left go back on the stack, their entries in tables become -1."""
-    dev, B, pages = _pages(tables, lengths, free, free_count, page)
+    key = None
+    if stream is None and type(page) is int:
+        try:
+            key = (_form(tables), _form(lengths), _form(keep), _form(free), _form(free_count), page, "truncate")
+            plan = _known(key)
+        except AttributeError:  # no tensors: the checks say so
+            key = plan = None
+        if plan is not None:
+            index, sizes = plan
+            _check(lib.fgd_truncate_pages(ctypes.byref(_state(sizes, tables, lengths, free, free_count)),
+                                          keep.data_ptr(), _current(index)), "fgd_truncate_pages")
+            return
+    dev, B, sizes = _pages(tables, lengths, free, free_count, page)
     _ints("keep", keep, B, dev)
     _on_gpu("lengths", lengths, None)
     with _on(dev, stream):
-        fgd_truncate_pages(pages, keep, _current(dev))
+        fgd_truncate_pages(_state(sizes, tables, lengths, free, free_count), keep, _current(dev))
+    if key is not None:
+        _keep(key, dev.index, sizes)

@@ -183,11 +183,16 @@ def _on(device, stream=None):
 
 
 def _current(device):
-    """torch's current stream on `device` (its number spares torch a search for
-    the current one, which takes longer than the rest of a call)."""
+    """torch's current stream on `device`, a torch device or its number (which
+    spares torch a search for the current one, which takes longer than the rest
+    of a call)."""
     import torch
 
-    return torch.cuda.current_stream(device.index).cuda_stream
+    index = device if type(device) is int else device.index
+    try:
+        return torch._C._cuda_getCurrentRawStream(index)  # 0.1 us; the stream's object takes 1.1
+    except AttributeError:  # a torch without it
+        return torch.cuda.current_stream(index).cuda_stream
 
 
 def _is_mx4(q, name):
