@@ -178,19 +178,35 @@ struct Rows {
                 }
                 const u32x4 a = {fp4_pair<0>(x.k[u][p], scale), fp4_pair<1>(x.k[u][p], scale),
                                  fp4_pair<2>(x.k[u][p], scale), fp4_pair<3>(x.k[u][p], scale)};
-#pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int j = kQ - 1; j >= 0; --j) s[r][u] = mfma(a, q[r][j][p], s[r][u]);
+                score(a, p, s, u);
             }
         }
+    }
+
+    // Adds the products of piece p of a group's keys to its scores.
+    __device__ void score(const u32x4 &k, int p, f32x4 (&s)[R][2], int u) const {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = kQ - 1; j >= 0; --j) s[r][u] = mfma(k, q[r][j][p], s[r][u]);
+    }
+
+    // Adds the weighted values of block b: its even and its odd elements.
+    __device__ void add_block(const u32x4 &even, const u32x4 &odd, int b, const u32x4 (&p)[R][kP]) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = kP - 1; j >= 0; --j) {
+                o[r][b][0] = mfma(even, p[r][j], o[r][b][0]);
+                o[r][b][1] = mfma(odd, p[r][j], o[r][b][1]);
+            }
     }
 
     // Scores of keys that a row does not see become -inf.  A weight of 0 does
     // not take away a NaN or an infinity (bytes above 252, which no finite
     // block has): such values are taken out as well and kept in mind for the
     // rows that see them.
-    __device__ void mask(Raw<NB> &x, int first, int lane, f32x4 (&s)[R][2]) {
+    __device__ void mask(uint32_t (&vs)[2][NB], int first, int lane, f32x4 (&s)[R][2]) {
         const int h = lane >> 4;
         uint32_t seen[R];  // bit 4 u + i: the lane's row sees key first + 16 u + 4 h + i
 #pragma unroll
@@ -211,7 +227,7 @@ struct Rows {
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const uint32_t w = x.vs[u][b];
+                const uint32_t w = vs[u][b];
                 bad |= ((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u;
             }
         if (!__any(bad != 0)) return;
@@ -221,16 +237,15 @@ struct Rows {
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if ((x.vs[u][b] >> (8 * i) & 255) > 252) {
-                        x.vs[u][b] &= ~(255u << (8 * i));
+                    if ((vs[u][b] >> (8 * i) & 255) > 252) {
+                        vs[u][b] &= ~(255u << (8 * i));
 #pragma unroll
                         for (int r = 0; r < R; ++r) poison[r] |= (seen[r] >> (4 * u + i) & 1) << b;
                     }
     }
 
-    // Scores to weights, as the parts that the second product takes; c =
-    // scale log2(e).
-    __device__ void weights(const f32x4 (&s)[R][2], float c, u32x4 (&p)[R][kP]) {
+    // Moves the rows' maxima where the scores ask for it; c = scale log2(e).
+    __device__ void raise(const f32x4 (&s)[R][2], float c) {
         bool move = false;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -254,6 +269,10 @@ struct Rows {
                 for (int b = 0; b < NB; ++b) o[r][b][0] *= f, o[r][b][1] *= f;
             }
         }
+    }
+
+    // Scores to weights, as the parts that the second product takes.
+    __device__ void weights(const f32x4 (&s)[R][2], float c, u32x4 (&p)[R][kP]) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             // s - m before the factor: the largest weight is 1 exactly, and
@@ -291,13 +310,7 @@ struct Rows {
                 even[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
                 odd[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
             }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int j = kP - 1; j >= 0; --j) {
-                    o[r][b][0] = mfma(even, p[r][j], o[r][b][0]);
-                    o[r][b][1] = mfma(odd, p[r][j], o[r][b][1]);
-                }
+            add_block(even, odd, b, p);
             // Else the scheduler converts all blocks first, in twice the registers.
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -393,77 +406,238 @@ __device__ inline void load_rows(const AttendArgs &a, const Span &seq, int kh, i
     }
 }
 
-// Where a step's two groups of 16 keys lie.  A group outside of what the rows
-// see is not read, but the nearest in its place; a bad page is not read
-// either.
+// Where a step's two groups of 16 keys lie, for steps in ascending order.  A
+// group outside of what the rows see is not read, but the nearest in its
+// place; a bad page is not read either.  A lane holds one of 64 pages, and of
+// the 64 after them, so that a step waits for no table.
 struct Groups {
     const int32_t *table;
     int first, last, shift;  // groups that hold keys which some row sees; groups of a page
-    int kh;
+    int kh, lane;
     bool bad;
+    int at, here, next;  // which 64 pages, and their numbers
+
+    __device__ Groups(const AttendArgs &a, const Span &seq, int b, const Keys &any, int kh, int lane)
+        : table(a.tables + b * a.table_stride), first(any.lo / kCacheGroup), last((any.hi - 1) / kCacheGroup),
+          shift(a.cache.page_shift - 4), kh(kh), lane(lane), bad(seq.bad), at(-1), here(0), next(0) {}
+    // Of groups first .. last (there is one).
+    __device__ int load(int block) const {
+        return table[min(max(block * 64 + lane, first >> shift), last >> shift)];
+    }
+    __device__ void begin(int t) {
+        at = (min(max(2 * t, first), last) >> shift) >> 6;
+        here = load(at);
+        next = load(at + 1);
+    }
     __device__ void aim(const CacheView &c, int t, int64_t (&base)[2]) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int g = min(max(2 * t + u, first), last);
-            int64_t p = table[g >> shift];
+            const int g = min(max(2 * t + u, first), last), i = g >> shift;
+            if (i >> 6 != at) {
+                if (i >> 6 == at + 1)
+                    at = i >> 6, here = next, next = load(at + 1);
+                else
+                    begin(t);
+            }
+            int p = __builtin_amdgcn_readlane(here, i & 63);
             if (p < 0 || p >= c.pages) bad = true, p = 0;
             base[u] = c.group(p, kh, g & ((1 << shift) - 1));
         }
     }
 };
 
-// Rows of their own for each wave, which goes through the keys by itself: its
-// four waves' rows are neighbours and read the same keys at about the same
-// time, from the first-level cache.  (From one ring in LDS, a barrier a step:
-// 473 us for 428 at 4 x 512 queries, 32 heads of 128 over 8 of 8192 keys.)
+// The sequence of the rank-th greatest length, of 64 at most (the first of equal ones first).
+__device__ inline int of_rank(const int32_t *lengths, int sequences, int rank, int lane) {
+    const int mine = lane < sequences ? lengths[lane] : INT32_MIN;
+    int before = 0;
+    for (int i = 0; i < sequences; ++i) {
+        const int other = __builtin_amdgcn_readlane(mine, i);
+        before += other > mine || (other == mine && i < lane);
+    }
+    const uint64_t found = __ballot(lane < sequences && before == rank);
+    return found ? __builtin_ctzll(found) : 0;
+}
+
+// Steps' keys and values as the products' left operands, in LDS, with the
+// values' scales: what a block of rows_kernel works from.
+template <int NB>
+struct Operands {
+    u32x4 k[2][2][NB][64];     // step, group, piece of 8 elements, lane
+    u32x4 v[2][NB][2][64];     // step, block, even or odd elements, lane
+    uint32_t vs[2][2][4][NB];  // step, group, four tokens, block
+};
+
+// What a wave converts of a step: of one group the first or the second half
+// of the pieces and of the blocks (where NB is odd the first has one less).
+template <int N>
+struct __attribute__((packed, aligned(4))) Run {
+    uint32_t w[N];
+};
+template <int NB>
+struct Share {
+    static constexpr int kMost = NB - NB / 2, kScales = NB % 4 == 0 ? 1 : kMost;
+    Run<kMost> k, v, vs;
+    uint8_t ks[kScales];
+
+    // Where a half begins: of an odd number of pieces they share one.
+    static __device__ int first_of(int wave) { return wave & 1 ? NB / 2 : 0; }
+
+    __device__ void load_keys(const uint8_t *g, int lane, int first) {
+        k = *reinterpret_cast<const Run<kMost> *>(g + lane * 4 * NB + 4 * first);
+#pragma unroll
+        for (int i = 0; i < kScales; ++i)
+            ks[i] = g[16 * 32 * NB + (lane & 15) * NB + ((lane >> 4) * NB + first + i) / 4];
+    }
+    __device__ void load_values(const uint8_t *g, int lane, int first) {
+        constexpr int D = 32 * NB;
+        v = *reinterpret_cast<const Run<kMost> *>(g + 8 * D + lane * 4 * NB + 4 * first);
+        vs = *reinterpret_cast<const Run<kMost> *>(g + 16 * D + D / 2 + (lane >> 4) * 4 * NB + 4 * first);
+    }
+    __device__ void convert_keys(Operands<NB> &to, int step, int u, int lane, int first) const {
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const float scale = __uint_as_float(static_cast<uint32_t>(ks[i % kScales]) << 23);
+            to.k[step & 1][u][first + i][lane] = u32x4{fp4_pair<0>(k.w[i], scale), fp4_pair<1>(k.w[i], scale),
+                                                       fp4_pair<2>(k.w[i], scale), fp4_pair<3>(k.w[i], scale)};
+        }
+    }
+    // clean: values that no weight of 0 would take away become zeros.
+    __device__ void convert_values(Operands<NB> &to, int step, int u, int lane, int first, bool clean) const {
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            uint32_t by = vs.w[i];
+            if ((lane & 15) == 0) to.vs[step & 1][u][lane >> 4][first + i] = by;
+            if (clean) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if ((by >> (8 * j) & 255) > 252) by &= ~(255u << (8 * j));
+            }
+            const uint32_t w[4] = {fp4_pair<0>(v.w[i], scale_of(by, 0)), fp4_pair<1>(v.w[i], scale_of(by, 1)),
+                                   fp4_pair<2>(v.w[i], scale_of(by, 2)), fp4_pair<3>(v.w[i], scale_of(by, 3))};
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            reinterpret_cast<u32x2 *>(&to.v[step & 1][first + i][0][lane])[u] =
+                u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x05040100u), __builtin_amdgcn_perm(w[3], w[2], 0x05040100u)};
+            reinterpret_cast<u32x2 *>(&to.v[step & 1][first + i][1][lane])[u] =
+                u32x2{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u), __builtin_amdgcn_perm(w[3], w[2], 0x07060302u)};
+        }
+    }
+};
+
+// Rows of their own for each wave; a block's four waves go through the keys
+// together and share the conversion of a step to bf16, a quarter each, through
+// LDS.  The scores of a step are computed beside the weights of the one
+// before, and the next operands converted beside the second product; what is
+// converted was read two steps before.  4 x 512 queries, 32 heads of 128 over
+// 8 of up to 8192 keys in 345 us, 560 TFLOP/s (every wave converting for
+// itself: 428; in the sequences' order: 393).  Bound by the vector
+// instructions of weights and conversion and by the products, which overlap
+// little with two waves on a SIMD.
 template <typename T, int NB, int R>
-__global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(AttendArgs a, int tiles_at_once) {
     using State = Rows<T, NB, R>;
+    constexpr int kRows = 16 * R * kWaves;
+    __shared__ Operands<NB> ops;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int group = a.q_heads / a.cache.heads, kh = blockIdx.y;
+    const int group = a.q_heads / a.cache.heads;
     const float c = a.scale * kLog2e;
-    for (int b = blockIdx.z; b < a.sequences; b += gridDim.z) {
+    const int64_t each = static_cast<int64_t>(tiles_at_once) * a.cache.heads, all = each * a.sequences;
+    for (int64_t id = blockIdx.x; id < all; id += gridDim.x) {
+        // Neighbouring blocks take the heads of keys, which then stay in one
+        // die's cache.  The longest sequences come first; where all blocks run
+        // at once, those of the second half, which join the first ones on
+        // their compute units, in reverse.
+        int64_t place = id;
+        if (a.sequences <= 64 && all > 256 && all <= 256 * kOccupancy<T, NB, R> && id >= 256)
+            place = 256 + (all - 1 - id);
+        const int rank = static_cast<int>(place / each), in = static_cast<int>(place - rank * each);
+        const int kh = in % a.cache.heads;
+        const int b = a.sequences <= 64 ? of_rank(a.lengths, a.sequences, rank, lane) : rank;
         const Span seq = span_of(a, b);
         const int rows = seq.n * group;  // the launcher holds tokens x q_heads below 2^31
-        const int row_tiles = (rows - 1) / (16 * R) + (rows > 0);
-        for (int tile = blockIdx.x * kWaves + wave; tile < row_tiles; tile += gridDim.x * kWaves) {
-            const int row0 = tile * 16 * R, row1 = min(rows - row0, 16 * R) + row0 - 1;
+        const int tiles = (rows - 1) / kRows + (rows > 0);
+        // The last rows, which see the most keys, first.
+        for (int tile = tiles - 1 - in / a.cache.heads; tile >= 0; tile -= tiles_at_once) {
+            const int row0 = tile * kRows, row1 = min(rows - row0, kRows) + row0 - 1;
             const Keys any = keys_of(a, seq, row0 / group, row1 / group);
             const int lo_all = keys_of(a, seq, row1 / group, row1 / group).lo,
                       hi_all = keys_of(a, seq, row0 / group, row0 / group).hi;
             State st;
             Place at[R];
             bool real[R];
-            load_rows(a, seq, kh, group, rows, row0, lane, st, at, real);
+            load_rows(a, seq, kh, group, rows, row0 + wave * 16 * R, lane, st, at, real);
             const int t0 = any.lo / kTile, t1 = (any.hi + kTile - 1) / kTile;
-            Groups groups = {a.tables + b * a.table_stride, any.lo / kCacheGroup, (any.hi - 1) / kCacheGroup,
-                             a.cache.page_shift - 4, kh, seq.bad};
-            // A step's keys and values are read into the registers of the
-            // step before as soon as those are free: the keys before the
-            // weights and the second product, the values after it.
+            Groups groups(a, seq, b, any, kh, lane);
+            auto masked = [&](int t) { return t * kTile < lo_all || t * kTile + kTile > hi_all; };
             if (any.lo < any.hi) {
-                Raw<NB> x;
-                int64_t base[2];
-                groups.aim(a.cache, t0, base);
+                const int u = wave >> 1, half = Share<NB>::first_of(wave);
+                groups.begin(t0);
+                // The group of a step that this wave converts; past the last step that one again.
+                auto group_of = [&](int t) {
+                    int64_t base[2];
+                    groups.aim(a.cache, min(t, t1 - 1), base);
+                    return a.cache.data + (u ? base[1] : base[0]);
+                };
+                auto scores = [&](int t, f32x4 (&s)[R][2]) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    load_keys<NB>(a.cache.data + base[u], lane, u, x);
-                    load_values<NB>(a.cache.data + base[u], lane, u, x);
-                }
-                groups.aim(a.cache, min(t0 + 1, t1 - 1), base);
+                    for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int i = 0; i < NB; ++i)
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) st.score(ops.k[t & 1][g][i][lane], i, s, g);
+                };
+                // On their way: the keys of two steps and the values of two,
+                // those one step behind.
+                Share<NB> now, then;
+                const uint8_t *g0 = group_of(t0), *g1 = group_of(t0 + 1), *g2 = group_of(t0 + 2), *g3 = group_of(t0 + 3);
+                now.load_keys(g0, lane, half);
+                now.load_values(g0, lane, half);
+                then.load_keys(g1, lane, half);
+                now.convert_keys(ops, t0, u, lane, half);
+                now.convert_values(ops, t0, u, lane, half, masked(t0));
+                then.convert_keys(ops, t0 + 1, u, lane, half);
+                now.load_keys(g2, lane, half);
+                now.load_values(g1, lane, half);
+                then.load_keys(g3, lane, half);
+                then.load_values(g2, lane, half);
+                __syncthreads();
+                f32x4 s[R][2];
+                scores(t0, s);
+                __syncthreads();  // step t0's keys are read
                 for (int t = t0; t < t1; ++t) {
-                    f32x4 s[R][2];
+                    // Here: scores of t; in LDS the keys of t + 1 and the
+                    // values of t; on their way the keys of t + 2 and the
+                    // values of t + 1 (now), and those of the step after.
+                    const uint8_t *g4 = group_of(t + 4);
+                    if (masked(t)) {
+                        uint32_t vs[2][NB];
+#pragma unroll
+                        for (int g = 0; g < 2; ++g)
+#pragma unroll
+                            for (int i = 0; i < NB; ++i) vs[g][i] = ops.vs[t & 1][g][lane >> 4][i];
+                        st.mask(vs, t * kTile, lane, s);
+                    }
+                    st.raise(s, c);
+                    f32x4 next[R][2];
                     u32x4 p[R][State::kP];
-                    st.scores(x, lane, s);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) load_keys<NB>(a.cache.data + base[u], lane, u, x);
-                    const int first = t * kTile;
-                    if (first < lo_all || first + kTile > hi_all) st.mask(x, first, lane, s);
+                    scores(t + 1, next);
                     st.weights(s, c, p);
-                    st.add(x, p);
+                    u32x4 even = ops.v[t & 1][0][0][lane], odd = ops.v[t & 1][0][1][lane];
+                    now.convert_keys(ops, t + 2, u, lane, half);
+                    now.convert_values(ops, t + 1, u, lane, half, masked(t + 1));
+                    now = then;
+                    then.load_keys(g4, lane, half);
+                    then.load_values(g3, lane, half);
+                    g3 = g4;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) load_values<NB>(a.cache.data + base[u], lane, u, x);
-                    groups.aim(a.cache, min(t + 2, t1 - 1), base);
+                    for (int i = 0; i < NB; ++i) {
+                        const int n = i + 1 < NB ? i + 1 : i;
+                        const u32x4 e = ops.v[t & 1][n][0][lane], o = ops.v[t & 1][n][1][lane];
+                        st.add_block(even, odd, i, p);
+                        even = e, odd = o;
+                    }
+#pragma unroll
+                    for (int r = 0; r < R; ++r) s[r][0] = next[r][0], s[r][1] = next[r][1];
+                    __syncthreads();
                 }
             }
 #pragma unroll
@@ -626,8 +800,7 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
                   hi_all = keys_of(a, seq, row0 / group, row0 / group).hi;
         // This wave's steps: every fourth of the block's.
         const int t0 = all.lo / kTile + n0 + wave, t1 = all.lo / kTile + n1;
-        Groups groups = {a.tables + b * a.table_stride, any.lo / kCacheGroup, (any.hi - 1) / kCacheGroup,
-                         a.cache.page_shift - 4, kh, seq.bad};
+        Groups groups(a, seq, b, any, kh, lane);
         // Copies a step straight to LDS, 16 bytes a lane, as it lies.  Past
         // the last step that one is copied again (a branch around the loads
         // would cost more).
@@ -649,6 +822,7 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
         };
         const bool work = any.lo < any.hi && t0 < t1;
         if (work) {
+            groups.begin(t0);
 #pragma unroll
             for (int i = 0; i < kSlots<NB>; ++i) {
                 groups.aim(a.cache, min(t0 + i * kWaves, t1 - 1), base);
@@ -675,7 +849,8 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
 #pragma unroll
                 for (int u = 0; u < 2; ++u) load_values<NB>(stage + u * 544 * NB, lane, u, x);
                 const int first = t * kTile;
-                if (first < lo_all || first + kTile > hi_all) st.mask(x, first, lane, s);
+                if (first < lo_all || first + kTile > hi_all) st.mask(x.vs, first, lane, s);
+                st.raise(s, c);
                 st.weights(s, c, p);
                 // The step is in registers: its slot is free.
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -870,9 +1045,9 @@ template <typename T, int NB>
 void launch(const AttendArgs &a, const Plan &p, char *workspace, hipStream_t stream) {
     if (p.own) {
         constexpr int R = sizeof(T) == 4 ? 1 : kOwnTiles;
-        const unsigned x = static_cast<unsigned>((p.tiles * (kOwnTiles / R) + kWaves - 1) / kWaves);
-        rows_kernel<T, NB, R>
-            <<<dim3(x, a.cache.heads, static_cast<unsigned>(std::min(a.sequences, 65535))), 256, 0, stream>>>(a);
+        const int64_t tiles = (p.tiles * (kOwnTiles / R) + kWaves - 1) / kWaves;  // of 64 R rows
+        const int64_t blocks = std::min<int64_t>(tiles * a.cache.heads * a.sequences, 1 << 22);
+        rows_kernel<T, NB, R><<<static_cast<unsigned>(blocks), 256, 0, stream>>>(a, static_cast<int>(tiles));
         return;
     }
     auto *parts = reinterpret_cast<float *>(workspace);
