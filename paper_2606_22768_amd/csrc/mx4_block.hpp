@@ -52,6 +52,25 @@ __device__ inline void load_block(const T *src, int64_t valid, float (&v)[32]) {
     }
 }
 
+// Eight values of a block whose largest magnitude has the bits `top` to their
+// four code bytes, and the block's scale byte.
+__device__ inline uint32_t encode_eight(const float (&v)[8], uint32_t top, uint32_t &byte) {
+    const uint32_t field = top >> 23;
+    if (field == 255) {
+        byte = 255;
+        return 0;
+    }
+    byte = field > 2 ? field - 2 : 0;
+    const float lift = byte == 0 ? 0x1p64f : 1.0f;  // as in encode_block
+    const float scale = __uint_as_float((byte == 0 ? 64u : byte) << 23);
+    uint32_t r = 0;
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0] * lift, v[1] * lift, scale, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2] * lift, v[3] * lift, scale, 1);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4] * lift, v[5] * lift, scale, 2);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6] * lift, v[7] * lift, scale, 3);
+    return r;
+}
+
 // One block of 32 values to its 16 code bytes; returns the scale byte.
 __device__ inline uint32_t encode_block(const float (&v)[32], uint4 &codes) {
     uint32_t top = 0;
