@@ -624,10 +624,10 @@ typedef struct {
     uint32_t struct_size; /* sizeof(fgd_attention), checked for equality */
     int32_t dtype;        /* of q and out */
     int32_t sequences;
-    int32_t table_width;  /* entries of a sequence's table; table_width * page below 2^31 */
+    int32_t table_width;  /* entries of a sequence's table; table_width * page is at most 2^31 - 64 */
     int32_t q_heads;      /* a multiple of the cache's heads: neighbouring ones share a head of keys */
     int32_t window;       /* above 0: a query sees the last `window` keys up to its own; 0: all of them */
-    int64_t tokens;       /* rows of q */
+    int64_t tokens;       /* rows of q; tokens * q_heads is at most 2^31 - 4096 */
     int64_t most_queries; /* of a sequence, as far as the program knows: steers the launch, results do not need it */
     float scale;          /* above 0; of the scores */
     int32_t reserved;     /* 0 */

@@ -118,7 +118,7 @@ class Mx4Cache:
     (uint8, laid out as fgd.h says), allocated when not given; its bytes need
     no initial value."""
 
-    __slots__ = ("data", "pages", "page", "heads", "dim", "_c", "_form")
+    __slots__ = ("_data", "_form", "_c")
 
     def __init__(self, pages, page, heads, dim, device=None, data=None):
         import torch
@@ -132,17 +132,21 @@ class Mx4Cache:
             _array("data", data, torch.uint8, data.device if device is None else torch.device(device))
             if data.numel() != need:
                 raise ValueError(f"data: expected {need} bytes, got {data.numel()}")
-        self.data, self.pages, self.page, self.heads, self.dim = data, pages, page, heads, dim
-        self._c = fgd_mx4_cache(page, heads, dim, pages, data.data_ptr())
+        self._data = data
         self._form = (pages, page, heads, dim, data.device)
+        self._c = fgd_mx4_cache(page, heads, dim, pages, data.data_ptr())
 
-    @property
-    def device(self):
-        return self.data.device
+    # Fixed for a cache's life: the kernels read as many bytes as they say.
+    data = property(lambda self: self._data)
+    pages = property(lambda self: self._form[0])
+    page = property(lambda self: self._form[1])
+    heads = property(lambda self: self._form[2])
+    dim = property(lambda self: self._form[3])
+    device = property(lambda self: self._form[4])
 
     @property
     def nbytes(self):
-        return self.data.numel()
+        return self._data.numel()
 
     def __repr__(self):
         return (f"Mx4Cache(pages={self.pages}, page={self.page}, heads={self.heads}, dim={self.dim}, "

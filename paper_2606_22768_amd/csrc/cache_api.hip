@@ -90,12 +90,12 @@ fgd_status check_attention(const fgd_mx4_cache *cache, const fgd_attention *s, b
     if (s->window < 0) return api_fail(FGD_ERR_INVALID_ARG, "window must not be negative");
     if (!(s->scale > 0) || isinf(s->scale))
         return api_fail(FGD_ERR_INVALID_ARG, "scale must be finite and above 0");
-    if (static_cast<int64_t>(s->table_width) * cache->page > INT32_MAX)
-        return api_fail(FGD_ERR_INVALID_ARG, "table_width times page must be below 2^31");
+    if (static_cast<int64_t>(s->table_width) * cache->page > INT32_MAX - 63)
+        return api_fail(FGD_ERR_INVALID_ARG, "table_width times page must be at most 2^31 - 64");
     if (cache->pages == 0 && s->table_width > 0)
         return api_fail(FGD_ERR_INVALID_ARG, "a cache without pages has tables of width 0 only");
-    if (s->tokens * s->q_heads > INT32_MAX)
-        return api_fail(FGD_ERR_INVALID_ARG, "attention: sizes are too large");
+    if (s->tokens * s->q_heads > INT32_MAX - 4095)
+        return api_fail(FGD_ERR_INVALID_ARG, "attention: tokens times q_heads must be at most 2^31 - 4096");
     a->tokens = s->tokens;
     a->sequences = s->sequences;
     a->width = s->table_width;

@@ -209,7 +209,7 @@ def test_attend_refusals():
                      (dict(q_heads=65_536), "multiple"), (dict(most_queries=-1), "most_queries"),
                      (dict(window=-1), "window"), (dict(scale=0.0), "scale"), (dict(scale=-1.0), "scale"),
                      (dict(scale=float("inf")), "scale"), (dict(scale=float("nan")), "scale"),
-                     (dict(table_width=1 << 25), "below 2\\^31")]:
+                     (dict(table_width=1 << 25), "at most 2\\^31"), (dict(tokens=1 << 28), "at most 2\\^31")]:
         refused(lambda: attend(**kw), text)
         refused(lambda: fgd.fgd_mx4_attend_workspace_size(cache(), attention(**kw)), text)
     refused(lambda: attend(cache(pages=0)), "width 0")

@@ -144,6 +144,35 @@ def test_long_sequences_are_split(env, D, dtype):
     Batch(env, [3000, 2500], [5, 2], 4, 1, D, 16, dtype, seed=3, spare=90).check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_sequences_and_pages(env, dtype):
+    # More sequences than a wave has lanes, and tables of more pages.
+    rng = np.random.default_rng(7)
+    b = Batch(env, rng.integers(0, 90, 150).tolist(), [1] * 150, 2, 1, 32, 16, dtype, seed=3)
+    b.check(starts=False)
+    b = Batch(env, rng.integers(0, 60, 140).tolist(), rng.integers(0, 3, 140).tolist(), 2, 1, 64, 16, dtype, seed=3)
+    b.check()
+    for most in (1, 50_000):
+        Batch(env, [2500, 1040], [30, 17], 4, 2, 64, 16, dtype, seed=5).check(max_q=most)
+        Batch(env, [1030] * 3, [9] * 3, 4, 2, 96, 16, dtype, seed=6).check(window=900, max_q=most)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("most", [1, 50_000])
+@pytest.mark.parametrize("power", [-100, -118, -121, 100, 120])
+def test_values_of_any_size(env, power, most, dtype):
+    # One key is seen: its value comes out as it is held, down to 2^-126.
+    def keys(_, k, v):
+        v *= 2.0 ** power
+    b = Batch(env, [20, 33], [2, 3], 2, 1, 64, 16, dtype, seed=power, keys=keys)
+    got = _np(b.run(window=1, max_q=most))
+    want = np.concatenate([np.repeat(b.v[0][18:], 2, 1), np.repeat(b.v[1][30:], 2, 1)])
+    assert abs(want).max() > 0
+    small = abs(want) < 2.0 ** -126  # numbers that a float32 sum may flush
+    assert np.array_equal(np.where(small, 0, got), np.where(small, 0, want))
+    assert np.all(abs(got[small] - want[small]) < 2.0 ** -126)
+
+
 def test_large_scores_and_scales(env):
     def keys(b, k, v):
         k *= 30
