@@ -544,11 +544,13 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(Atten
     for (int64_t id = blockIdx.x; id < all; id += gridDim.x) {
         // Neighbouring blocks take the heads of keys, which then stay in one
         // die's cache.  The longest sequences come first; where all blocks run
-        // at once, those of the second half, which join the first ones on
-        // their compute units, in reverse.
+        // at once, every second 256 of them, which join the 256 before on
+        // their compute units, stand in reverse.
         int64_t place = id;
-        if (a.sequences <= 64 && all > 256 && all <= 256 * kOccupancy<T, NB, R> && id >= 256)
-            place = 256 + (all - 1 - id);
+        if (a.sequences <= 64 && all <= 256 * kOccupancy<T, NB, R> && (id >> 8 & 1)) {
+            const int64_t layer = id & ~255, last = min(layer + 256, all) - 1;
+            place = layer + (last - id);
+        }
         const int rank = static_cast<int>(place / each), in = static_cast<int>(place - rank * each);
         const int kh = in % a.cache.heads;
         const int b = a.sequences <= 64 ? of_rank(a.lengths, a.sequences, rank, lane) : rank;
