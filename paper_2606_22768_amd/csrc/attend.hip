@@ -742,11 +742,10 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
             const Span s = span_of(a, b);
             mine = static_cast<int64_t>(items_of(a, s, group)) * length_of(a, s);
         }
-        int64_t sum = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(static_cast<long long>(sum), o);
-        line.total += sum;
+        line.total += mine;
     }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) line.total += __shfl_xor(static_cast<long long>(line.total), o);
     if (line.total == 0) return;
     line.count = static_cast<int>(min(max(line.total / kLeast, INT64_C(1)), static_cast<int64_t>(gridDim.x)));
     const int block = blockIdx.x;

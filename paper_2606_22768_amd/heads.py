@@ -255,11 +255,11 @@ def rotate_heads_grads(dq, dk, q, k, positions, freqs, q_weight=None, k_weight=N
         except AttributeError:
             key = plan = None
         if plan is not None:
-            index, sizes, need, strides, q_shape, k_shape = plan
+            index, sizes, need, strides = plan
             q_grad = torch.empty_like(dq, memory_format=torch.contiguous_format)
             k_grad = None if dk is None else torch.empty_like(dk, memory_format=torch.contiguous_format)
-            wq = None if q_weight is None else q_weight.new_empty(q_shape, dtype=torch.float32)
-            wk = None if k_weight is None else k_weight.new_empty(k_shape, dtype=torch.float32)
+            wq = None if q_weight is None else torch.empty_like(q_weight, dtype=torch.float32)
+            wk = None if k_weight is None else torch.empty_like(k_weight, dtype=torch.float32)
             work = dq.new_empty(need, dtype=torch.uint8) if need else None
             _check(lib.fgd_rotate_heads_grads(ctypes.byref(sizes), dq.data_ptr(), strides[0], _at(dk), strides[1],
                                               _at(q), strides[2], _at(k), strides[3], _at(positions), _at(freqs),
@@ -291,6 +291,5 @@ def rotate_heads_grads(dq, dk, q, k, positions, freqs, q_weight=None, k_weight=N
                                0 if workspace is None else workspace.numel() * workspace.element_size(),
                                _current(dq.device))
     if plain and key is not None:
-        _keep(key, dq.device.index, sizes, need, tuple(_strides(_axes(t)) for t in (dq, dk, q, k, q_grad, k_grad)),
-              *(None if w is None else w.shape for w in (q_weight, k_weight)))
+        _keep(key, dq.device.index, sizes, need, tuple(_strides(_axes(t)) for t in (dq, dk, q, k, q_grad, k_grad)))
     return q_grad, k_grad, wq, wk

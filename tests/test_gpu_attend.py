@@ -344,6 +344,14 @@ def test_equal_calls_streams_and_graphs(env):
     got = b.run(starts=False, stream=s), c.run(stream=s)
     s.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(want, got))
+    # Two calls at once, on streams and workspaces of their own.
+    t = torch.cuda.Stream()
+    for _ in range(5):
+        for x in (s, t):
+            x.wait_stream(torch.cuda.current_stream())
+        got = [(b.run(starts=False, stream=x), c.run(stream=x)) for x in (s, t, s, t)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(w, g) for pair in got for w, g in zip(want, pair))
     # Two graphs that share a workspace, replayed one after the other.
     need = max(fgd.fgd_mx4_attend_workspace_size(x.cache._c, fgd.fgd_attention(
         "bf16", x.tables.shape[0], x.tables.shape[1], 8, 0, x.T, 64, 1.0)) for x in (b, c))
