@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.hpp"
 
@@ -674,9 +675,8 @@ template <int NB>
 constexpr int kSlots = NB <= 2 ? 4 : NB <= 4 ? 3 : 2;
 
 // LDS of a block: its waves' rings, or their parts of the output, and maxima and sums.
-template <int NB>
-constexpr int kLineLds = 512 + kWaves * (kStage<NB> * kSlots<NB> > 16 * (32 * NB + 4) * 4 ? kStage<NB> * kSlots<NB>
-                                                                                      : 16 * (32 * NB + 4) * 4);
+template <int NB, int R>
+constexpr int kLineLds = 512 * R + kWaves * std::max(kStage<NB> * kSlots<NB>, 16 * R * (32 * NB + 4) * 4);
 
 // Waits until at most N of this wave's loads are on their way.
 template <int N>
@@ -706,14 +706,22 @@ constexpr int kItemCost = 16;  // 64 sequences of 500 to 8192 keys: 86 us (8: 90
 // and a window of 1000: 13 us; 4: 14, 16: 15, 40: 23).
 constexpr int kLeast = 8;
 
+// A number that is one for the wave, in a scalar register.
+__device__ inline int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ inline int64_t uniform(int64_t v) {
+    const uint32_t lo = uniform(static_cast<int>(v)), hi = uniform(static_cast<int>(v >> 32));
+    return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
 // An item's length for sequence s (a step where its rows see no key: they are
 // written as well), and its items.
 __device__ inline int length_of(const AttendArgs &a, const Span &s) {
     const Keys k = keys_of(a, s, 0, s.n - 1);
     return kItemCost + (k.lo < k.hi ? (k.hi + kTile - 1) / kTile - k.lo / kTile : 1);
 }
+template <int R>
 __device__ inline int items_of(const AttendArgs &a, const Span &s, int group) {
-    return (s.n * group + 15) / 16 * a.cache.heads;
+    return (s.n * group + 16 * R - 1) / (16 * R) * a.cache.heads;
 }
 
 // Which blocks hold the parts of a row's output: `parts` of them from `first`
@@ -722,80 +730,29 @@ struct Parts16 {
     int first, parts, row, pad;
 };
 
-template <typename T, int NB>
-__global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(AttendArgs a, float *parts, float2 *stats,
-                                                                          Parts16 *where) {
-    constexpr int D = 32 * NB;
-    using State = Rows<T, NB, 1>;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kLineLds<NB> - 512];
-    __shared__ float all_m[kWaves][16], all_sum[kWaves][16];
-    auto all_o = reinterpret_cast<float(*)[16][D + 4]>(lds);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Waves of a SIMD of it: few values of it are not the wave's.
+template <typename T, int NB, int R>
+constexpr int kLineOccupancy = kRegisters<T, NB, R> <= 126 ? 4 : kOccupancy<T, NB, R>;
+
+// An item is 16 R rows of a head of keys, shared by a block's four waves, which
+// split its keys.  kWhole: a block takes items as they are, `tiles` row tiles of
+// a sequence at once, and nothing is left to join; else its stretch of the line.
+template <typename T, int NB, int R, bool kWhole>
+__global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(AttendArgs a, int tiles, float *parts,
+                                                                              float2 *stats, Parts16 *where) {
+    constexpr int D = 32 * NB, kRows = 16 * R;
+    using State = Rows<T, NB, R>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kLineLds<NB, R> - 512 * R];
+    __shared__ float all_m[kWaves][kRows], all_sum[kWaves][kRows];
+    auto all_o = reinterpret_cast<float(*)[kRows][D + 4]>(lds);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = blockIdx.x;
     const int group = a.q_heads / a.cache.heads;
     const float c = a.scale * kLog2e;
-    // The line's length, 64 sequences at a time (the last 64 stay in registers).
-    Line line = {0, 0};
-    int64_t mine = 0;
-    for (int b = lane; b < (a.sequences + 63) / 64 * 64; b += 64) {
-        mine = 0;
-        if (b < a.sequences) {
-            const Span s = span_of(a, b);
-            mine = static_cast<int64_t>(items_of(a, s, group)) * length_of(a, s);
-        }
-        line.total += mine;
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) line.total += __shfl_xor(static_cast<long long>(line.total), o);
-    if (line.total == 0) return;
-    line.count = static_cast<int>(min(max(line.total / kLeast, INT64_C(1)), static_cast<int64_t>(gridDim.x)));
-    const int block = blockIdx.x;
-    if (block >= line.count) return;
-    int64_t w = line.from(block);
-    const int64_t w_end = line.from(block + 1);
-    // The sequence that w is in, and where that begins.
-    int b = 0;
-    int64_t begin = 0;
-    for (int b0 = 0; b0 < a.sequences; b0 += 64) {
-        if (a.sequences > 64) {
-            mine = 0;
-            if (b0 + lane < a.sequences) {
-                const Span s = span_of(a, b0 + lane);
-                mine = static_cast<int64_t>(items_of(a, s, group)) * length_of(a, s);
-            }
-        }
-        int64_t upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t v = __shfl_up(static_cast<long long>(upto), o);
-            if (lane >= o) upto += v;
-        }
-        const uint64_t past = __ballot(begin + upto > w);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            b = b0 + l;
-            begin += __shfl(static_cast<long long>(upto - mine), l);
-            break;
-        }
-        begin += __shfl(static_cast<long long>(upto), 63);
-    }
-    b = __builtin_amdgcn_readfirstlane(b);
-    while (w < w_end) {
-        const Span seq = span_of(a, b);
-        const int length = length_of(a, seq), items = items_of(a, seq, group), rows = seq.n * group;
-        const int64_t of_sequence = static_cast<int64_t>(items) * length;
-        if (w >= begin + of_sequence) {  // its rows are through, or it has none
-            begin += of_sequence;
-            ++b;
-            continue;
-        }
-        const int item = static_cast<int>((w - begin) / length), kh = item % a.cache.heads, row0 = item / a.cache.heads * 16;
-        const int64_t item_begin = begin + static_cast<int64_t>(item) * length;
-        // The block's steps of the item, [n0, n1).
-        const int n0 = max(static_cast<int>(w - item_begin) - kItemCost, 0),
-                  n1 = static_cast<int>(min(w_end - item_begin, static_cast<int64_t>(length))) - kItemCost;
-        w = min(w_end, item_begin + length);
-        if (n0 >= n1) continue;
-        const int row1 = min(rows - row0, 16) + row0 - 1;
+
+    // Steps [n0, n1) of the item of rows from row0; `share` of them (0: the
+    // item is whole) will be joined.
+    auto work = [&](const Span &seq, int b, int kh, int row0, int n0, int n1, int share) {
+        const int rows = seq.n * group, row1 = min(rows - row0, kRows) + row0 - 1;
         const Keys all = keys_of(a, seq, 0, seq.n - 1), any = keys_of(a, seq, row0 / group, row1 / group);
         const int lo_all = keys_of(a, seq, row1 / group, row1 / group).lo,
                   hi_all = keys_of(a, seq, row0 / group, row0 / group).hi;
@@ -821,8 +778,8 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
                         (__attribute__((address_space(3))) void *)(ring + slot * kStage<NB> + i * 1024), 16, 0, 0);
             }
         };
-        const bool work = any.lo < any.hi && t0 < t1;
-        if (work) {
+        const bool steps = any.lo < any.hi && t0 < t1;
+        if (steps) {
             groups.begin(t0);
 #pragma unroll
             for (int i = 0; i < kSlots<NB>; ++i) {
@@ -832,18 +789,18 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
             groups.aim(a.cache, min(t0 + kSlots<NB> * kWaves, t1 - 1), base);
         }
         State st;
-        Place at[1];
-        bool real[1];
+        Place at[R];
+        bool real[R];
         load_rows(a, seq, kh, group, rows, row0, lane, st, at, real);
-        if (work) {
+        if (steps) {
             outstanding<0>();  // the queries are not counted below
             int slot = 0;
             for (int t = t0; t < t1; t += kWaves) {
                 outstanding<(kSlots<NB> - 1) * kLoads>();
                 const uint8_t *stage = ring + slot * kStage<NB>;
                 Raw<NB> x;
-                f32x4 s[1][2];
-                u32x4 p[1][State::kP];
+                f32x4 s[R][2];
+                u32x4 p[R][State::kP];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) load_keys<NB>(stage + u * 544 * NB, lane, u, x);
                 st.scores(x, lane, s);
@@ -863,19 +820,24 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
             outstanding<0>();  // the ring's memory is used again
         }
         // The waves' parts are brought to one maximum and added.
-        float total = groups.bad ? NAN : st.sum[0];
-        total += __shfl_xor(total, 16);
-        total += __shfl_xor(total, 32);
-        st.poison[0] |= __shfl_xor(st.poison[0], 16);
-        st.poison[0] |= __shfl_xor(st.poison[0], 32);
-        if (lane < 16) all_m[wave][lane] = st.m[0], all_sum[wave][lane] = total;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float total = groups.bad ? NAN : st.sum[r];
+            total += __shfl_xor(total, 16);
+            total += __shfl_xor(total, 32);
+            st.poison[r] |= __shfl_xor(st.poison[r], 16);
+            st.poison[r] |= __shfl_xor(st.poison[r], 32);
+            if (lane < 16) all_m[wave][16 * r + lane] = st.m[r], all_sum[wave][16 * r + lane] = total;
+        }
         __syncthreads();  // all waves are through with their rings
-        if (real[0]) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (!real[r]) continue;
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                float4 *dst = reinterpret_cast<float4 *>(&all_o[wave][lane & 15][32 * n + 8 * (lane >> 4)]);
-                const bool nan = st.poison[0] >> n & 1;
-                const f32x4 e = st.o[0][n][0], o = st.o[0][n][1];
+                float4 *dst = reinterpret_cast<float4 *>(&all_o[wave][16 * r + (lane & 15)][32 * n + 8 * (lane >> 4)]);
+                const bool nan = st.poison[r] >> n & 1;
+                const f32x4 e = st.o[r][n][0], o = st.o[r][n][1];
                 dst[0] = nan ? make_float4(NAN, NAN, NAN, NAN) : make_float4(e[0], o[0], e[1], o[1]);
                 dst[1] = nan ? make_float4(NAN, NAN, NAN, NAN) : make_float4(e[2], o[2], e[3], o[3]);
             }
@@ -883,9 +845,11 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
         __syncthreads();
         // A thread takes some of a row's elements.
         constexpr int kPer = D / 16;
-        const int rr = threadIdx.x >> 4, e0 = (threadIdx.x & 15) * kPer, rw = row0 + rr;
-        const bool whole = n0 == 0 && n1 == length - kItemCost;
-        if (rw < rows) {
+        const int e0 = (threadIdx.x & 15) * kPer;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int rr = 16 * r + (threadIdx.x >> 4), rw = row0 + rr;
+            if (rw >= rows) break;
             float m = all_m[0][rr], f[kWaves], sum = 0;
 #pragma unroll
             for (int v = 1; v < kWaves; ++v) m = fmaxf(m, all_m[v][rr]);
@@ -897,14 +861,12 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
             const int i = rw / group;
             const int64_t token = seq.first + i;
             const int head = kh * group + rw - i * group;
-            const int64_t slot = (2 * block + (n0 == 0)) * 16 + rr;  // where a part goes
-            if ((threadIdx.x & 15) == 0) {
-                if (!whole) stats[slot] = make_float2(m, sum);
-                if (n0 == 0)
-                    where[token * a.q_heads + head] =
-                        Parts16{block, whole ? 0 : line.block_of(item_begin + length - 1) - block + 1, rr, 0};
+            const int64_t slot = (2 * block + (n0 == 0)) * kRows + rr;  // where a part goes
+            if (!kWhole && (threadIdx.x & 15) == 0) {
+                if (share) stats[slot] = make_float2(m, sum);
+                if (n0 == 0) where[token * a.q_heads + head] = Parts16{block, share, rr, 0};
             }
-            const float inv = !whole ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
+            const float inv = share ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
             T *dst = static_cast<T *>(a.out.p) + token * a.out.token_stride + head * a.out.head_stride + e0;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
@@ -912,7 +874,7 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
 #pragma unroll
                 for (int u = 0; u < kWaves; ++u) v += f[u] * all_o[u][rr][e0 + j];
                 v *= inv;
-                if (!whole)
+                if (share)
                     parts[slot * D + e0 + j] = v;
                 else if constexpr (sizeof(T) == 4)
                     dst[j] = v;
@@ -921,6 +883,84 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
             }
         }
         __syncthreads();
+    };
+
+    if constexpr (kWhole) {
+        const int64_t each = static_cast<int64_t>(tiles) * a.cache.heads, all = each * a.sequences;
+        for (int64_t id = block; id < all; id += gridDim.x) {
+            const int b = static_cast<int>(id / each), in = static_cast<int>(id - b * each), kh = in % a.cache.heads;
+            const Span seq = span_of(a, b);
+            for (int row0 = in / a.cache.heads * kRows; row0 < seq.n * group; row0 += tiles * kRows)
+                work(seq, b, kh, row0, 0, length_of(a, seq) - kItemCost, 0);
+        }
+        return;
+    }
+    // The line's length, 64 sequences at a time (the last 64 stay in registers).
+    Line line = {0, 0};
+    int64_t mine = 0;
+    for (int b = lane; b < (a.sequences + 63) / 64 * 64; b += 64) {
+        mine = 0;
+        if (b < a.sequences) {
+            const Span s = span_of(a, b);
+            mine = static_cast<int64_t>(items_of<R>(a, s, group)) * length_of(a, s);
+        }
+        line.total += mine;
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) line.total += __shfl_xor(static_cast<long long>(line.total), o);
+    line.total = uniform(line.total);
+    if (line.total == 0) return;
+    line.count = static_cast<int>(min(max(line.total / kLeast, INT64_C(1)), static_cast<int64_t>(gridDim.x)));
+    if (block >= line.count) return;
+    int64_t w = line.from(block);
+    const int64_t w_end = line.from(block + 1);
+    // The sequence that w is in, and where that begins.
+    int b = 0;
+    int64_t begin = 0;
+    for (int b0 = 0; b0 < a.sequences; b0 += 64) {
+        if (a.sequences > 64) {
+            mine = 0;
+            if (b0 + lane < a.sequences) {
+                const Span s = span_of(a, b0 + lane);
+                mine = static_cast<int64_t>(items_of<R>(a, s, group)) * length_of(a, s);
+            }
+        }
+        int64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t v = __shfl_up(static_cast<long long>(upto), o);
+            if (lane >= o) upto += v;
+        }
+        const uint64_t past = __ballot(begin + upto > w);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            b = b0 + l;
+            begin += __shfl(static_cast<long long>(upto - mine), l);
+            break;
+        }
+        begin += __shfl(static_cast<long long>(upto), 63);
+    }
+    b = uniform(b);
+    begin = uniform(begin);
+    while (w < w_end) {
+        const Span seq = span_of(a, b);
+        const int length = length_of(a, seq);
+        const int64_t of_sequence = static_cast<int64_t>(items_of<R>(a, seq, group)) * length;
+        if (w >= begin + of_sequence) {  // its rows are through, or it has none
+            begin += of_sequence;
+            ++b;
+            continue;
+        }
+        const int item = static_cast<int>((w - begin) / length);
+        const int64_t item_begin = begin + static_cast<int64_t>(item) * length;
+        // The block's steps of the item.
+        const int n0 = max(static_cast<int>(w - item_begin) - kItemCost, 0),
+                  n1 = static_cast<int>(min(w_end - item_begin, static_cast<int64_t>(length))) - kItemCost;
+        w = min(w_end, item_begin + length);
+        if (n0 >= n1) continue;
+        const bool whole = n0 == 0 && n1 == length - kItemCost;
+        const int share = whole ? 0 : n0 > 0 ? 1 : line.block_of(item_begin + length - 1) - block + 1;
+        work(seq, b, item % a.cache.heads, item / a.cache.heads * kRows, n0, n1, share);
     }
 }
 
@@ -929,7 +969,7 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, 1>)) void line_kernel(Atten
 // read at once (a wave per row, part after part: 51 us for 64 parts of 32 rows
 // of 128).
 template <typename T, int NB>
-__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, const float *__restrict__ parts,
+__global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int item_rows, const float *__restrict__ parts,
                                                    const float2 *__restrict__ stats,
                                                    const Parts16 *__restrict__ where) {
     constexpr int D = 32 * NB, kQuads = D / 4, kJoinSlots = 256 / kQuads;
@@ -945,7 +985,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, const float *__
     for (int64_t row = first * a.q_heads + blockIdx.x; row < end * a.q_heads; row += gridDim.x) {
         const Parts16 at = where[row];
         if (at.parts == 0) continue;
-        auto part = [&](int i) { return (2 * static_cast<int64_t>(at.first + i) + (i == 0)) * 16 + at.row; };
+        auto part = [&](int i) { return (2 * static_cast<int64_t>(at.first + i) + (i == 0)) * item_rows + at.row; };
         float m = -INFINITY;
         for (int i = lane; i < at.parts; i += 64) m = fmaxf(m, stats[part(i)].x);
 #pragma unroll
@@ -992,38 +1032,26 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, const float *__
 }
 
 struct Plan {
-    bool own;        // waves have rows of their own
-    int64_t tiles;   // own: row tiles (of 32 rows) of a sequence that the grid covers at once
-    int blocks;      // else: of the line
+    bool own;       // waves have rows of their own
+    bool wide;      // else: items of 32 rows
+    bool whole;     // that are not cut
+    int64_t tiles;  // row tiles of a sequence that the grid covers at once
+    int blocks;
     int64_t parts_bytes, stats_bytes, where_bytes;
 };
 
 constexpr int kOwnTiles = 2;  // R of waves with rows of their own
 
-// Blocks of a line that the card holds at once, by their registers and LDS.
+// Items of 32 rows convert a step once for twice the rows; the heads for which
+// two blocks still fit a compute unit.
 template <typename T, int NB>
-constexpr int kLineBlocks = 256 * std::min(kOccupancy<T, NB, 1>, 163840 / kLineLds<NB>);
-int line_blocks(const AttendArgs &a) {
-    switch (a.cache.dim / 32 * 2 + a.bf16) {
-        case 2: return kLineBlocks<float, 1>;
-        case 3: return kLineBlocks<uint16_t, 1>;
-        case 4: return kLineBlocks<float, 2>;
-        case 5: return kLineBlocks<uint16_t, 2>;
-        case 6: return kLineBlocks<float, 3>;
-        case 7: return kLineBlocks<uint16_t, 3>;
-        case 8: return kLineBlocks<float, 4>;
-        case 9: return kLineBlocks<uint16_t, 4>;
-        case 10: return kLineBlocks<float, 5>;
-        case 11: return kLineBlocks<uint16_t, 5>;
-        case 12: return kLineBlocks<float, 6>;
-        case 13: return kLineBlocks<uint16_t, 6>;
-        case 14: return kLineBlocks<float, 7>;
-        case 15: return kLineBlocks<uint16_t, 7>;
-        case 16: return kLineBlocks<float, 8>;
-        default: return kLineBlocks<uint16_t, 8>;
-    }
-}
+constexpr bool kWide = kRegisters<T, NB, 2> <= 235 && 2 * kLineLds<NB, 2> <= 163840;
 
+// Blocks of a line that the card holds at once, by their registers and LDS.
+template <typename T, int NB, int R>
+constexpr int kLineBlocks = 256 * std::min(kLineOccupancy<T, NB, R>, 163840 / kLineLds<NB, R>);
+
+template <typename T, int NB>
 Plan plan_of(const AttendArgs &a) {
     Plan p{};
     const int64_t group = a.q_heads / a.cache.heads;
@@ -1035,11 +1063,45 @@ Plan plan_of(const AttendArgs &a) {
         p.tiles = std::min<int64_t>(own, 1 << 20);
         return p;
     }
-    p.blocks = line_blocks(a);
-    p.parts_bytes = static_cast<int64_t>(p.blocks) * 2 * 16 * a.cache.dim * 4;
-    p.stats_bytes = static_cast<int64_t>(p.blocks) * 2 * 16 * 8;
+    // Few items keep 16 rows, for more blocks: 17 of up to 40 rows over 1000
+    // keys in 16 us (20); 512 of 20 rows over up to 4000 take 65 us for 70.
+    p.wide = kWide<T, NB> && rows > 16 && (rows + 31) / 32 * heads * seqs >= 128;
+    const int64_t item_rows = p.wide ? 32 : 16, items_of = (rows + item_rows - 1) / item_rows;
+    p.tiles = items_of;
+    p.blocks = kLineBlocks<T, NB, 1>;
+    if constexpr (kWide<T, NB>)
+        if (p.wide) p.blocks = kLineBlocks<T, NB, 2>;
+    // Where an item is short it is not cut, which spares the line's prologue
+    // and the launch that joins: one query of 200 keys in 7.5 us (12.8), 16
+    // of up to 1000 in 13.1 (15.1), 100 of up to 2000 in 34 (42); but 16 of up
+    // to 2000 in 20 (18), one of 4000 in 34 (13) and 64 of up to 8192 in 101
+    // (79), 8 heads of keys of 128 in bf16 each.
+    const int64_t items = p.tiles * heads * seqs, keys = static_cast<int64_t>(a.width) << a.cache.page_shift;
+    p.whole = keys <= 1152 || (keys <= 2304 && 2 * items >= p.blocks) || items >= 8 * p.blocks;
+    if (p.whole) {
+        p.blocks = static_cast<int>(std::min<int64_t>(items, 1 << 22));
+        return p;
+    }
+    p.parts_bytes = static_cast<int64_t>(p.blocks) * 2 * item_rows * a.cache.dim * 4;
+    p.stats_bytes = static_cast<int64_t>(p.blocks) * 2 * item_rows * 8;
     p.where_bytes = a.tokens * a.q_heads * static_cast<int64_t>(sizeof(Parts16));
     return p;
+}
+
+template <typename T, int NB, int R>
+void launch_line(const AttendArgs &a, const Plan &p, char *workspace, hipStream_t stream) {
+    const int tiles = static_cast<int>(p.tiles);
+    if (p.whole) {
+        line_kernel<T, NB, R, true><<<p.blocks, 256, 0, stream>>>(a, tiles, nullptr, nullptr, nullptr);
+        return;
+    }
+    auto *parts = reinterpret_cast<float *>(workspace);
+    auto *stats = reinterpret_cast<float2 *>(workspace + p.parts_bytes);
+    auto *where = reinterpret_cast<Parts16 *>(workspace + p.parts_bytes + p.stats_bytes);
+    line_kernel<T, NB, R, false><<<p.blocks, 256, 0, stream>>>(a, tiles, parts, stats, where);
+    const int64_t rows = a.tokens * a.q_heads;
+    join_kernel<T, NB>
+        <<<static_cast<unsigned>(std::min<int64_t>(rows, 1 << 20)), 256, 0, stream>>>(a, 16 * R, parts, stats, where);
 }
 
 template <typename T, int NB>
@@ -1051,44 +1113,43 @@ void launch(const AttendArgs &a, const Plan &p, char *workspace, hipStream_t str
         rows_kernel<T, NB, R><<<static_cast<unsigned>(blocks), 256, 0, stream>>>(a, static_cast<int>(tiles));
         return;
     }
-    auto *parts = reinterpret_cast<float *>(workspace);
-    auto *stats = reinterpret_cast<float2 *>(workspace + p.parts_bytes);
-    auto *where = reinterpret_cast<Parts16 *>(workspace + p.parts_bytes + p.stats_bytes);
-    line_kernel<T, NB><<<p.blocks, 256, 0, stream>>>(a, parts, stats, where);
-    const int64_t rows = a.tokens * a.q_heads;
-    join_kernel<T, NB>
-        <<<static_cast<unsigned>(std::min<int64_t>(rows, 1 << 20)), 256, 0, stream>>>(a, parts, stats, where);
+    if constexpr (kWide<T, NB>)
+        if (p.wide) return launch_line<T, NB, 2>(a, p, workspace, stream);
+    launch_line<T, NB, 1>(a, p, workspace, stream);
 }
 
-template <typename T>
-void launch(const AttendArgs &a, const Plan &p, char *workspace, hipStream_t stream) {
-    switch (a.cache.dim / 32) {
-        case 1: return launch<T, 1>(a, p, workspace, stream);
-        case 2: return launch<T, 2>(a, p, workspace, stream);
-        case 3: return launch<T, 3>(a, p, workspace, stream);
-        case 4: return launch<T, 4>(a, p, workspace, stream);
-        case 5: return launch<T, 5>(a, p, workspace, stream);
-        case 6: return launch<T, 6>(a, p, workspace, stream);
-        case 7: return launch<T, 7>(a, p, workspace, stream);
-        default: return launch<T, 8>(a, p, workspace, stream);
-    }
+// f(type, blocks of a head) of a call.
+template <typename F>
+auto for_kind(const AttendArgs &a, F f) {
+    auto with = [&](auto t) {
+        switch (a.cache.dim / 32) {
+            case 1: return f(t, std::integral_constant<int, 1>());
+            case 2: return f(t, std::integral_constant<int, 2>());
+            case 3: return f(t, std::integral_constant<int, 3>());
+            case 4: return f(t, std::integral_constant<int, 4>());
+            case 5: return f(t, std::integral_constant<int, 5>());
+            case 6: return f(t, std::integral_constant<int, 6>());
+            case 7: return f(t, std::integral_constant<int, 7>());
+            default: return f(t, std::integral_constant<int, 8>());
+        }
+    };
+    return a.bf16 ? with(uint16_t()) : with(float());
 }
 
 }  // namespace
 
 int64_t attend_workspace_bytes(const AttendArgs &a) {
     if (a.sequences == 0 || a.tokens == 0) return 0;
-    const Plan p = plan_of(a);
+    const Plan p = for_kind(a, [&](auto t, auto nb) { return plan_of<decltype(t), nb.value>(a); });
     return p.parts_bytes + p.stats_bytes + p.where_bytes;
 }
 
 bool attend_launch(const AttendArgs &a, void *workspace, hipStream_t stream) {
     if (a.sequences == 0 || a.tokens == 0) return true;
-    const Plan p = plan_of(a);
-    if (a.bf16)
-        launch<uint16_t>(a, p, static_cast<char *>(workspace), stream);
-    else
-        launch<float>(a, p, static_cast<char *>(workspace), stream);
+    for_kind(a, [&](auto t, auto nb) {
+        using T = decltype(t);
+        launch<T, nb.value>(a, plan_of<T, nb.value>(a), static_cast<char *>(workspace), stream);
+    });
     return hipGetLastError() == hipSuccess;
 }
 

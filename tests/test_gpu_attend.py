@@ -173,6 +173,17 @@ def test_values_of_any_size(env, power, most, dtype):
     assert np.all(abs(got[small] - want[small]) < 2.0 ** -126)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 192, 224, 256])
+def test_items_that_are_cut(env, D, dtype):
+    # Long tables: items of 16 rows and of 32, cut between blocks.
+    Batch(env, [700, 0, 1, 333], [1] * 4, 4, 2, D, 16, dtype, seed=D, spare=120).check()
+    b = Batch(env, [150, 40, 7, 500], [6, 1, 9, 13], 6, 2, D, 32, dtype, seed=D, spare=120)
+    for most in (13, 300):  # few items by the hint, and many
+        b.check(max_q=most)
+        b.check(window=60, max_q=most)
+
+
 def test_large_scores_and_scales(env):
     def keys(b, k, v):
         k *= 30
