@@ -1058,7 +1058,10 @@ Plan plan_of(const AttendArgs &a) {
     const int64_t rows = std::max<int64_t>(1, a.most_queries) * group;
     const int64_t seqs = std::max(1, a.sequences), heads = a.cache.heads;
     const int64_t own = (rows + 16 * kOwnTiles - 1) / (16 * kOwnTiles);
-    p.own = rows > 16 && own * heads * seqs >= 1024;
+    // Rows of their own for two waves of every SIMD; for fewer the line spreads
+    // the keys (2 x 512 queries over up to 8000 keys: 139 us for 330; 4 x 512
+    // over 4096 to 8192: 459 for 345; 32 heads of 128 over 8, bf16).
+    p.own = rows > 16 && own * heads * seqs >= 2048;
     if (p.own) {
         p.tiles = std::min<int64_t>(own, 1 << 20);
         return p;
