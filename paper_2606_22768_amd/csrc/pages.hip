@@ -4,6 +4,9 @@
 // sums the requests' needs, hands out pages from the top of the stack and
 // writes the tables; the tokens' positions and slots follow in the same
 // launch where they are few, else in a second over the card.
+// 64 requests of a token each: 4 us, given back in 3; 513 of up to 256: 9, 4 for
+// the tokens' slots, 9 (the pages' searches of two requests side by side in
+// a thread took 28 us for the three's 22).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
