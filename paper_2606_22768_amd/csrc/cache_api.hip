@@ -100,7 +100,7 @@ fgd_status check_attention(const fgd_mx4_cache *cache, const fgd_attention *s, b
     a->sequences = s->sequences;
     a->width = s->table_width;
     a->q_heads = s->q_heads;
-    a->most_queries = s->most_queries;
+    a->most_queries = static_cast<int32_t>(s->most_queries < s->tokens ? s->most_queries : s->tokens);
     a->window = s->window;
     a->scale = s->scale;
     a->bf16 = s->dtype == FGD_BF16;

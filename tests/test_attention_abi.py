@@ -197,6 +197,15 @@ def test_write_and_read_refusals():
     write(cache(pages=0, data=None))
 
 
+@pytest.mark.parametrize("most", [1 << 20, (1 << 31) - 1, 1 << 31, (1 << 32) + 1, (1 << 63) - 1])
+def test_most_queries_above_the_tokens(most):
+    # No sequence has more queries than there are: the same launch, so the same workspace.
+    def size(n):
+        return fgd.fgd_mx4_attend_workspace_size(cache(), attention(most_queries=n, table_width=4096, tokens=40, sequences=300))
+    assert size(40) != size(1)  # rows of 40 queries go another way than those of one
+    assert size(most) == size(40)
+
+
 def test_attend_refusals():
     s = attention()
     s.struct_size = 0
