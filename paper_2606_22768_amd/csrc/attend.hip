@@ -890,8 +890,10 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
         for (int64_t id = block; id < all; id += gridDim.x) {
             const int b = static_cast<int>(id / each), in = static_cast<int>(id - b * each), kh = in % a.cache.heads;
             const Span seq = span_of(a, b);
-            for (int row0 = in / a.cache.heads * kRows; row0 < seq.n * group; row0 += tiles * kRows)
-                work(seq, b, kh, row0, 0, length_of(a, seq) - kItemCost, 0);
+            // Counted in tiles: rows end near 2^31.
+            const int of_rows = (seq.n * group + kRows - 1) / kRows;
+            for (int tile = in / a.cache.heads; tile < of_rows; tile += tiles)
+                work(seq, b, kh, tile * kRows, 0, length_of(a, seq) - kItemCost, 0);
         }
         return;
     }
