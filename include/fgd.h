@@ -669,7 +669,7 @@ fgd_status fgd_mx4_attend_workspace_size(const fgd_mx4_cache *cache, const fgd_a
 typedef struct {
     uint32_t struct_size; /* sizeof(fgd_pages), checked for equality */
     int32_t page;         /* tokens, in [1, 65536] */
-    int32_t requests, table_width;
+    int32_t requests, table_width; /* their product is below 2^31 */
     int64_t table_stride;
     int32_t *tables;      /* device, request b's page numbers at b * table_stride */
     int32_t *lengths;     /* device [requests] */

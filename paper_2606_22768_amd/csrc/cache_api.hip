@@ -117,7 +117,8 @@ fgd_status check_pages(const fgd_pages *s, fgd::PagesView *p) {
         return api_fail(FGD_ERR_INVALID_ARG, "page must be in [1, 65536], got %d", s->page);
     if (s->table_stride < s->table_width && s->requests > 1)
         return api_fail(FGD_ERR_INVALID_ARG, "table_stride is below table_width");
-    if (static_cast<fgd::wide>(s->table_stride) * s->requests >= fgd::kMostBytes / 8)
+    if (static_cast<fgd::wide>(s->table_stride) * s->requests >= fgd::kMostBytes / 8 ||
+        static_cast<int64_t>(s->table_width) * s->requests > INT32_MAX)
         return api_fail(FGD_ERR_INVALID_ARG, "pages: sizes are too large");
     const bool table = s->requests > 0 && s->table_width > 0;
     if (fgd_status st = fgd::api_check_array("tables", s->tables, table, 4)) return st;
