@@ -75,6 +75,32 @@ fgd_status check_one(const char *what, const fgd_heads *s, int heads, const void
                                 strides[2], output, bytes);
 }
 
+// Whether an element of q is one of k, which differ in their heads only: views
+// of one array, whose spans may overlap and whose elements lie between each
+// other.  Arrays that do not step alike count as meeting where their spans do.
+bool heads_meet(const fgd_heads *s, const void *q, const int64_t *x, int64_t qb, const void *k, const int64_t *y,
+                int64_t kb) {
+    if (!fgd::api_overlap(q, qb, k, kb)) return false;
+    const int64_t D = s->head_dim, n[2] = {s->batch, s->tokens};
+    if ((n[0] > 1 && x[0] != y[0]) || (n[1] > 1 && x[1] != y[1]) || (s->q_heads + s->k_heads > 2 && x[2] != y[2]))
+        return true;
+    const int big = n[0] > 1 && (n[1] == 1 || x[0] >= x[1]) ? 0 : 1;
+    const int64_t from = (static_cast<const char *>(k) - static_cast<const char *>(q)) / fgd::api_elem_size(s->dtype);
+    // v less a number of steps of an axis, the one that leaves 0 or more or the next.
+    auto less = [&](int64_t v, int axis, int64_t up) {
+        if (n[axis] <= 1 || x[axis] == 0) return v;
+        const int64_t whole = v >= 0 ? v / x[axis] : -((-v + x[axis] - 1) / x[axis]);
+        const int64_t steps = whole + up, most = n[axis] - 1;
+        return v - (steps < -most ? -most : steps > most ? most : steps) * x[axis];
+    };
+    for (int64_t h = 1 - s->q_heads; h < s->k_heads; ++h)
+        for (int i = 0; i < 4; ++i) {
+            const int64_t v = less(less(from + h * x[2], big, i & 1), 1 - big, i >> 1);
+            if (v < D && v > -D) return true;
+        }
+    return false;
+}
+
 // The inputs that both calls have besides their heads.
 fgd_status check_common(const fgd_heads *s, const int32_t *positions, const double *freqs, const void *q_weight,
                         const void *k_weight, Spans *in) {
@@ -139,8 +165,9 @@ fgd_status fgd_rotate_heads(const fgd_heads *sizes, const void *q, const int64_t
     };
     // In place, views of one projection interleave: their spans overlap, their elements do not.
     const bool q_same = same(q, q_strides, q_out, q_out_strides, qb), k_same = same(k, k_strides, k_out, k_out_strides, kb);
-    if ((q_same || k_same) && qb > 0 && kb > 0 && q == k)
-        return api_fail(FGD_ERR_INVALID_ARG, "q and k must not be one array in place");
+    if ((q_same || k_same) && heads_meet(sizes, q, q_strides, qb, k, k_strides, kb))
+        return api_fail(FGD_ERR_INVALID_ARG, "in place q and k must not share elements");
+    const int common = in.count;
     if (!q_same) out.add(q_out, qob);
     if (!k_same) out.add(k_out, kob);
     if (!q_same || !k_same) {
@@ -152,8 +179,7 @@ fgd_status fgd_rotate_heads(const fgd_heads *sizes, const void *q, const int64_t
         Spans written, rest;
         if (q_same) written.add(q_out, qob);
         if (k_same) written.add(k_out, kob);
-        for (int i = 0; i < in.count; ++i)
-            if (in.p[i] != q && in.p[i] != k) rest.add(in.p[i], in.n[i]);
+        for (int i = 0; i < common; ++i) rest.add(in.p[i], in.n[i]);
         for (int i = 0; i < written.count; ++i)
             for (int j = 0; j < rest.count; ++j)
                 if (fgd::api_overlap(written.p[i], written.n[i], rest.p[j], rest.n[j]))

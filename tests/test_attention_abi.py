@@ -74,9 +74,37 @@ def test_heads_arrays():
     refused(lambda: rotate(ko=G), "overlap")
     refused(lambda: rotate(qo=E), "overlap")
     refused(lambda: rotate(qo=A, positions=A + 256), "overlap")
-    refused(lambda: rotate(qo=A, ks=SQ, k=A, k_heads=4, kos=SQ), "one array")
+    refused(lambda: rotate(qo=A, ks=SQ, k=A, k_heads=4, kos=SQ), "share elements")
     rotate(q=None, k=None, qo=None, ko=None, positions=None, freqs=None, tokens=0)
     rotate(q=None, qs=None, k=None, ks=None, qo=None, qos=None, ko=None, kos=None, q_heads=0, k_heads=0)
+
+
+@pytest.mark.parametrize("qh, kh, at, strides, batch, tokens, text", [
+    (4, 2, 256, (3840, 384, 64), 2, 10, None), (4, 2, 255, (3840, 384, 64), 2, 10, "share elements"),
+    (4, 2, 193, (3840, 384, 64), 2, 10, "share elements"), (4, 2, 0, (3840, 384, 64), 2, 10, "share elements"),
+    (4, 4, 64, (5120, 512, 128), 2, 10, None), (4, 4, 65, (5120, 512, 128), 2, 10, "share elements"),
+    (4, 2, 256 + 384, (3840, 384, 64), 2, 10, None), (4, 2, 257 + 384, (3840, 384, 64), 2, 10, "share elements"),
+    (4, 2, 256 + 3840, (7680, 384, 64), 2, 10, None), (4, 2, 320 - 384, (3840, 384, 64), 2, 10, "share elements"),
+    (2, 3, 1280, (3200, 64, 640), 2, 10, None), (2, 3, 1279, (3200, 64, 640), 2, 10, "share elements"),
+    (2, 1, 256, (192, 384, 64), 2, 10, "share elements"), (2, 1, 128, (192, 384, 64), 2, 10, None),
+    (1, 1, 64, (128, 128, 64), 1, 10, None), (1, 1, 32, (128, 128, 64), 1, 10, "share elements")])
+def test_heads_in_place_apart(qh, kh, at, strides, batch, tokens, text):
+    # k begins `at` elements after q: by hand, which elements the two have.
+    def elements(first, heads):
+        return {first + b * strides[0] + t * strides[1] + h * strides[2] + d
+                for b in range(batch) for t in range(tokens) for h in range(heads) for d in range(64)}
+    assert bool(elements(0, qh) & elements(at, kh)) == (text is not None)
+    # The positions refuse what passes the check, so that nothing is launched.
+    refused(lambda: rotate(q=B, qo=B, k=B + 4 * at, ko=B + 4 * at, qs=strides, qos=strides, ks=strides, kos=strides,
+                           q_heads=qh, k_heads=kh, batch=batch, tokens=tokens, positions=B + 64), text or "inputs")
+    refused(lambda: rotate(q=B, qo=B, k=B + 4 * at, ko=H, qs=strides, qos=strides, ks=strides, kos=(1 << 20, 1 << 14, 64),
+                           q_heads=qh, k_heads=kh, batch=batch, tokens=tokens, positions=B + 64), text or "inputs")
+
+
+def test_heads_in_place_strides():
+    refused(lambda: rotate(q=B, qo=B, k=B + 1024, ko=B + 1024, qs=(3840, 384, 64), qos=(3840, 384, 64),
+                           ks=(3840, 192, 64), kos=(3840, 192, 64)), "share elements")
+    refused(lambda: rotate(q=A, qo=A, positions=A), "inputs")
 
 
 def test_heads_gradients():
@@ -302,6 +330,14 @@ def pages(page=16, requests=3, table_width=4, table_stride=4, tables=A, lengths=
 
 def extend(p=None, counts=E, tokens=20, starts=F, positions=G, slots=H):
     fgd.fgd_extend_pages(pages() if p is None else p, counts, tokens, starts, positions, slots, 0)
+
+
+@pytest.mark.parametrize("requests, width", [(1 << 11, 1 << 20), (2, 1 << 30), ((1 << 31) - 1, 2)])
+def test_tables_past_2_to_31_entries(requests, width):
+    p = pages(requests=requests, table_width=width, table_stride=width, page=1, tables=A, lengths=A + (1 << 44),
+              free=A + (1 << 45), free_count=A + (1 << 46))
+    refused(lambda: extend(p), "too large")
+    refused(lambda: fgd.fgd_truncate_pages(p, A + (1 << 47), 0), "too large")
 
 
 def test_pages_refusals():
