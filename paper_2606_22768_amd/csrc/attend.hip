@@ -407,43 +407,51 @@ __device__ inline void load_rows(const AttendArgs &a, const Span &seq, int kh, i
     }
 }
 
-// Where a step's two groups of 16 keys lie, for steps in ascending order.  A
-// group outside of what the rows see is not read, but the nearest in its
-// place; a bad page is not read either.  A lane holds one of 64 pages, and of
-// the 64 after them, so that a step waits for no table.
+// Where groups of 16 keys lie, asked for in ascending order.  A group outside
+// of what the rows see is not read, but the nearest in its place; a bad page
+// is not read either.  A lane holds where one of 64 pages begins, and the
+// number of one of the 64 after them, so that a step waits for no table and
+// finds its place with a few scalar instructions (4 x 512 queries: 49 us of 340
+// with a page's number read, checked and multiplied for each group).
+template <int NB>
 struct Groups {
     const int32_t *table;
     int first, last, shift;  // groups that hold keys which some row sees; groups of a page
-    int kh, lane;
+    int lane;
     bool bad;
-    int at, here, next;  // which 64 pages, and their numbers
+    int at, next;            // which 64 pages; the numbers of the next ones
+    int64_t here, head, unit, pages;
 
     __device__ Groups(const AttendArgs &a, const Span &seq, int b, const Keys &any, int kh, int lane)
         : table(a.tables + b * a.table_stride), first(any.lo / kCacheGroup), last((any.hi - 1) / kCacheGroup),
-          shift(a.cache.page_shift - 4), kh(kh), lane(lane), bad(seq.bad), at(-1), here(0), next(0) {}
+          shift(a.cache.page_shift - 4), lane(lane), bad(seq.bad), at(-1), next(0), here(0),
+          head(a.cache.group(0, kh, 0)), unit(a.cache.group(1, 0, 0)), pages(a.cache.pages) {}
     // Of groups first .. last (there is one).
     __device__ int load(int block) const {
         return table[min(max(block * 64 + lane, first >> shift), last >> shift)];
     }
-    __device__ void begin(int t) {
-        at = (min(max(2 * t, first), last) >> shift) >> 6;
-        here = load(at);
+    __device__ int64_t begin_of(int page) {
+        const bool real = page >= 0 && page < pages;
+        bad |= __any(!real);
+        return (real ? page : 0) * unit + head;
+    }
+    __device__ void begin(int g) {
+        at = (min(max(g, first), last) >> shift) >> 6;
+        here = begin_of(load(at));
         next = load(at + 1);
     }
-    __device__ void aim(const CacheView &c, int t, int64_t (&base)[2]) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int g = min(max(2 * t + u, first), last), i = g >> shift;
-            if (i >> 6 != at) {
-                if (i >> 6 == at + 1)
-                    at = i >> 6, here = next, next = load(at + 1);
-                else
-                    begin(t);
-            }
-            int p = __builtin_amdgcn_readlane(here, i & 63);
-            if (p < 0 || p >= c.pages) bad = true, p = 0;
-            base[u] = c.group(p, kh, g & ((1 << shift) - 1));
+    __device__ int64_t aim(int g) {
+        g = min(max(g, first), last);
+        const int i = g >> shift;
+        if (i >> 6 != at) {
+            if (i >> 6 == at + 1)
+                at = i >> 6, here = begin_of(next), next = load(at + 1);
+            else
+                begin(g);
         }
+        const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(here), i & 63),
+                       hi = __builtin_amdgcn_readlane(static_cast<int>(here >> 32), i & 63);
+        return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo) + (g & ((1 << shift) - 1)) * (544 * NB);
     }
 };
 
@@ -502,17 +510,23 @@ struct Share {
                                                        fp4_pair<2>(k.w[i], scale), fp4_pair<3>(k.w[i], scale)};
         }
     }
-    // clean: values that no weight of 0 would take away become zeros.
-    __device__ void convert_values(Operands<NB> &to, int step, int u, int lane, int first, bool clean) const {
+    // In a masked step the values' scales are kept, and those that no weight
+    // of 0 would take away become zeros.  Apart from the conversion, which has
+    // no branch: products and other instructions then stand in one stretch of
+    // code, and the scheduler puts them beside each other.
+    __device__ void clean_values(Operands<NB> &to, int step, int u, int lane, int first) {
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
-            uint32_t by = vs.w[i];
-            if ((lane & 15) == 0) to.vs[step & 1][u][lane >> 4][first + i] = by;
-            if (clean) {
+            if ((lane & 15) == 0) to.vs[step & 1][u][lane >> 4][first + i] = vs.w[i];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if ((by >> (8 * j) & 255) > 252) by &= ~(255u << (8 * j));
-            }
+            for (int j = 0; j < 4; ++j)
+                if ((vs.w[i] >> (8 * j) & 255) > 252) vs.w[i] &= ~(255u << (8 * j));
+        }
+    }
+    __device__ void convert_values(Operands<NB> &to, int step, int u, int lane, int first) const {
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const uint32_t by = vs.w[i];
             const uint32_t w[4] = {fp4_pair<0>(v.w[i], scale_of(by, 0)), fp4_pair<1>(v.w[i], scale_of(by, 1)),
                                    fp4_pair<2>(v.w[i], scale_of(by, 2)), fp4_pair<3>(v.w[i], scale_of(by, 3))};
             typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -529,7 +543,7 @@ struct Share {
 // LDS.  The scores of a step are computed beside the weights of the one
 // before, and the next operands converted beside the second product; what is
 // converted was read two steps before.  4 x 512 queries, 32 heads of 128 over
-// 8 of up to 8192 keys in 345 us, 560 TFLOP/s (every wave converting for
+// 8 of up to 8192 keys in 307 us, 635 TFLOP/s (every wave converting for
 // itself: 428; in the sequences' order: 393).  Bound by the vector
 // instructions of weights and conversion and by the products, which overlap
 // little with two waves on a SIMD.
@@ -569,17 +583,13 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(Atten
             bool real[R];
             load_rows(a, seq, kh, group, rows, row0 + wave * 16 * R, lane, st, at, real);
             const int t0 = any.lo / kTile, t1 = (any.hi + kTile - 1) / kTile;
-            Groups groups(a, seq, b, any, kh, lane);
+            Groups<NB> groups(a, seq, b, any, kh, lane);
             auto masked = [&](int t) { return t * kTile < lo_all || t * kTile + kTile > hi_all; };
             if (any.lo < any.hi) {
                 const int u = wave >> 1, half = Share<NB>::first_of(wave);
-                groups.begin(t0);
+                groups.begin(2 * t0 + u);
                 // The group of a step that this wave converts; past the last step that one again.
-                auto group_of = [&](int t) {
-                    int64_t base[2];
-                    groups.aim(a.cache, min(t, t1 - 1), base);
-                    return a.cache.data + (u ? base[1] : base[0]);
-                };
+                auto group_of = [&](int t) { return a.cache.data + groups.aim(2 * min(t, t1 - 1) + u); };
                 auto scores = [&](int t, f32x4 (&s)[R][2]) {
 #pragma unroll
                     for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = f32x4{0, 0, 0, 0};
@@ -596,7 +606,8 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(Atten
                 now.load_values(g0, lane, half);
                 then.load_keys(g1, lane, half);
                 now.convert_keys(ops, t0, u, lane, half);
-                now.convert_values(ops, t0, u, lane, half, masked(t0));
+                if (masked(t0)) now.clean_values(ops, t0, u, lane, half);
+                now.convert_values(ops, t0, u, lane, half);
                 then.convert_keys(ops, t0 + 1, u, lane, half);
                 now.load_keys(g2, lane, half);
                 now.load_values(g1, lane, half);
@@ -619,6 +630,7 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(Atten
                             for (int i = 0; i < NB; ++i) vs[g][i] = ops.vs[t & 1][g][lane >> 4][i];
                         st.mask(vs, t * kTile, lane, s);
                     }
+                    if (masked(t + 1)) now.clean_values(ops, t + 1, u, lane, half);
                     st.raise(s, c);
                     f32x4 next[R][2];
                     u32x4 p[R][State::kP];
@@ -626,7 +638,7 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(Atten
                     st.weights(s, c, p);
                     u32x4 even = ops.v[t & 1][0][0][lane], odd = ops.v[t & 1][0][1][lane];
                     now.convert_keys(ops, t + 2, u, lane, half);
-                    now.convert_values(ops, t + 1, u, lane, half, masked(t + 1));
+                    now.convert_values(ops, t + 1, u, lane, half);
                     now = then;
                     then.load_keys(g4, lane, half);
                     then.load_values(g3, lane, half);
@@ -643,9 +655,10 @@ __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(Atten
                     __syncthreads();
                 }
             }
+            const bool bad = __syncthreads_or(groups.bad);  // of pages that a wave alone went to
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float total = groups.bad ? NAN : st.sum[r];
+                float total = bad ? NAN : st.sum[r];
                 total += __shfl_xor(total, 16);
                 total += __shfl_xor(total, 32);
                 st.poison[r] |= __shfl_xor(st.poison[r], 16);
@@ -758,13 +771,19 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
                   hi_all = keys_of(a, seq, row0 / group, row0 / group).hi;
         // This wave's steps: every fourth of the block's.
         const int t0 = all.lo / kTile + n0 + wave, t1 = all.lo / kTile + n1;
-        Groups groups(a, seq, b, any, kh, lane);
+        Groups<NB> groups(a, seq, b, any, kh, lane);
         // Copies a step straight to LDS, 16 bytes a lane, as it lies.  Past
         // the last step that one is copied again (a branch around the loads
         // would cost more).
         constexpr int kGroupChunks = 34 * NB, kLoads = (2 * kGroupChunks + 63) / 64;
         uint8_t *ring = lds + wave * kStage<NB> * kSlots<NB>;
         int64_t base[2];
+        // Past the last step that one again.
+        auto aim = [&](int t) {
+            t = min(t, t1 - 1);
+            base[0] = groups.aim(2 * t);
+            base[1] = groups.aim(2 * t + 1);
+        };
         auto fetch = [&](int slot) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
@@ -780,13 +799,13 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
         };
         const bool steps = any.lo < any.hi && t0 < t1;
         if (steps) {
-            groups.begin(t0);
+            groups.begin(2 * t0);
 #pragma unroll
             for (int i = 0; i < kSlots<NB>; ++i) {
-                groups.aim(a.cache, min(t0 + i * kWaves, t1 - 1), base);
+                aim(t0 + i * kWaves);
                 fetch(i);
             }
-            groups.aim(a.cache, min(t0 + kSlots<NB> * kWaves, t1 - 1), base);
+            aim(t0 + kSlots<NB> * kWaves);
         }
         State st;
         Place at[R];
@@ -813,7 +832,7 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
                 // The step is in registers: its slot is free.
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 fetch(slot);
-                groups.aim(a.cache, min(t + (kSlots<NB> + 1) * kWaves, t1 - 1), base);
+                aim(t + (kSlots<NB> + 1) * kWaves);
                 st.add(x, p);
                 slot = slot == kSlots<NB> - 1 ? 0 : slot + 1;
             }

@@ -280,6 +280,21 @@ def test_queries_of_nan_and_infinity(env):
     assert np.isfinite(_np(b.run(starts=False))[~bad]).all()
 
 
+@pytest.mark.parametrize("bad", [0, 1, 62, 63, 64, 65, 127, 128])
+def test_a_bad_page_of_many_rows(env, bad):
+    # Every page that rows see, wherever a program's 64 of them begin: by waves of their own, and in items.
+    fgd, torch = env
+    b = Batch(env, [129 * 16 - 3] * 2, [160, 160], 256, 16, 32, 16, "bf16", seed=bad)
+    for most in (None, 1):
+        assert np.isfinite(_np(b.run(max_q=most))).all()
+    b.tables[1, bad] = b.cache.pages
+    for most in (None, 1):
+        got = _np(b.run(max_q=most))
+        assert np.isfinite(got[:160]).all()
+        seen = [i for i in range(160, 320) if b.lens[1] - 160 + (i - 160) >= 16 * bad]
+        assert seen and np.isnan(got[seen]).any(-1).all()
+
+
 @pytest.mark.parametrize("shared", [True, False])
 def test_bad_pages_and_lengths(env, shared):
     fgd, torch = env
