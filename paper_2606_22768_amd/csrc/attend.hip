@@ -15,6 +15,8 @@
 // a lane.  The rows are the queries of all heads that share a key head.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -43,6 +45,20 @@ struct Parts<uint16_t> {
 template <>
 struct Parts<float> {
     static constexpr int q = 3, p = 3;
+};
+
+// The maximum that a row's weights refer to.  f32 outputs: a score, so that
+// the weight of the largest, (s - m) c, is exactly 1 and equal keys give their
+// value back.  bf16 outputs: c times one, rounded, and exponents c s - m in one
+// operation: what the rounding leaves is a factor of all the row's weights, and
+// the sum of two bf16 numbers is off by less than a bf16 output shows (4 x 512
+// queries: 282 us for 310).
+template <typename T>
+struct Top {
+    static constexpr bool scaled = sizeof(T) == 2;
+    static constexpr float none = scaled ? -FLT_MAX : -INFINITY;  // of no key
+    // log2 of a weight that refers to `from` where it refers to `to`.
+    static __device__ float between(float from, float to, float c) { return scaled ? from - to : (from - to) * c; }
 };
 
 __device__ inline uint32_t pack_bf16(float a, float b) {
@@ -122,14 +138,14 @@ struct Rows {
     static constexpr int D = 32 * NB, kQ = Parts<T>::q, kP = Parts<T>::p;
     u32x4 q[R][kQ][NB];      // the right operand of the scores: row l & 15, elements (l >> 4) D/4 + 8 s ...
     f32x4 o[R][NB][2];       // O^T: row l & 15, elements 32 b + 8 (l >> 4) + 2 i + (0 or 1)
-    float m[R], sum[R];      // the maximum that weights refer to, in scores (not scaled); the lane's part of their sum
+    float m[R], sum[R];      // the maximum that weights refer to; the lane's part of their sum
     int lo[R], hi[R];        // the keys that the lane's row sees
     uint32_t poison[R];      // blocks in which the row sees a NaN value
 
     __device__ void clear() {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            m[r] = -INFINITY, sum[r] = 0, poison[r] = 0;
+            m[r] = Top<T>::none, sum[r] = 0, poison[r] = 0;
 #pragma unroll
             for (int b = 0; b < NB; ++b) o[r][b][0] = o[r][b][1] = f32x4{0, 0, 0, 0};
         }
@@ -246,43 +262,57 @@ struct Rows {
     }
 
     // Moves the rows' maxima where the scores ask for it; c = scale log2(e).
-    __device__ void raise(const f32x4 (&s)[R][2], float c) {
+    // From here on s are the weights' exponents where maxima are scaled.
+    __device__ void raise(f32x4 (&s)[R][2], float c) {
+        using To = Top<T>;
+        auto largest = [&](const f32x4 (&x)[2]) {
+            float top = x[0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
+            return top;
+        };
         bool move = false;
+        f32x4 e[R][2];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float top = s[r][0][0];
+            if constexpr (To::scaled) {
 #pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, s[r][i >> 2][i & 3]);
-            move |= (top - m[r]) * c > kSlack;  // infinite at first; false for two infinities
+                for (int i = 0; i < 8; ++i) e[r][i >> 2][i & 3] = __builtin_fmaf(s[r][i >> 2][i & 3], c, -m[r]);
+                move |= largest(e[r]) > kSlack;
+            } else {
+                move |= (largest(s[r]) - m[r]) * c > kSlack;  // infinite at first; false for two infinities
+            }
         }
         if (__any(move)) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float top = s[r][0][0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) top = fmaxf(top, s[r][i >> 2][i & 3]);
+                float top = largest(s[r]) * (To::scaled ? c : 1.0f);
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(m[r], fmaxf(top, __shfl_xor(top, 32)));
-                const float f = top == m[r] ? 1.0f : __builtin_amdgcn_exp2f((m[r] - top) * c);
+                const float f = top == m[r] ? 1.0f : __builtin_amdgcn_exp2f(To::between(m[r], top, c));
                 m[r] = top;
                 sum[r] *= f;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) o[r][b][0] *= f, o[r][b][1] *= f;
+                if constexpr (To::scaled)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) e[r][i >> 2][i & 3] = __builtin_fmaf(s[r][i >> 2][i & 3], c, -top);
             }
         }
+        if constexpr (To::scaled)
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r][0] = e[r][0], s[r][1] = e[r][1];
     }
 
-    // Scores to weights, as the parts that the second product takes.
+    // What raise() left to weights, as the parts that the second product takes.
     __device__ void weights(const f32x4 (&s)[R][2], float c, u32x4 (&p)[R][kP]) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            // s - m before the factor: the largest weight is 1 exactly, and
-            // large scores lose nothing (m c would be rounded by itself).
             const float base = m[r] == -INFINITY ? 0.0f : m[r];
+            auto weight = [&](float x) { return __builtin_amdgcn_exp2f(Top<T>::scaled ? x : (x - base) * c); };
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                float a = __builtin_amdgcn_exp2f((s[r][i >> 1][2 * (i & 1)] - base) * c),
-                      b = __builtin_amdgcn_exp2f((s[r][i >> 1][2 * (i & 1) + 1] - base) * c);
+                float a = weight(s[r][i >> 1][2 * (i & 1)]), b = weight(s[r][i >> 1][2 * (i & 1) + 1]);
                 sum[r] += a + b;
 #pragma unroll
                 for (int j = 0; j < kP; ++j) {
@@ -543,10 +573,10 @@ struct Share {
 // LDS.  The scores of a step are computed beside the weights of the one
 // before, and the next operands converted beside the second product; what is
 // converted was read two steps before.  4 x 512 queries, 32 heads of 128 over
-// 8 of up to 8192 keys in 307 us, 635 TFLOP/s (every wave converting for
-// itself: 428; in the sequences' order: 393).  Bound by the vector
-// instructions of weights and conversion and by the products, which overlap
-// little with two waves on a SIMD.
+// 8 of up to 8192 keys in 282 us, 695 TFLOP/s (before later steps, 345: every
+// wave converting for itself: 428; in the sequences' order: 393).  Bound by
+// the instructions of weights, conversion and products, of which two waves on
+// a SIMD hide little of each other's.
 template <typename T, int NB, int R>
 __global__ __launch_bounds__(256, (kOccupancy<T, NB, R>)) void rows_kernel(AttendArgs a, int tiles_at_once) {
     using State = Rows<T, NB, R>;
@@ -874,7 +904,7 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
             for (int v = 1; v < kWaves; ++v) m = fmaxf(m, all_m[v][rr]);
 #pragma unroll
             for (int v = 0; v < kWaves; ++v) {
-                f[v] = all_m[v][rr] == m ? 1.0f : __builtin_amdgcn_exp2f((all_m[v][rr] - m) * c);
+                f[v] = all_m[v][rr] == m ? 1.0f : __builtin_amdgcn_exp2f(Top<T>::between(all_m[v][rr], m, c));
                 sum += f[v] * all_sum[v][rr];
             }
             const int i = rw / group;
@@ -1019,8 +1049,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int item_rows, 
                 const int64_t p = part(i);
                 const float2 x = stats[p];
                 const float4 y = *reinterpret_cast<const float4 *>(parts + p * D + 4 * quad);
-                // A part that saw no key has a maximum of -inf, and zeros.
-                const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f((x.x - m) * c);
+                // A part that saw no key has the lowest maximum, and zeros.
+                const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f(Top<T>::between(x.x, m, c));
                 sum += f * x.y;
                 v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
             }
@@ -1080,8 +1110,8 @@ Plan plan_of(const AttendArgs &a) {
     const int64_t seqs = std::max(1, a.sequences), heads = a.cache.heads;
     const int64_t own = (rows + 16 * kOwnTiles - 1) / (16 * kOwnTiles);
     // Rows of their own for two waves of every SIMD; for fewer the line spreads
-    // the keys (2 x 512 queries over up to 8000 keys: 139 us for 330; 4 x 512
-    // over 4096 to 8192: 459 for 345; 32 heads of 128 over 8, bf16).
+    // the keys (2 x 512 queries over up to 8000 keys: 139 us for 330, as a line; 4 x 512
+    // over 4096 to 8192: 282 for 459; 32 heads of 128 over 8, bf16).
     p.own = rows > 16 && own * heads * seqs >= 2048;
     if (p.own) {
         p.tiles = std::min<int64_t>(own, 1 << 20);

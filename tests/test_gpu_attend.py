@@ -3,8 +3,8 @@ reference of the values that the cache holds.
 
 Tolerances are the reference's bound of a float32 computation, plus for bf16
 outputs what weights in two bf16 parts leave out (2^-17 of each) and half a
-step of the rounding (2^-8 of the value).  Where one key is seen, or keys are
-equal, every number is exact and the bits have to be.
+step of the rounding (2^-8 of the value).  Where one key is seen the bits have
+to be equal, and for f32 outputs where keys are equal: every number is exact.
 """
 
 import numpy as np
@@ -209,7 +209,14 @@ def test_exact_where_one_key_is_seen(env, shared, dtype):
     b = Batch(env, [64] * n, [1] * n, 16, 16, 96, 16, dtype, seed=9, keys=keys)
     got = _np(b.run(max_q=1 if shared else 40))
     for i in range(n):
-        assert np.array_equal(got[i], _round(torch, b.v[i].mean(0), dtype))
+        want, size = b.v[i].mean(0), abs(b.v[i]).mean(0)
+        if dtype == "f32":  # every weight is 1
+            assert np.array_equal(got[i], _round(torch, want, dtype))
+            continue
+        # bf16: every weight is one number near 1, held in two parts to 2^-17 of itself. The sum of 2 x 64 exact terms is
+        # off by 2^-23 of the terms' at each addition, 2^-16 of it in all; and then the result's half step.
+        tol = 2.0 ** -16 * (size + abs(want))
+        assert np.all(abs(got[i] - want) <= tol + 2.0 ** -8 * (abs(want) + tol))
 
 
 def _round(torch, a, dtype):
