@@ -33,7 +33,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4, kTile = 32;  // waves of a block; keys of a wave's step
 constexpr float kLog2e = 1.44269504f;
 // The running maximum is moved when a score passes it by this much (in
-// powers of two): weights stay below 2^8, and most steps spare the rescaling.
+// powers of two): weights stay near 2^8 at most, and most steps spare the
+// rescaling.
 constexpr float kSlack = 8.0f;
 
 template <typename T>
@@ -47,19 +48,25 @@ struct Parts<float> {
     static constexpr int q = 3, p = 3;
 };
 
-// The maximum that a row's weights refer to.  f32 outputs: a score, so that
-// the weight of the largest, (s - m) c, is exactly 1 and equal keys give their
-// value back.  bf16 outputs: c times one, rounded, and exponents c s - m in one
-// operation: what the rounding leaves is a factor of all the row's weights, and
-// the sum of two bf16 numbers is off by less than a bf16 output shows (4 x 512
-// queries: 282 us for 310).
+// The maximum m that a row's weights refer to.  f32 outputs: a score, and
+// weights' exponents (s - m) c: a score equal to m has the weight 1 exactly,
+// so that equal keys give their value back.  bf16 outputs: c times a score,
+// rounded, and exponents c s - m in one operation: what the rounding leaves is
+// a factor of all the row's weights, and the sum of two bf16 numbers is off by
+// less than a bf16 output shows (4 x 512 queries: 276 us for 310).  That
+// factor is near 1 only where m is not far: a wave that holds a row with m
+// past kFar works with scores as f32 outputs do (its rows are `raw`), which is
+// also right where c s passes the float32 numbers.  What it takes to tell costs
+// 276 us for 273, or 300 for 288 where most steps move a maximum (scale 1).
 template <typename T>
-struct Top {
-    static constexpr bool scaled = sizeof(T) == 2;
-    static constexpr float none = scaled ? -FLT_MAX : -INFINITY;  // of no key
-    // log2 of a weight that refers to `from` where it refers to `to`.
-    static __device__ float between(float from, float to, float c) { return scaled ? from - to : (from - to) * c; }
-};
+constexpr bool kScaled = sizeof(T) == 2;
+constexpr float kFar = 0x1p20f;  // the factor is 2^(2^-4) at most
+
+// The power of two of weights that refer to `from` where they refer to `to`
+// (Rows::reference): 0 for what saw no key, where there is another.
+__device__ inline float factor(double from, double to) {
+    return from == to ? 1.0f : __builtin_amdgcn_exp2f(static_cast<float>(from - to));
+}
 
 __device__ inline uint32_t pack_bf16(float a, float b) {
     bf16x2 v;
@@ -139,13 +146,17 @@ struct Rows {
     u32x4 q[R][kQ][NB];      // the right operand of the scores: row l & 15, elements (l >> 4) D/4 + 8 s ...
     f32x4 o[R][NB][2];       // O^T: row l & 15, elements 32 b + 8 (l >> 4) + 2 i + (0 or 1)
     float m[R], sum[R];      // the maximum that weights refer to; the lane's part of their sum
+    int raw;                 // 1: m are scores, those of f32 outputs always (an int: 276 us as above for 288)
     int lo[R], hi[R];        // the keys that the lane's row sees
     uint32_t poison[R];      // blocks in which the row sees a NaN value
 
-    __device__ void clear() {
+    // c = scale log2(e).  Above 1 it may take every score of a row to -inf,
+    // which its first maximum would not show: such rows begin raw.
+    __device__ void clear(float c) {
+        raw = !kScaled<T> || c > 1;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            m[r] = Top<T>::none, sum[r] = 0, poison[r] = 0;
+            m[r] = raw ? -INFINITY : -FLT_MAX, sum[r] = 0, poison[r] = 0;
 #pragma unroll
             for (int b = 0; b < NB; ++b) o[r][b][0] = o[r][b][1] = f32x4{0, 0, 0, 0};
         }
@@ -261,21 +272,21 @@ struct Rows {
                     }
     }
 
-    // Moves the rows' maxima where the scores ask for it; c = scale log2(e).
-    // From here on s are the weights' exponents where maxima are scaled.
-    __device__ void raise(f32x4 (&s)[R][2], float c) {
-        using To = Top<T>;
-        auto largest = [&](const f32x4 (&x)[2]) {
-            float top = x[0][0];
+    static __device__ float largest(const f32x4 (&x)[2]) {
+        float top = x[0][0];
 #pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
-            return top;
-        };
+        for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
+        return top;
+    }
+
+    // Moves the rows' maxima where the scores ask for it; c = scale log2(e).
+    // From here on s are the weights' exponents where kScaled<T>.
+    __device__ void raise(f32x4 (&s)[R][2], float c) {
         bool move = false;
         f32x4 e[R][2];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if constexpr (To::scaled) {
+            if constexpr (kScaled<T>) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) e[r][i >> 2][i & 3] = __builtin_fmaf(s[r][i >> 2][i & 3], c, -m[r]);
                 move |= largest(e[r]) > kSlack;
@@ -283,25 +294,89 @@ struct Rows {
                 move |= (largest(s[r]) - m[r]) * c > kSlack;  // infinite at first; false for two infinities
             }
         }
-        if (__any(move)) {
+        if constexpr (kScaled<T>) {
+            if ((__ballot(move) | static_cast<uint64_t>(raw)) != 0) settle(s, c, e);
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r][0] = e[r][0], s[r][1] = e[r][1];
+        } else if (__any(move)) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                float top = largest(s[r]) * (To::scaled ? c : 1.0f);
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(m[r], fmaxf(top, __shfl_xor(top, 32)));
-                const float f = top == m[r] ? 1.0f : __builtin_amdgcn_exp2f(To::between(m[r], top, c));
+                const float top = fmaxf(m[r], of_row(largest(s[r])));
+                const float f = top == m[r] ? 1.0f : __builtin_amdgcn_exp2f((m[r] - top) * c);
                 m[r] = top;
                 sum[r] *= f;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) o[r][b][0] *= f, o[r][b][1] *= f;
-                if constexpr (To::scaled)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[r][i >> 2][i & 3] = __builtin_fmaf(s[r][i >> 2][i & 3], c, -top);
             }
         }
-        if constexpr (To::scaled)
+    }
+
+    // The largest of the four lanes that share a row.
+    static __device__ float of_row(float x) {
+        x = fmaxf(x, __shfl_xor(x, 16));
+        return fmaxf(x, __shfl_xor(x, 32));
+    }
+
+    // raise() where maxima move or are raw: also the exponents e.
+    __device__ void settle(const f32x4 (&s)[R][2], float c, f32x4 (&e)[R][2]) {
+        float top[R], f[R];
+        bool near = !raw;
 #pragma unroll
-            for (int r = 0; r < R; ++r) s[r][0] = e[r][0], s[r][1] = e[r][1];
+        for (int r = 0; r < R; ++r) {
+            top[r] = of_row(largest(s[r]));
+            f[r] = fmaxf(m[r], top[r] * c);
+            near &= fabsf(f[r]) <= kFar || !(top[r] > -INFINITY);  // or has seen no key
+        }
+        if (__all(near)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float n = f[r];
+                f[r] = __builtin_amdgcn_exp2f(m[r] - n);
+                m[r] = n;
+            }
+        } else {
+            refer(top, c, f);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            sum[r] *= f[r];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[r][b][0] *= f[r], o[r][b][1] *= f[r];
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float x = raw && m[r] > -INFINITY ? m[r] : 0.0f, y = raw ? 0.0f : -m[r];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                e[r][i >> 2][i & 3] = __builtin_fmaf(s[r][i >> 2][i & 3] - x, c, y);
+        }
+    }
+
+    // settle()'s new maxima where they were raw or one is far, and the factors
+    // of the weights so far.  They are raw from here on if one is far or, of
+    // those that began so, belongs to a row that will see a key and has not.
+    __device__ void refer(const float (&top)[R], float c, float (&f)[R]) {
+        const int was = raw;
+        bool near = true;
+        double from[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            from[r] = reference(was, m[r], c);
+            m[r] = fmaxf(was ? m[r] : m[r] == -FLT_MAX ? -INFINITY : m[r] / c, top[r]);
+            near &= fabsf(m[r] * c) <= kFar || lo[r] >= hi[r];
+        }
+        raw = __builtin_amdgcn_readfirstlane(__ballot(!near) != 0);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (!raw) m[r] = fmaxf(m[r] * c, -FLT_MAX);
+            f[r] = factor(from[r], reference(raw, m[r], c));
+        }
+    }
+
+    // c times a maximum, exactly.
+    static __device__ double reference(bool raw, float m, float c) {
+        if (!kScaled<T> || raw) return static_cast<double>(m) * static_cast<double>(c);
+        return m == -FLT_MAX ? -INFINITY : static_cast<double>(m);
     }
 
     // What raise() left to weights, as the parts that the second product takes.
@@ -309,7 +384,7 @@ struct Rows {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const float base = m[r] == -INFINITY ? 0.0f : m[r];
-            auto weight = [&](float x) { return __builtin_amdgcn_exp2f(Top<T>::scaled ? x : (x - base) * c); };
+            auto weight = [&](float x) { return __builtin_amdgcn_exp2f(kScaled<T> ? x : (x - base) * c); };
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float a = weight(s[r][i >> 1][2 * (i & 1)]), b = weight(s[r][i >> 1][2 * (i & 1) + 1]);
@@ -420,7 +495,7 @@ __device__ inline Keys keys_of(const AttendArgs &a, const Span &s, int query0, i
 template <typename T, int NB, int R>
 __device__ inline void load_rows(const AttendArgs &a, const Span &seq, int kh, int group, int rows, int row0, int lane,
                                  Rows<T, NB, R> &st, Place (&at)[R], bool (&real)[R]) {
-    st.clear();
+    st.clear(a.scale * kLog2e);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int row = row0 + 16 * r + (lane & 15);
@@ -719,7 +794,7 @@ constexpr int kSlots = NB <= 2 ? 4 : NB <= 4 ? 3 : 2;
 
 // LDS of a block: its waves' rings, or their parts of the output, and maxima and sums.
 template <int NB, int R>
-constexpr int kLineLds = 512 * R + kWaves * std::max(kStage<NB> * kSlots<NB>, 16 * R * (32 * NB + 4) * 4);
+constexpr int kLineLds = 768 * R + kWaves * std::max(kStage<NB> * kSlots<NB>, 16 * R * (32 * NB + 4) * 4);
 
 // Waits until at most N of this wave's loads are on their way.
 template <int N>
@@ -773,6 +848,12 @@ struct Parts16 {
     int first, parts, row, pad;
 };
 
+// What a part's weights refer to, and their sum.
+struct Stats {
+    double m;
+    float sum, pad;
+};
+
 // Waves of a SIMD of it: few values of it are not the wave's.
 template <typename T, int NB, int R>
 constexpr int kLineOccupancy = kRegisters<T, NB, R> <= 126 ? 4 : kOccupancy<T, NB, R>;
@@ -782,11 +863,12 @@ constexpr int kLineOccupancy = kRegisters<T, NB, R> <= 126 ? 4 : kOccupancy<T, N
 // a sequence at once, and nothing is left to join; else its stretch of the line.
 template <typename T, int NB, int R, bool kWhole>
 __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(AttendArgs a, int tiles, float *parts,
-                                                                              float2 *stats, Parts16 *where) {
+                                                                              Stats *stats, Parts16 *where) {
     constexpr int D = 32 * NB, kRows = 16 * R;
     using State = Rows<T, NB, R>;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kLineLds<NB, R> - 512 * R];
-    __shared__ float all_m[kWaves][kRows], all_sum[kWaves][kRows];
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kLineLds<NB, R> - 768 * R];
+    __shared__ double all_m[kWaves][kRows];
+    __shared__ float all_sum[kWaves][kRows];
     auto all_o = reinterpret_cast<float(*)[kRows][D + 4]>(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), block = blockIdx.x;
     const int group = a.q_heads / a.cache.heads;
@@ -876,7 +958,7 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
             total += __shfl_xor(total, 32);
             st.poison[r] |= __shfl_xor(st.poison[r], 16);
             st.poison[r] |= __shfl_xor(st.poison[r], 32);
-            if (lane < 16) all_m[wave][16 * r + lane] = st.m[r], all_sum[wave][16 * r + lane] = total;
+            if (lane < 16) all_m[wave][16 * r + lane] = st.reference(st.raw, st.m[r], c), all_sum[wave][16 * r + lane] = total;
         }
         __syncthreads();  // all waves are through with their rings
 #pragma unroll
@@ -899,12 +981,13 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
         for (int r = 0; r < R; ++r) {
             const int rr = 16 * r + (threadIdx.x >> 4), rw = row0 + rr;
             if (rw >= rows) break;
-            float m = all_m[0][rr], f[kWaves], sum = 0;
+            double m = all_m[0][rr];
+            float f[kWaves], sum = 0;
 #pragma unroll
-            for (int v = 1; v < kWaves; ++v) m = fmaxf(m, all_m[v][rr]);
+            for (int v = 1; v < kWaves; ++v) m = fmax(m, all_m[v][rr]);
 #pragma unroll
             for (int v = 0; v < kWaves; ++v) {
-                f[v] = all_m[v][rr] == m ? 1.0f : __builtin_amdgcn_exp2f(Top<T>::between(all_m[v][rr], m, c));
+                f[v] = factor(all_m[v][rr], m);
                 sum += f[v] * all_sum[v][rr];
             }
             const int i = rw / group;
@@ -912,7 +995,7 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
             const int head = kh * group + rw - i * group;
             const int64_t slot = (2 * block + (n0 == 0)) * kRows + rr;  // where a part goes
             if (!kWhole && (threadIdx.x & 15) == 0) {
-                if (share) stats[slot] = make_float2(m, sum);
+                if (share) stats[slot] = Stats{m, sum, 0};
                 if (n0 == 0) where[token * a.q_heads + head] = Parts16{block, share, rr, 0};
             }
             const float inv = share ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
@@ -1021,13 +1104,12 @@ __global__ __launch_bounds__(256, (kLineOccupancy<T, NB, R>)) void line_kernel(A
 // of 128).
 template <typename T, int NB>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int item_rows, const float *__restrict__ parts,
-                                                   const float2 *__restrict__ stats,
+                                                   const Stats *__restrict__ stats,
                                                    const Parts16 *__restrict__ where) {
     constexpr int D = 32 * NB, kQuads = D / 4, kJoinSlots = 256 / kQuads;
     __shared__ float4 sums[kJoinSlots][kQuads];
     __shared__ float totals[kJoinSlots];
     const int quad = threadIdx.x % kQuads, slot = threadIdx.x / kQuads, lane = threadIdx.x & 63;
-    const float c = a.scale * kLog2e;
     int64_t first = 0, end = a.tokens;
     if (a.starts) {  // rows behind the last sequence stay as they are
         first = min(max(static_cast<int64_t>(a.starts[0]), INT64_C(0)), a.tokens);
@@ -1037,21 +1119,21 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a, int item_rows, 
         const Parts16 at = where[row];
         if (at.parts == 0) continue;
         auto part = [&](int i) { return (2 * static_cast<int64_t>(at.first + i) + (i == 0)) * item_rows + at.row; };
-        float m = -INFINITY;
-        for (int i = lane; i < at.parts; i += 64) m = fmaxf(m, stats[part(i)].x);
+        double m = -INFINITY;
+        for (int i = lane; i < at.parts; i += 64) m = fmax(m, stats[part(i)].m);
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+        for (int o = 1; o < 64; o <<= 1) m = fmax(m, __shfl_xor(m, o));
         float4 v = make_float4(0, 0, 0, 0);
         float sum = 0;
         if (slot < kJoinSlots) {
 #pragma unroll 4
             for (int i = slot; i < at.parts; i += kJoinSlots) {
                 const int64_t p = part(i);
-                const float2 x = stats[p];
+                const Stats x = stats[p];
                 const float4 y = *reinterpret_cast<const float4 *>(parts + p * D + 4 * quad);
                 // A part that saw no key has the lowest maximum, and zeros.
-                const float f = x.x == m ? 1.0f : __builtin_amdgcn_exp2f(Top<T>::between(x.x, m, c));
-                sum += f * x.y;
+                const float f = factor(x.m, m);
+                sum += f * x.sum;
                 v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
             }
             sums[slot][quad] = v;
@@ -1137,7 +1219,7 @@ Plan plan_of(const AttendArgs &a) {
         return p;
     }
     p.parts_bytes = static_cast<int64_t>(p.blocks) * 2 * item_rows * a.cache.dim * 4;
-    p.stats_bytes = static_cast<int64_t>(p.blocks) * 2 * item_rows * 8;
+    p.stats_bytes = static_cast<int64_t>(p.blocks) * 2 * item_rows * static_cast<int64_t>(sizeof(Stats));
     p.where_bytes = a.tokens * a.q_heads * static_cast<int64_t>(sizeof(Parts16));
     return p;
 }
@@ -1150,7 +1232,7 @@ void launch_line(const AttendArgs &a, const Plan &p, char *workspace, hipStream_
         return;
     }
     auto *parts = reinterpret_cast<float *>(workspace);
-    auto *stats = reinterpret_cast<float2 *>(workspace + p.parts_bytes);
+    auto *stats = reinterpret_cast<Stats *>(workspace + p.parts_bytes);
     auto *where = reinterpret_cast<Parts16 *>(workspace + p.parts_bytes + p.stats_bytes);
     line_kernel<T, NB, R, false><<<p.blocks, 256, 0, stream>>>(a, tiles, parts, stats, where);
     const int64_t rows = a.tokens * a.q_heads;

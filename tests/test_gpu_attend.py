@@ -404,3 +404,86 @@ def test_equal_calls_streams_and_graphs(env):
         torch.cuda.synchronize()
         for g, out, x, kw in graphs:
             assert torch.equal(out, x.run(**kw))
+
+
+def _route(route):
+    """(sequences, query heads, key heads, queries each, hint, spare pages) of a call that goes this way."""
+    return {"items": (3, 4, 2, 5, 5, 2), "cut items": (3, 4, 2, 5, 5, 120), "items of 32": (40, 16, 4, 8, 8, 2),
+            "cut items of 32": (40, 16, 4, 8, 8, 120), "own rows": (70, 16, 16, 5, 40, 2)}[route]
+
+
+ROUTES = ["items", "cut items", "items of 32", "cut items of 32", "own rows"]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0.125, 0.69, 0.7, 4.0, 1e30])
+@pytest.mark.parametrize("sign", ["both", "negative"])
+@pytest.mark.parametrize("route", ROUTES)
+def test_scores_far_from_zero(env, route, sign, scale, dtype):
+    # Exact scores q.k of 2^10 to 2^127.2 with 2^9 between any two: finite, while scale log2(e) times them may not be.
+    # The largest that a query sees has the weight 1, the others together at most 2^-92 of it, times values of 2^7 at most
+    # and 100 keys less than 2^-78.  A float32 sum is off by 2^-23 of itself at each of its 3 x 100 additions at most, which
+    # a bf16 output does not show.
+    fgd, torch = env
+    n, HQ, HK, count, most, spare = _route(route)
+    rng = np.random.default_rng(ROUTES.index(route))
+
+    def keys(b, k, v):
+        k.zero_()
+        for h in range(HK):
+            i = rng.permutation(106)[:len(k)]
+            size = 2.0 ** (10 + i % 53) * np.where(i < 53, 1.0, 1.5)
+            size *= rng.choice([-1, 1], len(k)) if sign == "both" else 1
+            k[:, h, 0] = torch.from_numpy(size).float().cuda()
+
+    b = Batch(env, [100 - b % 60 for b in range(n)], [count] * n, HQ, HK, 64, 16, dtype, seed=3, spare=spare, keys=keys)
+    b.q.zero_()
+    by = rng.choice([1.0, 1.5], (b.T, HQ)) * 2.0 ** rng.choice([0, 3, 64], (b.T, HQ)) * (-1 if sign == "negative" else 1)
+    b.q[..., 0] = torch.from_numpy(by).to(b.q.dtype).cuda()
+    for window in (0, 37):
+        got = _np(b.run(window, scale, max_q=most)).reshape(n, count, HQ, 64)
+        for i in range(n):
+            s = np.einsum("thd,khd->thk", _np(b.q[count * i:count * i + count]), np.repeat(b.k[i], HQ // HK, 1))
+            at = b.lens[i] - count + np.arange(count)[:, None, None]
+            key = np.arange(b.lens[i])
+            s = np.where((key <= at) & (key > at - (window or 1000)), s, -np.inf)
+            want = np.stack([b.v[i][s[:, h].argmax(-1), h // (HQ // HK)] for h in range(HQ)], 1)
+            assert abs(b.v[i]).max() <= 128
+            assert np.all(abs(got[i] - want) <= 300 * 2.0 ** -23 * abs(want) + 2.0 ** -78)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("route", ROUTES)
+def test_scales_above_one(env, route, dtype):
+    def keys(b, k, v):
+        k *= 5
+
+    n, HQ, HK, count, most, spare = _route(route)
+    b = Batch(env, [100 - b % 60 for b in range(n)], [count] * n, HQ, HK, 64, 16, dtype, seed=4, spare=spare, keys=keys)
+    for scale in (0.69, 0.7, 5.0):
+        b.check(scale=scale, max_q=most)
+    b.check(33, 1.5, max_q=most)
+
+
+def test_large_scores_and_scales_bf16(env):
+    def keys(b, k, v):
+        k *= 30
+
+    for scale in (1e-6, 0.3, 5.0):
+        Batch(env, [50, 300], [3, 1], 4, 2, 64, dtype="bf16", seed=1, keys=keys).check(scale=scale)
+
+
+@pytest.mark.parametrize("scale", [0.125, 3.0])
+@pytest.mark.parametrize("route", ROUTES)
+def test_bf16_queries_of_nan_and_infinity(env, route, scale):
+    fgd, torch = env
+    n, HQ, HK, count, most, spare = _route(route)
+    b = Batch(env, [50] * n, [count] * n, HQ, HK, 64, 16, "bf16", seed=5, spare=spare)
+    b.q[1, 2, 7] = float("nan")
+    b.q[2, 1, 9] = float("inf")
+    got = _np(b.run(scale=scale, max_q=most))
+    bad = np.zeros((b.T, HQ), bool)
+    bad[1, 2] = bad[2, 1] = True
+    assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
+    b.q[2, 1, 9] = 3e38  # finite: its scores may pass every number, the rows beside it are not touched
+    assert np.isfinite(_np(b.run(scale=scale, max_q=most))[~bad]).all()
