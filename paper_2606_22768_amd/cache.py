@@ -129,7 +129,10 @@ class Mx4Cache:
         if data is None:
             data = torch.empty(need, dtype=torch.uint8, device="cuda" if device is None else device)
         else:
-            _array("data", data, torch.uint8, data.device if device is None else torch.device(device))
+            at = data.device if device is None else torch.device(device)
+            if at.index is None and at.type == data.device.type:  # "cuda": whichever it is on
+                at = data.device
+            _array("data", data, torch.uint8, at)
             if data.numel() != need:
                 raise ValueError(f"data: expected {need} bytes, got {data.numel()}")
         self._data = data

@@ -322,6 +322,16 @@ def test_cache_tensors():
             run(**bad)
 
 
+def test_cache_of_given_data_on_a_named_device():
+    data = torch.zeros(544, dtype=torch.uint8)
+    for device in (None, "cpu", data.device):
+        c = fgd.Mx4Cache(1, 16, 1, 32, device=device, data=data)
+        assert c.data is data and c.device == data.device
+    for device in ("meta", "cuda", "cuda:0"):
+        with pytest.raises(ValueError, match="data: expected a tensor on"):
+            fgd.Mx4Cache(1, 16, 1, 32, device=device, data=data)
+
+
 # ------------------------------------------------------------------ pages
 
 def pages(page=16, requests=3, table_width=4, table_stride=4, tables=A, lengths=B, free=C, free_count=D, capacity=9):

@@ -203,3 +203,17 @@ def test_kept_data_and_streams(env):
     _same(got[0], ref.cached(_np(k)))
     again = fgd.Mx4Cache(4, 16, 2, 64, data=cache.data.clone())
     assert torch.equal(fgd.mx4_cache_read(again, slots)[0], got[0])
+
+
+def test_data_on_the_current_gpu(env):
+    fgd, torch = env
+    data = torch.empty(fgd.Mx4Cache(3, 16, 2, 64).nbytes, dtype=torch.uint8, device="cuda")
+    k = _heads(torch, 5, 2, 64, "f32")
+    slots = torch.arange(5, device="cuda") * 7
+    for device in ("cuda", "cuda:0", torch.device("cuda")):
+        cache = fgd.Mx4Cache(3, 16, 2, 64, device=device, data=data)
+        fgd.mx4_cache_write(cache, k, k, slots)
+        _same(fgd.mx4_cache_read(cache, slots)[0], ref.cached(_np(k)))
+    for device in ("cpu", "cuda:1"):
+        with pytest.raises(ValueError, match="data: expected a tensor on"):
+            fgd.Mx4Cache(3, 16, 2, 64, device=device, data=data)
