@@ -14,6 +14,7 @@ calls behave as those of mx4.py do.
 from __future__ import annotations
 
 import ctypes
+import math
 
 from . import DTYPES, FGD_F32, _check, _dev, _stream, lib
 from .heads import _array, _at, _form, _heads, _keep, _known
@@ -106,9 +107,15 @@ def fgd_truncate_pages(pages, keep, stream=None):
 
 def _int(name, v, lo, hi):
     """A whole number of a C type's range (ctypes would take its lower bits)."""
-    if not lo <= int(v) <= hi:
+    try:
+        n = int(v)
+    except (OverflowError, ValueError):  # infinity, NaN
+        n = None
+    if n is None or n != v:
+        raise ValueError(f"{name}: expected a whole number, got {v}")
+    if not lo <= n <= hi:
         raise ValueError(f"{name}: {v} is outside [{lo}, {hi}]")
-    return int(v)
+    return n
 
 
 class Mx4Cache:
@@ -312,15 +319,16 @@ def mx4_attend(q, cache, tables, lengths, starts=None, max_q=None, scale=None, w
         _heads("out", out, q)
         if out.shape != q.shape:
             raise ValueError(f"out: expected shape {tuple(q.shape)}, got {tuple(out.shape)}")
-    _on_gpu("cache", cache.data, None)
-    _on_gpu("q", q, dev)
+    window = _int("window", window, 0, math.inf)
     if starts is None:
         most = 1
     elif max_q is None:
         most = min(T, -(-2 * T // max(B, 1)))  # twice the mean
     else:
         most = min(_int("max_q", max_q, 0, 1 << 62), T)
-    sizes = fgd_attention(code, B, W, heads, _int("window", min(int(window), 0x7fffffff), 0, 0x7fffffff), T, most,
+    _on_gpu("cache", cache.data, None)
+    _on_gpu("q", q, dev)
+    sizes = fgd_attention(code, B, W, heads, min(window, 0x7fffffff), T, most,
                           cache.dim ** -0.5 if scale is None else float(scale))
     need = fgd_mx4_attend_workspace_size(cache._c, sizes)
     if workspace is not None:

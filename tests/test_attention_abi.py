@@ -2,6 +2,7 @@
 and every refusal before anything is launched (no call here reaches a
 kernel)."""
 
+import numpy as np
 import pytest
 import torch
 
@@ -330,6 +331,42 @@ def test_cache_of_given_data_on_a_named_device():
     for device in ("meta", "cuda", "cuda:0"):
         with pytest.raises(ValueError, match="data: expected a tensor on"):
             fgd.Mx4Cache(1, 16, 1, 32, device=device, data=data)
+
+
+BROKEN = [0.5, 2.9, 16.7, float("nan"), float("inf")]
+
+
+@pytest.mark.parametrize("bad", BROKEN)
+def test_sizes_that_are_no_whole_numbers(bad):
+    for at in range(4):
+        with pytest.raises(ValueError, match="whole number"):
+            fgd.Mx4Cache(*(bad if i == at else 32 for i in range(4)), device="cpu")
+    c = fgd.Mx4Cache(3, 16, 2, 64, device="cpu")
+    q, t, n = torch.zeros(3, 4, 64), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    starts = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="window: expected a whole number"):
+        fgd.mx4_attend(q, c, t, n, window=bad)
+    with pytest.raises(ValueError, match="max_q: expected a whole number"):
+        fgd.mx4_attend(q, c, t, n, starts, max_q=bad)
+    free, count = torch.zeros(9, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="page: expected a whole number"):
+        fgd.extend_pages(t, n, n, free, count, bad, 5)
+    with pytest.raises(ValueError, match="tokens: expected a whole number"):
+        fgd.extend_pages(t, n, n, free, count, 16, bad)
+    with pytest.raises(ValueError, match="page: expected a whole number"):
+        fgd.truncate_pages(t, n, n, free, count, bad)
+
+
+def test_whole_numbers_of_other_types():
+    for kind in (float, np.int64, np.float32, torch.tensor):
+        c = fgd.Mx4Cache(*map(kind, (3, 16, 2, 64)), device="cpu")
+        assert (c.pages, c.page, c.heads, c.dim) == (3, 16, 2, 64) and type(c.pages) is int
+        q, t, n = torch.zeros(3, 4, 64), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+        for window in (5, 2 ** 40):  # the checks after that of the window refuse what is not on a GPU
+            with pytest.raises(ValueError, match="on a GPU"):
+                fgd.mx4_attend(q, c, t, n, window=kind(window))
+        with pytest.raises(ValueError, match="window"):
+            fgd.mx4_attend(q, c, t, n, window=kind(-1))
 
 
 # ------------------------------------------------------------------ pages
