@@ -487,3 +487,41 @@ def test_bf16_queries_of_nan_and_infinity(env, route, scale):
     assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
     b.q[2, 1, 9] = 3e38  # finite: its scores may pass every number, the rows beside it are not touched
     assert np.isfinite(_np(b.run(scale=scale, max_q=most))[~bad]).all()
+
+
+@pytest.mark.parametrize("D, dtype", [(32, "f32"), (64, "f32"), (96, "f32"), (32, "bf16"), (64, "bf16"), (96, "bf16"),
+                                      (128, "bf16")])
+@pytest.mark.parametrize("cut", [False, True])
+def test_items_of_32_rows(env, D, dtype, cut):
+    # 8 queries of 4 heads a key head: items for 40 sequences of 4 key heads, some without a row or with one tile of
+    # two, some sequences of two items; whole, and cut between blocks where the tables are long.
+    fgd, torch = env
+    rng = np.random.default_rng(D + cut)
+    lengths = rng.integers(0, 500 if cut else 300, 40)
+    counts = rng.integers(0, 9, 40)
+    lengths[:6], counts[:6] = [1, 0, 33, 297, 64, 150], [8, 3, 1, 8, 4, 12]
+    b = Batch(env, lengths.tolist(), counts.tolist(), 16, 4, D, 16, dtype, seed=D, spare=120 if cut else 2)
+    b.check(max_q=8)
+    b.check(window=41, max_q=8)
+
+    def need(most):
+        return fgd.fgd_mx4_attend_workspace_size(b.cache._c, fgd.fgd_attention(
+            dtype, 40, b.tables.shape[1], 16, 0, b.T, most, 1.0))
+    # Whole items leave no parts; of cut ones 32 rows have their place, or 16 of them by a hint of one query. Where two
+    # blocks are launched for each one of twice the rows, both need as much.
+    if not cut:
+        assert need(8) == need(1) == 0
+    elif (D, dtype) in ((64, "f32"), (96, "bf16")):
+        assert need(8) == need(1) > 0
+    else:
+        assert need(8) > need(1) > 0
+
+
+@pytest.mark.parametrize("D, dtype", [(32, "bf16"), (128, "bf16"), (96, "f32")])
+def test_items_of_32_rows_of_long_sequences(env, D, dtype):
+    # Items of many blocks each, of one block, and blocks of several items.
+    lengths = [3000, 1, 2047, 20, 700, 2500] + [60] * 26
+    counts = [8, 1, 7, 8, 2, 5] + [6] * 26
+    b = Batch(env, lengths, counts, 16, 4, D, 16, dtype, seed=D)
+    b.check(max_q=8)
+    b.check(window=1100, max_q=8)
