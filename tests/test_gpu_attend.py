@@ -525,3 +525,28 @@ def test_items_of_32_rows_of_long_sequences(env, D, dtype):
     b = Batch(env, lengths, counts, 16, 4, D, 16, dtype, seed=D)
     b.check(max_q=8)
     b.check(window=1100, max_q=8)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 96, 128, 160, 256])
+def test_own_rows_of_long_sequences(env, D, dtype):
+    # Rows of their own in all four waves and both of their tiles, blocks of a sequence one after the other, 4 heads a
+    # key head; steps enough for every buffer to be used again, and pages past the first 64.
+    lengths = [1500, 260, 64, 1, 0, 700] + [30] * 58
+    counts = [200, 130, 33, 1, 4, 17] + [2] * 58
+    b = Batch(env, lengths, counts, 16, 4, D, 16, dtype, seed=D)
+    b.check(max_q=200)
+    b.check(window=300, max_q=200)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("HQ, HK", [(7, 1), (6, 2)])
+def test_own_rows_of_many_sequences(env, HQ, HK, dtype):
+    # Over 64 sequences, which keep their order; groups that do not divide a tile.
+    rng = np.random.default_rng(HQ)
+    lengths = rng.integers(100, 250, 100)
+    counts = rng.integers(0, 40, 100)
+    counts[::9] = 100
+    b = Batch(env, lengths.tolist(), counts.tolist(), HQ, HK, 64, 32, dtype, seed=HQ)
+    for window in (0, 50):
+        b.check(window, max_q=400)
