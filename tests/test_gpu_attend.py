@@ -550,3 +550,37 @@ def test_own_rows_of_many_sequences(env, HQ, HK, dtype):
     b = Batch(env, lengths.tolist(), counts.tolist(), HQ, HK, 64, 32, dtype, seed=HQ)
     for window in (0, 50):
         b.check(window, max_q=400)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("power", [-122, -123, -124, -125, -126])
+@pytest.mark.parametrize("route", ROUTES)
+def test_values_of_the_smallest_scales(env, route, power, dtype):
+    # Blocks of scale byte 0 (largest magnitude below 2^-124): one key is seen, its value comes out as it is held.
+    n, HQ, HK, count, most, spare = _route(route)
+
+    def keys(_, k, v):
+        v *= 2.0 ** power
+    b = Batch(env, [40] * n, [count] * n, HQ, HK, 96, 16, dtype, seed=-power, keys=keys, spare=spare)
+    got = _np(b.run(window=1, max_q=most))
+    want = np.concatenate([np.repeat(v[40 - count:], HQ // HK, 1) for v in b.v])
+    small = abs(want) < 2.0 ** -126  # numbers that a float32 sum may flush
+    assert (~small).any() and (abs(want) < 2.0 ** -124).any()
+    assert np.array_equal(np.where(small, 0, got), np.where(small, 0, want))
+    assert np.all(abs(got[small] - want[small]) < 2.0 ** -126)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("route", ROUTES)
+def test_keys_of_the_smallest_scales(env, route, dtype):
+    # Keys of 2^-126 to 2^-124 in blocks of scale byte 0 and queries of 2^123: scores of ordinary size.
+    fgd, torch = env
+    n, HQ, HK, count, most, spare = _route(route)
+
+    def keys(_, k, v):
+        k[:] = torch.where(k < 0, -1.0, 1.0) * (2.0 ** -126 * (1 + (abs(k) > 1).float() + (abs(k) > 2).float()))
+    b = Batch(env, [40] * n, [count] * n, HQ, HK, 96, 16, dtype, seed=8, keys=keys, spare=spare)
+    for k in b.k:
+        assert abs(k).min() == 2.0 ** -126 and abs(k).max() == 3 * 2.0 ** -126
+    b.q.mul_(2.0 ** 123)
+    b.check(scale=0.3, max_q=most)
