@@ -549,7 +549,9 @@ typedef struct {
  *   q_weight,        device, weight_dtype [head_dim], or of every batch
  *   k_weight         entry; NULL: no norm
  *   q_out, k_out     may be the input itself with the same strides (in
- *                    place); no other overlap
+ *                    place); no other overlap.  The two may be views of one
+ *                    array of the same strides, whose heads lie between each
+ *                    other's
  * Enqueued on `stream`. */
 fgd_status fgd_rotate_heads(const fgd_heads *sizes, const void *q, const int64_t *q_strides, const void *k,
                             const int64_t *k_strides, const int32_t *positions, const double *freqs,
@@ -561,6 +563,7 @@ fgd_status fgd_rotate_heads(const fgd_heads *sizes, const void *q, const int64_t
  * [head_dim] where batch entries share the weights: the sum over all of
  * them; else [batch][head_dim]), each given with its weight.  q and k may be
  * NULL where they have no weight.  Sums run in an order that the sizes fix.
+ * No output may overlap another array; q_grad and k_grad may be views of one.
  *   workspace   device memory of at least
  *               fgd_rotate_heads_grads_workspace_size bytes, 16-byte aligned,
  *               overlapping none of the arrays; left undefined.  Calls that

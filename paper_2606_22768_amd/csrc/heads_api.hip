@@ -50,18 +50,6 @@ struct Spans {
     void add(const void *q, int64_t bytes) { p[count] = q, n[count++] = bytes; }
 };
 
-fgd_status check_apart(const Spans &in, const Spans &out) {
-    for (int i = 0; i < out.count; ++i) {
-        for (int j = 0; j < in.count; ++j)
-            if (fgd::api_overlap(out.p[i], out.n[i], in.p[j], in.n[j]))
-                return api_fail(FGD_ERR_INVALID_ARG, "outputs and the workspace must not overlap the inputs");
-        for (int j = 0; j < i; ++j)
-            if (fgd::api_overlap(out.p[i], out.n[i], out.p[j], out.n[j]))
-                return api_fail(FGD_ERR_INVALID_ARG, "outputs and the workspace must not overlap each other");
-    }
-    return FGD_OK;
-}
-
 fgd::HeadArray array_of(const void *p, const int64_t *strides) {
     return p ? fgd::HeadArray{const_cast<void *>(p), strides[0], strides[1], strides[2]} : fgd::HeadArray{};
 }
@@ -99,6 +87,20 @@ bool heads_meet(const fgd_heads *s, const void *q, const int64_t *x, int64_t qb,
             if (v < D && v > -D) return true;
         }
     return false;
+}
+
+// That no output overlaps an input or another output.  `pair`: the first two
+// are those of q and k and have been compared by their elements.
+fgd_status check_apart(const Spans &in, const Spans &out, bool pair) {
+    for (int i = 0; i < out.count; ++i) {
+        for (int j = 0; j < in.count; ++j)
+            if (fgd::api_overlap(out.p[i], out.n[i], in.p[j], in.n[j]))
+                return api_fail(FGD_ERR_INVALID_ARG, "outputs and the workspace must not overlap the inputs");
+        for (int j = pair && i == 1 ? 1 : 0; j < i; ++j)
+            if (fgd::api_overlap(out.p[i], out.n[i], out.p[j], out.n[j]))
+                return api_fail(FGD_ERR_INVALID_ARG, "outputs and the workspace must not overlap each other");
+    }
+    return FGD_OK;
 }
 
 // The inputs that both calls have besides their heads.
@@ -174,7 +176,8 @@ fgd_status fgd_rotate_heads(const fgd_heads *sizes, const void *q, const int64_t
         in.add(q, qb);
         in.add(k, kb);
     }
-    if (fgd_status st = check_apart(in, out)) return st;
+    const bool pair = out.count == 2 && !heads_meet(sizes, q_out, q_out_strides, qob, k_out, k_out_strides, kob);
+    if (fgd_status st = check_apart(in, out, pair)) return st;
     if (q_same || k_same) {
         Spans written, rest;
         if (q_same) written.add(q_out, qob);
@@ -244,7 +247,8 @@ fgd_status fgd_rotate_heads_grads(const fgd_heads *sizes, const void *dq, const 
     out.add(q_weight_grad, grads);
     out.add(k_weight_grad, grads);
     out.add(workspace, need);
-    if (fgd_status st = check_apart(in, out)) return st;
+    const bool pair = !heads_meet(sizes, q_grad, q_grad_strides, qob, k_grad, k_grad_strides, kob);
+    if (fgd_status st = check_apart(in, out, pair)) return st;
     a.side[0].x = array_of(qb ? q : nullptr, q_strides);
     a.side[1].x = array_of(kb ? k : nullptr, k_strides);
     a.side[0].dy = array_of(dqb ? dq : nullptr, dq_strides);

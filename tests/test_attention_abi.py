@@ -34,8 +34,8 @@ def rotate(s=None, q=A, qs=SQ, k=B, ks=SK, positions=C, freqs=D, wq=E, wk=F, qo=
 
 
 def grads(dq=A, dk=B, q=I, k=J, positions=C, freqs=D, wq=E, wk=F, gq=G, gk=H, gwq=K, gwk=K + (1 << 20), work=K + (1 << 30),
-          n=1 << 24, gqs=SQ, **kw):
-    fgd.fgd_rotate_heads_grads(sizes(**kw), dq, SQ, dk, SK, q, SQ, k, SK, positions, freqs, wq, wk, gq, gqs, gk, SK, gwq,
+          n=1 << 24, gqs=SQ, gks=SK, **kw):
+    fgd.fgd_rotate_heads_grads(sizes(**kw), dq, SQ, dk, SK, q, SQ, k, SK, positions, freqs, wq, wk, gq, gqs, gk, gks, gwq,
                                gwk, work, n, 0)
 
 
@@ -100,6 +100,25 @@ def test_heads_in_place_apart(qh, kh, at, strides, batch, tokens, text):
                            q_heads=qh, k_heads=kh, batch=batch, tokens=tokens, positions=B + 64), text or "inputs")
     refused(lambda: rotate(q=B, qo=B, k=B + 4 * at, ko=H, qs=strides, qos=strides, ks=strides, kos=(1 << 20, 1 << 14, 64),
                            q_heads=qh, k_heads=kh, batch=batch, tokens=tokens, positions=B + 64), text or "inputs")
+
+
+@pytest.mark.parametrize("at, apart", [(256, True), (255, False), (257, False), (0, False), (320, False), (256 + 384, True),
+                                       (-128, True), (-127, False), (256 + 3840, True)])
+def test_gradients_between_each_other(at, apart):
+    # Gradients of 4 and 2 heads of 64 as views of one array of 6: their spans meet, their elements do or do not.
+    s = (3840, 384, 64)
+    q = {b * 3840 + t * 384 + d for b in range(2) for t in range(10) for d in range(256)}
+    k = {at + b * 3840 + t * 384 + d for b in range(2) for t in range(10) for d in range(128)}
+    assert bool(q & k) != apart
+    # A weight's gradient in place of a weight refuses what passes, so that nothing is launched.
+    refused(lambda: grads(gq=G, gk=G + 4 * at, gqs=s, gks=s, gwq=E), "the inputs" if apart else "each other")
+    refused(lambda: grads(gq=G, gk=G + 4 * at, gqs=s, gks=s, positions=G + 64), "the inputs")
+    # Of other strides they count as meeting where their spans do.
+    if abs(at) < 3840:
+        refused(lambda: grads(gq=G, gk=G + 4 * at, gqs=s, gks=(3840, 384, 128), gwq=E), "each other")
+    refused(lambda: rotate(qo=G, ko=G + 4 * at, qos=s, kos=s, positions=G + 64), "the inputs")
+    if not apart:
+        refused(lambda: rotate(qo=G, ko=G + 4 * at, qos=s, kos=s), "each other")
 
 
 def test_heads_in_place_strides():

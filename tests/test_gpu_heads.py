@@ -155,6 +155,30 @@ def test_views_of_a_projection_and_in_place(env, D, dtype):
         assert torch.equal(qkv[..., 8 * D:], before[..., 8 * D:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_outputs_that_are_views_of_one_array(env, dtype):
+    fgd, torch = env
+    D = 64
+    c = Case(env, 2, 13, 6, 2, D, D, dtype)
+    want = c.forward()
+    both = torch.full((2, 13, 10 * D), 3.0, dtype=c.q.dtype, device="cuda")
+    q, k = both[..., :6 * D].unflatten(-1, (6, D)), both[..., 6 * D:8 * D].unflatten(-1, (2, D))
+    fgd.rotate_heads(c.q, c.k, c.positions, c.freqs, *c.w, q_out=q, k_out=k)
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1]) and (both[..., 8 * D:] == 3).all()
+    with pytest.raises(fgd.FgdError, match="each other"):
+        fgd.rotate_heads(c.q, c.k, c.positions, c.freqs, *c.w, q_out=q, k_out=both[..., 1 + 5 * D:1 + 7 * D].unflatten(-1, (2, D)))
+    # The gradients too, by the C call.
+    want = fgd.rotate_heads_grads(c.dq, c.dk, c.q, c.k, c.positions, c.freqs, *c.w)
+    sizes = fgd.fgd_heads(dtype, 2, 6, 2, D, D, 0, 13, 0, D, 1e-6)
+    work = torch.empty(fgd.fgd_rotate_heads_grads_workspace_size(sizes), dtype=torch.uint8, device="cuda")
+    wq, wk = torch.empty((2, 2, D), device="cuda").unbind()
+    axes = lambda t: tuple(t.stride()[:3])  # noqa: E731
+    fgd.fgd_rotate_heads_grads(sizes, c.dq, axes(c.dq), c.dk, axes(c.dk), c.q, axes(c.q), c.k, axes(c.k), c.positions,
+                               c.freqs, *c.w, q, axes(q), k, axes(k), wq, wk, work, work.numel(),
+                               torch.cuda.current_stream().cuda_stream)
+    assert all(torch.equal(a, b) for a, b in zip((q, k, wq, wk), want)) and (both[..., 8 * D:] == 3).all()
+
+
 def test_positions_of_every_batch_entry(env):
     fgd, torch = env
     c = Case(env, 3, 8, 2, 1, 64, 64, "f32")
