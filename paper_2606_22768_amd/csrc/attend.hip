@@ -98,7 +98,9 @@ __device__ inline f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
                                                    0, 0);
 }
 
-// Byte i of w as the float32 2^(byte - 127).
+// Byte i of w as the float32 2^(byte - 127), a scale operand.  Byte 0 gives
+// 0.0: the conversions look at an operand's exponent field alone and take it
+// as 2^-127, which the tests of the smallest scales pin.
 __device__ inline float scale_of(uint32_t w, int i) {
     return __uint_as_float((i < 3 ? w << (23 - 8 * i) : w >> 1) & 0x7f800000u);
 }
@@ -472,7 +474,10 @@ struct Place {
 };
 
 // Waves of a SIMD that the registers are kept few enough for: a row tile's
-// sums and queries, a step's codes and scales, and about 70 more.
+// sums and queries, a step's codes and scales, and about 70 more.  An estimate:
+// rows_kernel keeps 11 registers of a lane in memory for bf16 heads of 32 and
+// 160 and f32 heads of 96, 3 for f32 heads of 192, line_kernel one for f32 heads
+// of 32 in items of 32 that are cut.
 template <typename T, int NB, int R>
 constexpr int kRegisters = R * NB * (8 + 4 * Parts<T>::q) + 6 * NB + 60 + 10 * R;
 template <typename T, int NB, int R>
@@ -648,7 +653,7 @@ struct Share {
 // LDS.  The scores of a step are computed beside the weights of the one
 // before, and the next operands converted beside the second product; what is
 // converted was read two steps before.  4 x 512 queries, 32 heads of 128 over
-// 8 of up to 8192 keys in 282 us, 695 TFLOP/s (before later steps, 345: every
+// 8 of up to 8192 keys in 276 us, 706 TFLOP/s (before later steps, 345: every
 // wave converting for itself: 428; in the sequences' order: 393).  Bound by
 // the instructions of weights, conversion and products, of which two waves on
 // a SIMD hide little of each other's.
@@ -810,18 +815,20 @@ __device__ inline void outstanding() {
 // keys.  Each of `count` blocks takes an equal stretch of it, whatever the
 // sequences' lengths.  Beginning an item and joining its waves takes a block
 // about as long as kItemCost steps, which stand before its first one in the
-// line (without them 64 sequences of 500 to 8192 keys: blocks done after 55
-// to 106 us).
+// line (without them, in an earlier state, 64 sequences of 500 to 8192 keys:
+// blocks done after 55 to 106 us).
 struct Line {
     int64_t total;  // steps
     int count;      // blocks
     __device__ int64_t from(int i) const { return total * i / count; }
     __device__ int block_of(int64_t w) const { return static_cast<int>(((w + 1) * count - 1) / total); }
 };
-constexpr int kItemCost = 16;  // 64 sequences of 500 to 8192 keys: 86 us (8: 90, 12: 87, 24: 87, 40: 94)
+// 64 sequences of 500 to 8192 keys: 73.7 us (8: 77.1, 12: 74.0, 24: 72.8, 40:
+// 75.0); one of 65 536: 28.5 (24 and 40: 29.3).
+constexpr int kItemCost = 16;
 // The least stretch of a block: short calls have fewer blocks, each of which
 // costs the rest a part to join (17 sequences of up to 3001 keys, 5 queries
-// and a window of 1000: 13 us; 4: 14, 16: 15, 40: 23).
+// and a window of 1000: 15.0 us; 4: 15.9, 16: 16.6, 40: 24.2).
 constexpr int kLeast = 8;
 
 // A number that is one for the wave, in a scalar register.
@@ -832,7 +839,10 @@ __device__ inline int64_t uniform(int64_t v) {
 }
 
 // An item's length for sequence s (a step where its rows see no key: they are
-// written as well), and its items.
+// written as well), and its items.  All items of a sequence run the steps that
+// any of its rows sees, so that an item's place in the line is a product: a
+// prompt from its first token runs twice the steps that its rows see, 512
+// queries with a window of 128 four times.
 __device__ inline int length_of(const AttendArgs &a, const Span &s) {
     const Keys k = keys_of(a, s, 0, s.n - 1);
     return kItemCost + (k.lo < k.hi ? (k.hi + kTile - 1) / kTile - k.lo / kTile : 1);

@@ -6,16 +6,20 @@
 // dy: dw = sum over tokens and heads of g x r, and dx = r (g w - n mean(g w n)),
 // n = x r.  Without w there is no norm: y = R x, dx = g.
 //
-// Bound by memory: every element is read once and written once.  A head lies
-// in a group of lanes (a power of two), four pairs to a lane, so that a
+// Every element is read once and written once.  A head lies in a group of lanes (a power of two), four pairs to a lane, so that a
 // rotation stays in a lane and a norm's sum crosses the group alone; a
 // block's tokens share their angles, which one thread each works out in
 // float64 (a position of 10^6 has 4 digits left of a float32 angle).
-// 4 x 2048 tokens of 32 + 8 heads of 128 in bf16: 46 us, 3.6 TB/s; the gradients
-// 79, 3.5 TB/s, at four waves on a SIMD, and 5 for the weights' sums (held in
-// registers over a block's tokens; read anew for each side of queries and keys:
-// 53 and 87 us, registers spilled).  A call of 64 tokens takes 8 us, its
-// latency: angles, then elements, then sums across a group.
+// 4 x 2048 tokens of 32 + 8 heads of 128 in bf16: 46 us, 3.6 TB/s of a copy's
+// 5.35; without a rotation, and so without angles and their barrier, 45.  The
+// gradients take 78 us, 3.5 TB/s, and 5 for the weights' sums.  They keep
+// weights and sums in registers over a block's tokens, which at four waves on a
+// SIMD leaves 10 of a lane's registers (f32: 14) in memory: 95 MB are written
+// for 84 of outputs (weights read anew for each side of queries and keys, which
+// spilled as well: 53 and 87 us).  Heads or rotated parts that are no multiples
+// of 8 go element by element: 8192 tokens of 40 heads of 80, 20 of them rotated,
+// take 64 us, all 80 rotated 34.  A call of 64 tokens takes 8 us (without a
+// rotation 7), its latency: angles, then elements, then sums across a group.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
